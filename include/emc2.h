@@ -3,7 +3,8 @@
  *   multi-scale voxelization  ->  27-offset kernel map  ->  sparse 3D conv (+ fused affine/ReLU)
  *   ->  point-to-image projection with bilinear feature gather,
  * and on the same data structures: inverse kernel map + bird's-eye-view flattening (decoder side),
- * Multiscale Pooling of image features + multimodal fusion, the scene dispatcher, an int8 sparse conv.
+ * Multiscale Pooling of image features + multimodal fusion, the scene dispatcher, an int8 sparse conv, and operators that mix
+ * along the voxels of whole frames: layer norm, a gated linear recurrence, a gated feed-forward network, with their gradients.
  *
  * Conventions
  *   - Pointers named d_* are DEVICE pointers (HBM, on the context's device); h_* and plain
@@ -472,6 +473,90 @@ emc2_status emc2_project_gather(emc2_ctx* ctx, const float* d_points, int32_t st
                                 int64_t n_points, const float P[12], const void* d_img, int32_t H,
                                 int32_t W, int32_t C, void* d_out, uint8_t* d_valid, float* d_uv,
                                 void* stream);
+
+/*
+ * Sequence operators over the rows of packed frames (the paper's experts build on 3D CNN backbones, Sec. 3.3, which see a neighbourhood of
+ * 27 cells; these mix along a frame's whole list of voxels.  The operators are the library's own addition): layer norm, a gated linear
+ * recurrence and a gated feed-forward network, each with its gradients, of F32, F16 or BF16 rows.
+ *   - Rows lie `ld_*` elements apart (>= channels), so that a slice of wider rows can be an operand; pointers must be aligned to their
+ *     element.  Where all rows of a call begin at multiples of 16 bytes and hold a multiple of 16 bytes, rows move in 16-byte pieces,
+ *     else value by value.
+ *   - `d_n` (device int32, or NULL): rows present, of `capacity` at most; rows beyond are neither read nor written.
+ *   - Parameters and states of float* are fp32 whatever the rows' type; sums are fp32; each result is rounded once, to nearest even.
+ *   - Results may lie where inputs of the same call do, if pointer and pitch are the same; otherwise they must not overlap.
+ *   - d_work: caller's scratch, 16-byte aligned, of at least emc2_*_work bytes; its contents need not be kept between calls.  The calls touch
+ *     no mutable context state but the status word and may run on several streams at once, each with a d_work of its own.
+ *   - Results do not depend on the run: no sum is taken in an order that may change.
+ * The *_work and *_size calls are host-only queries; -1 for arguments that the call itself would refuse.
+ */
+
+/* First row of every frame: d_offsets[b] = number of rows of d_coords [capacity][4] (b, z, y, x), sorted by b as every voxel list here is, whose
+ * frame is below b, for b in [0, n_batch); d_offsets[0] = 0 and d_offsets[n_batch] = the rows present.  d_coords 16-byte aligned. */
+emc2_status emc2_frame_offsets(emc2_ctx* ctx, const int32_t* d_coords, const int32_t* d_n, int64_t capacity, int32_t n_batch,
+                               int32_t* d_offsets, void* stream);
+
+/*
+ * Layer norm over the channels of each row:
+ *   s = x (+ res);  y = (s - mean(s)) / sqrt(var(s) + eps) * gamma + beta,   var the mean of the squared differences
+ * d_res NULL: no residual.  d_sum (may be NULL, needs d_res): receives s, rounded; y is taken from s before that.  channels in [1, 1024].
+ */
+emc2_status emc2_layernorm(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_res, int64_t ld_res,
+                           const float* d_gamma, const float* d_beta, float eps, const int32_t* d_n, int64_t capacity, int32_t channels,
+                           void* d_sum, int64_t ld_sum, void* d_y, int64_t ld_y, void* stream);
+/* Its gradients for dy: dx (+ add: the gradient that reaches x on another way, may be NULL), dgamma and dbeta [channels] summed over the rows.
+ * x is what was normalised (d_sum of the forward call, if it had a residual). */
+int64_t emc2_layernorm_work(emc2_dtype dtype, int64_t capacity, int32_t channels);
+emc2_status emc2_layernorm_backward(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_dy, int64_t ld_dy,
+                                    const void* d_add, int64_t ld_add, const float* d_gamma, float eps, const int32_t* d_n, int64_t capacity,
+                                    int32_t channels, void* d_dx, int64_t ld_dx, float* d_dgamma, float* d_dbeta, void* d_work,
+                                    int64_t work_bytes, void* stream);
+
+/*
+ * Gated linear recurrence along the rows of every sequence, per channel:
+ *   a_t = 1 / (1 + exp(-gate_t));  h_t = a_t h_{t-1} + (1 - a_t) x_t;  y_t = h_t
+ * Sequence s has rows [d_offsets[s], d_offsets[s + 1]) (device int32 [n_seq + 1], rising from 0; emc2_frame_offsets makes them); sequences
+ * may be empty.  d_offsets[n_seq] is the number of rows, of `capacity` at most (EMC2_ERR_CAPACITY through the status word if it is more; the
+ * rows beyond are then left out).  backwards != 0: every sequence is walked from its last row to its first.
+ *   d_h0 [n_seq][channels] states before the first row, NULL = zeros; d_last [n_seq][channels] receives the states after the last
+ *   (an empty sequence's is its d_h0), NULL to skip.  d_last must not overlap d_h0 (nor d_dh0 d_dlast below).
+ * The states are fp32 throughout; what an infinity or NaN in x or gate makes of a sequence stays within it and its channel.
+ */
+int64_t emc2_recurrence_work(emc2_dtype dtype, int64_t capacity, int32_t channels);
+emc2_status emc2_recurrence(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate,
+                            const int32_t* d_offsets, int32_t n_seq, int64_t capacity, int32_t channels, int32_t backwards,
+                            const float* d_h0, void* d_y, int64_t ld_y, float* d_last, void* d_work, int64_t work_bytes, void* stream);
+/* Its gradients for dy and d_dlast [n_seq][channels] (of the last states, NULL = zeros): dx, dgate and d_dh0 [n_seq][channels] (NULL to skip).
+ * The states are computed again; nothing but the call's own inputs is needed. */
+emc2_status emc2_recurrence_backward(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate,
+                                     const int32_t* d_offsets, int32_t n_seq, int64_t capacity, int32_t channels, int32_t backwards,
+                                     const float* d_h0, const void* d_dy, int64_t ld_dy, const float* d_dlast, void* d_dx, int64_t ld_dx,
+                                     void* d_dgate, int64_t ld_dgate, float* d_dh0, void* d_work, int64_t work_bytes, void* stream);
+/* The recurrence for one row per sequence (serving a stream): d_h_out = a d_h + (1 - a) x, [rows][channels] fp32 (d_h_out may be d_h), y the same rounded. */
+emc2_status emc2_recurrence_step(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate,
+                                 const float* d_h, int64_t rows, int32_t channels, float* d_h_out, void* d_y, int64_t ld_y, void* stream);
+
+/*
+ * Gated feed-forward network per row:
+ *   y = (act(x Wg) * (x Wu)) Wd (+ res);   x, y [n][channels], Wg and Wu [channels][hidden], Wd [hidden][channels], all of `dtype`
+ *   act: EMC2_ACT_SILU g / (1 + exp(-g)); EMC2_ACT_GELU its tanh form 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
+ * The products run on the matrix cores with fp32 sums; the hidden values act * up are rounded to `dtype` between them (as are their gradients in
+ * the backward pass) and never leave the chip.  channels in [1, 256], hidden in [1, 65536].
+ * emc2_ffn_pack: the three weights, contiguous, re-ordered into matrix-core fragments: d_packed [emc2_ffn_packed_size] values of `dtype`,
+ * 16-byte aligned; once per model for serving, after every change of the weights in training.
+ */
+typedef enum { EMC2_ACT_SILU = 0, EMC2_ACT_GELU = 1 } emc2_activation;
+int64_t emc2_ffn_packed_size(emc2_dtype dtype, int32_t channels, int32_t hidden);
+emc2_status emc2_ffn_pack(emc2_ctx* ctx, emc2_dtype dtype, const void* d_wg, const void* d_wu, const void* d_wd, int32_t channels,
+                          int32_t hidden, void* d_packed, void* stream);
+emc2_status emc2_ffn(emc2_ctx* ctx, emc2_dtype dtype, int32_t activation, const void* d_x, int64_t ld_x, const void* d_packed,
+                     const void* d_res, int64_t ld_res, const int32_t* d_n, int64_t capacity, int32_t channels, int32_t hidden, void* d_y,
+                     int64_t ld_y, void* stream);
+/* Its gradients for dy: dx, and dWg, dWu, dWd summed over the rows, in the weights' type and shapes (contiguous). */
+int64_t emc2_ffn_work(emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t hidden);
+emc2_status emc2_ffn_backward(emc2_ctx* ctx, emc2_dtype dtype, int32_t activation, const void* d_x, int64_t ld_x, const void* d_packed,
+                              const void* d_dy, int64_t ld_dy, const int32_t* d_n, int64_t capacity, int32_t channels, int32_t hidden,
+                              void* d_dx, int64_t ld_dx, void* d_dwg, void* d_dwu, void* d_dwd, void* d_work, int64_t work_bytes,
+                              void* stream);
 
 #ifdef __cplusplus
 }

@@ -24,6 +24,7 @@ SUBM, STRIDED = 0, 1
 EPI_NONE, EPI_AFFINE, EPI_AFFINE_RELU = 0, 1, 2
 W_PLAIN, W_PACKED = 0, 1
 POOL_MEAN, POOL_MAX = 0, 1
+ACT_SILU, ACT_GELU = 0, 1
 MAP_ANY = -1   # emc2_spconv map_hint: SUBM / STRIDED as passed to build_kmap, or unknown
 
 _TORCH_DTYPE = {F32: torch.float32, F16: torch.float16, BF16: torch.bfloat16}
@@ -32,7 +33,10 @@ EXPORTS = ["emc2_create", "emc2_destroy", "emc2_status_sync", "emc2_last_error",
            "emc2_build_kmap", "emc2_spconv", "emc2_project_gather", "emc2_pack_weights", "emc2_spconv_uses_mfma",
            "emc2_spconv_kernel", "emc2_build_inverse_kmap", "emc2_bev_flatten", "emc2_pool_image", "emc2_fuse", "emc2_dispatch", "emc2_spconv_i8_supported",
            "emc2_quantize_i8", "emc2_pack_weights_i8", "emc2_spconv_i8", "emc2_build_kmap_static", "emc2_group_points", "emc2_quantize_e4m3", "emc2_spconv_e4m3",
-           "emc2_build_stacks", "emc2_spconv_list", "emc2_group_slots"]
+           "emc2_build_stacks", "emc2_spconv_list", "emc2_group_slots",
+           "emc2_frame_offsets", "emc2_layernorm", "emc2_layernorm_work", "emc2_layernorm_backward", "emc2_recurrence", "emc2_recurrence_work",
+           "emc2_recurrence_backward", "emc2_recurrence_step", "emc2_ffn_packed_size", "emc2_ffn_pack", "emc2_ffn", "emc2_ffn_work",
+           "emc2_ffn_backward"]
 
 
 class Emc2Error(RuntimeError):
@@ -148,6 +152,34 @@ def load_library() -> ctypes.CDLL:
     lib.emc2_build_inverse_kmap.argtypes = [vp, vp, vp, i64, ctypes.POINTER(i32), i32, i32, vp, vp, vp]
     lib.emc2_bev_flatten.restype = ctypes.c_int
     lib.emc2_bev_flatten.argtypes = [vp, ctypes.c_int, vp, vp, vp, i64, ctypes.POINTER(i32), i32, i32, vp, vp]
+    f32 = ctypes.c_float
+    lib.emc2_frame_offsets.restype = ctypes.c_int
+    lib.emc2_frame_offsets.argtypes = [vp, vp, vp, i64, i32, vp, vp]
+    lib.emc2_layernorm.restype = ctypes.c_int
+    lib.emc2_layernorm.argtypes = [vp, ctypes.c_int, vp, i64, vp, i64, vp, vp, f32, vp, i64, i32, vp, i64, vp, i64, vp]
+    lib.emc2_layernorm_work.restype = i64
+    lib.emc2_layernorm_work.argtypes = [ctypes.c_int, i64, i32]
+    lib.emc2_layernorm_backward.restype = ctypes.c_int
+    lib.emc2_layernorm_backward.argtypes = [vp, ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, f32, vp, i64, i32, vp, i64, vp, vp, vp, i64, vp]
+    lib.emc2_recurrence.restype = ctypes.c_int
+    lib.emc2_recurrence.argtypes = [vp, ctypes.c_int, vp, i64, vp, i64, vp, i32, i64, i32, i32, vp, vp, i64, vp, vp, i64, vp]
+    lib.emc2_recurrence_work.restype = i64
+    lib.emc2_recurrence_work.argtypes = [ctypes.c_int, i64, i32]
+    lib.emc2_recurrence_backward.restype = ctypes.c_int
+    lib.emc2_recurrence_backward.argtypes = [vp, ctypes.c_int, vp, i64, vp, i64, vp, i32, i64, i32, i32, vp, vp, i64, vp, vp, i64, vp, i64, vp,
+                                             vp, i64, vp]
+    lib.emc2_recurrence_step.restype = ctypes.c_int
+    lib.emc2_recurrence_step.argtypes = [vp, ctypes.c_int, vp, i64, vp, i64, vp, i64, i32, vp, vp, i64, vp]
+    lib.emc2_ffn_packed_size.restype = i64
+    lib.emc2_ffn_packed_size.argtypes = [ctypes.c_int, i32, i32]
+    lib.emc2_ffn_pack.restype = ctypes.c_int
+    lib.emc2_ffn_pack.argtypes = [vp, ctypes.c_int, vp, vp, vp, i32, i32, vp, vp]
+    lib.emc2_ffn.restype = ctypes.c_int
+    lib.emc2_ffn.argtypes = [vp, ctypes.c_int, i32, vp, i64, vp, vp, i64, vp, i64, i32, i32, vp, i64, vp]
+    lib.emc2_ffn_work.restype = i64
+    lib.emc2_ffn_work.argtypes = [ctypes.c_int, i64, i32, i32]
+    lib.emc2_ffn_backward.restype = ctypes.c_int
+    lib.emc2_ffn_backward.argtypes = [vp, ctypes.c_int, i32, vp, i64, vp, vp, i64, vp, i64, i32, i32, vp, i64, vp, vp, vp, vp, i64, vp]
     _lib = lib
     return lib
 
@@ -163,6 +195,42 @@ def _stream() -> ctypes.c_void_p:
 def _dev_check(t: torch.Tensor, dtype: torch.dtype, name: str) -> None:
     if not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name}: need a contiguous {dtype} device tensor, got {t.dtype} on {t.device}")
+
+
+def _rows_check(t: torch.Tensor, dtype: torch.dtype, like: Tuple[int, int], name: str) -> int:
+    """Rows of a sequence operator: [n][channels] with neighbouring channels, rows any distance apart; returns that distance."""
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or tuple(t.shape) != like:
+        raise ValueError(f"{name}: need a {dtype} device tensor {like}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.numel() == 0:
+        return like[1]
+    ld, step = t.stride()
+    if (step != 1 and like[1] > 1) or (ld < like[1] and like[0] > 1):
+        raise ValueError(f"{name}: channels of a row must be neighbours and rows must not overlap, got strides {t.stride()}")
+    return max(ld, like[1])
+
+
+def _params_check(t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...], name: str) -> None:
+    if t is not None:
+        _dev_check(t, dtype, name)
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: need {shape}, got {tuple(t.shape)}")
+
+
+def _count_check(n: Optional[torch.Tensor]) -> None:
+    if n is not None:
+        _dev_check(n, torch.int32, "n")
+        if n.numel() < 1:
+            raise ValueError("n: need one count")
+
+
+def _work_check(work: torch.Tensor, need: int) -> int:
+    """Bytes of a work buffer; `need`: what the library's query says."""
+    if not work.is_cuda or not work.is_contiguous():
+        raise ValueError(f"work: need a contiguous device tensor, got {work.device}")
+    size = work.numel() * work.element_size()
+    if size < need:
+        raise ValueError(f"work: {size} bytes, {need} are needed")
+    return size
 
 
 _SHAPE_TYPE_PLACE = operator.attrgetter("shape", "dtype", "is_cuda")
@@ -598,3 +666,126 @@ class Context:
         pm = (ctypes.c_float * 12)(*[float(v) for v in pmat])
         self._chk(self.lib.emc2_project_gather(self.h, _ptr(points), stride, n, pm, _ptr(img), h, w, c, _ptr(out),
                                                _ptr(valid), _ptr(uv), _stream()))
+
+    # ------------------------------------------------------------------------------------------
+    # sequence operators: rows [n][channels], any distance apart, of packed frames
+    def frame_offsets(self, coords: torch.Tensor, n: Optional[torch.Tensor], capacity: int, n_batch: int, offsets: torch.Tensor) -> None:
+        """offsets[n_batch + 1] = first row of every frame of a voxel list, and the number of rows."""
+        _dev_check(coords, torch.int32, "coords")
+        _dev_check(offsets, torch.int32, "offsets")
+        _count_check(n)
+        if coords.numel() < 4 * capacity or offsets.numel() < n_batch + 1:
+            raise ValueError("coords smaller than capacity or offsets smaller than n_batch + 1")
+        self._chk(self.lib.emc2_frame_offsets(self.h, _ptr(coords), _ptr(n), capacity, n_batch, _ptr(offsets), _stream()))
+
+    def layernorm(self, dtype: int, x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float, y: torch.Tensor,
+                  residual: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None) -> None:
+        """y = layer norm of x (+ residual, the sum going to `total` if it is given); n: device count of the rows present."""
+        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
+        ld = [_rows_check(t, td, like, nm) if t is not None else 0
+              for t, nm in ((x, "x"), (residual, "residual"), (total, "total"), (y, "y"))]
+        _params_check(gamma, torch.float32, like[1:], "gamma")
+        _params_check(beta, torch.float32, like[1:], "beta")
+        _count_check(n)
+        self._chk(self.lib.emc2_layernorm(self.h, dtype, _ptr(x), ld[0], _ptr(residual), ld[1], _ptr(gamma), _ptr(beta), eps, _ptr(n), like[0],
+                                          like[1], _ptr(total), ld[2], _ptr(y), ld[3], _stream()))
+
+    def layernorm_work(self, dtype: int, capacity: int, channels: int) -> int:
+        return self.lib.emc2_layernorm_work(dtype, capacity, channels)
+
+    def layernorm_backward(self, dtype: int, x: torch.Tensor, gamma: torch.Tensor, eps: float, dy: torch.Tensor, dx: torch.Tensor,
+                           dgamma: torch.Tensor, dbeta: torch.Tensor, work: torch.Tensor, add: Optional[torch.Tensor] = None,
+                           n: Optional[torch.Tensor] = None) -> None:
+        """dx (+ add), dgamma, dbeta of a layer norm of x for dy."""
+        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
+        ld = [_rows_check(t, td, like, nm) if t is not None else 0 for t, nm in ((x, "x"), (dy, "dy"), (add, "add"), (dx, "dx"))]
+        for t, nm in ((gamma, "gamma"), (dgamma, "dgamma"), (dbeta, "dbeta")):
+            _params_check(t, torch.float32, like[1:], nm)
+        _count_check(n)
+        size = _work_check(work, self.lib.emc2_layernorm_work(dtype, *like))
+        self._chk(self.lib.emc2_layernorm_backward(self.h, dtype, _ptr(x), ld[0], _ptr(dy), ld[1], _ptr(add), ld[2], _ptr(gamma), eps, _ptr(n),
+                                                   like[0], like[1], _ptr(dx), ld[3], _ptr(dgamma), _ptr(dbeta), _ptr(work), size, _stream()))
+
+    def recurrence_work(self, dtype: int, capacity: int, channels: int) -> int:
+        return self.lib.emc2_recurrence_work(dtype, capacity, channels)
+
+    def recurrence(self, dtype: int, x: torch.Tensor, gate: torch.Tensor, offsets: torch.Tensor, y: torch.Tensor, work: torch.Tensor,
+                   backwards: bool = False, h0: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None) -> None:
+        """y_t = h_t = a_t h_{t-1} + (1 - a_t) x_t along every sequence, a = sigmoid(gate); offsets [sequences + 1] device int32."""
+        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
+        ld = [_rows_check(t, td, like, nm) for t, nm in ((x, "x"), (gate, "gate"), (y, "y"))]
+        _dev_check(offsets, torch.int32, "offsets")
+        n_seq = offsets.numel() - 1
+        _params_check(h0, torch.float32, (n_seq, like[1]), "h0")
+        _params_check(last, torch.float32, (n_seq, like[1]), "last")
+        size = _work_check(work, self.lib.emc2_recurrence_work(dtype, *like))
+        self._chk(self.lib.emc2_recurrence(self.h, dtype, _ptr(x), ld[0], _ptr(gate), ld[1], _ptr(offsets), n_seq, like[0], like[1],
+                                           int(bool(backwards)), _ptr(h0), _ptr(y), ld[2], _ptr(last), _ptr(work), size, _stream()))
+
+    def recurrence_backward(self, dtype: int, x: torch.Tensor, gate: torch.Tensor, offsets: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor,
+                            dgate: torch.Tensor, work: torch.Tensor, backwards: bool = False, h0: Optional[torch.Tensor] = None,
+                            dlast: Optional[torch.Tensor] = None, dh0: Optional[torch.Tensor] = None) -> None:
+        """dx, dgate and dh0 of a recurrence over x and gate, for dy and the gradient of the last states."""
+        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
+        ld = [_rows_check(t, td, like, nm) for t, nm in ((x, "x"), (gate, "gate"), (dy, "dy"), (dx, "dx"), (dgate, "dgate"))]
+        _dev_check(offsets, torch.int32, "offsets")
+        n_seq = offsets.numel() - 1
+        for t, nm in ((h0, "h0"), (dlast, "dlast"), (dh0, "dh0")):
+            _params_check(t, torch.float32, (n_seq, like[1]), nm)
+        size = _work_check(work, self.lib.emc2_recurrence_work(dtype, *like))
+        self._chk(self.lib.emc2_recurrence_backward(self.h, dtype, _ptr(x), ld[0], _ptr(gate), ld[1], _ptr(offsets), n_seq, like[0], like[1],
+                                                    int(bool(backwards)), _ptr(h0), _ptr(dy), ld[2], _ptr(dlast), _ptr(dx), ld[3], _ptr(dgate),
+                                                    ld[4], _ptr(dh0), _ptr(work), size, _stream()))
+
+    def recurrence_step(self, dtype: int, x: torch.Tensor, gate: torch.Tensor, h: torch.Tensor, h_out: torch.Tensor, y: torch.Tensor) -> None:
+        """One row per sequence: h_out = a h + (1 - a) x (h_out may be h), y the same rounded."""
+        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
+        ld = [_rows_check(t, td, like, nm) for t, nm in ((x, "x"), (gate, "gate"), (y, "y"))]
+        _params_check(h, torch.float32, like, "h")
+        _params_check(h_out, torch.float32, like, "h_out")
+        self._chk(self.lib.emc2_recurrence_step(self.h, dtype, _ptr(x), ld[0], _ptr(gate), ld[1], _ptr(h), like[0], like[1], _ptr(h_out), _ptr(y),
+                                                ld[2], _stream()))
+
+    def ffn_packed_size(self, dtype: int, channels: int, hidden: int) -> int:
+        """Values of the packed weights of a gated feed-forward network."""
+        return self.lib.emc2_ffn_packed_size(dtype, channels, hidden)
+
+    def ffn_pack(self, dtype: int, wg: torch.Tensor, wu: torch.Tensor, wd: torch.Tensor, packed: torch.Tensor) -> None:
+        """wg, wu [channels][hidden], wd [hidden][channels] -> packed, in matrix-core fragment order."""
+        td, (c, f) = _TORCH_DTYPE[dtype], tuple(wg.shape)
+        for t, shape, nm in ((wg, (c, f), "wg"), (wu, (c, f), "wu"), (wd, (f, c), "wd")):
+            _params_check(t, td, shape, nm)
+        self._packed_check(packed, dtype, c, f)
+        self._chk(self.lib.emc2_ffn_pack(self.h, dtype, _ptr(wg), _ptr(wu), _ptr(wd), c, f, _ptr(packed), _stream()))
+
+    def _packed_check(self, packed: torch.Tensor, dtype: int, c: int, f: int) -> None:
+        _dev_check(packed, _TORCH_DTYPE[dtype], "packed")
+        if packed.numel() < self.lib.emc2_ffn_packed_size(dtype, c, f):
+            raise ValueError("packed: smaller than ffn_packed_size")
+
+    def ffn(self, dtype: int, activation: int, x: torch.Tensor, packed: torch.Tensor, hidden: int, y: torch.Tensor,
+            residual: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None) -> None:
+        """y = (act(x wg) * (x wu)) wd (+ residual); packed: ffn_pack's; n: device count of the rows present."""
+        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
+        ld = [_rows_check(t, td, like, nm) if t is not None else 0 for t, nm in ((x, "x"), (residual, "residual"), (y, "y"))]
+        _count_check(n)
+        self._packed_check(packed, dtype, like[1], hidden)
+        self._chk(self.lib.emc2_ffn(self.h, dtype, activation, _ptr(x), ld[0], _ptr(packed), _ptr(residual), ld[1], _ptr(n), like[0], like[1],
+                                    hidden, _ptr(y), ld[2], _stream()))
+
+    def ffn_work(self, dtype: int, capacity: int, channels: int, hidden: int) -> int:
+        return self.lib.emc2_ffn_work(dtype, capacity, channels, hidden)
+
+    def ffn_backward(self, dtype: int, activation: int, x: torch.Tensor, packed: torch.Tensor, hidden: int, dy: torch.Tensor, dx: torch.Tensor,
+                     dwg: torch.Tensor, dwu: torch.Tensor, dwd: torch.Tensor, work: torch.Tensor, n: Optional[torch.Tensor] = None) -> None:
+        """dx and the weights' gradients of ffn for dy."""
+        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
+        ld = [_rows_check(t, td, like, nm) for t, nm in ((x, "x"), (dy, "dy"), (dx, "dx"))]
+        c = like[1]
+        for t, shape, nm in ((dwg, (c, hidden), "dwg"), (dwu, (c, hidden), "dwu"), (dwd, (hidden, c), "dwd")):
+            _params_check(t, td, shape, nm)
+        _count_check(n)
+        self._packed_check(packed, dtype, c, hidden)
+        size = _work_check(work, self.lib.emc2_ffn_work(dtype, like[0], c, hidden))
+        self._chk(self.lib.emc2_ffn_backward(self.h, dtype, activation, _ptr(x), ld[0], _ptr(packed), _ptr(dy), ld[1], _ptr(n), like[0], c, hidden,
+                                             _ptr(dx), ld[2], _ptr(dwg), _ptr(dwu), _ptr(dwd), _ptr(work), size, _stream()))

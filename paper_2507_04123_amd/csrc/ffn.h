@@ -1,0 +1,147 @@
+// Gated feed-forward network: the matrix-core fragments that its forward pass (ffn.hip) and its gradients (ffn_grad.hip) share.
+//   G = x Wg, U = x Wu, H = act(G) * U, y = H Wd;   x [n][C], Wg and Wu [C][F], Wd [F][C]
+// Everything is computed in tiles of 32 rows (voxels) by 32 hidden units with v_mfma_f32_32x32 (16 products deep for 16-bit values, 2
+// for fp32).  A fragment is what one lane group of 64 holds of a 32-wide operand: lane l holds line l % 32 and, of the KF values
+// along the contraction, PER = 16 bytes' worth: with half = l / 32 those at PER * half + e (e = 0 .. PER - 1).
+// A result tile leaves lane l with column l % 32 and rows 8 j + 4 half + i in register 4 j + i.  Read as a fragment, its registers
+// PER m .. PER m + PER - 1 are values hidden_of(m, half, e) along its rows: a product's result is the next product's operand
+// without leaving the registers, if the other operand (packed weights) has its values in that order.  So H, dG and dU never leave the chip.
+#pragma once
+#include "rows.h"
+
+template <typename T> struct emc2_tile {
+  static constexpr int kPer = 16 / sizeof(T);       // values of a fragment in a lane
+  static constexpr int kDeep = 2 * kPer;            // and along the contraction (KF)
+  typedef emc2_vec<T, kPer> frag;
+};
+typedef emc2_fvec<16> emc2_acc;
+
+template <typename T> __device__ __forceinline__ emc2_acc emc2_mma(emc2_vec<T, 16 / sizeof(T)> a, emc2_vec<T, 16 / sizeof(T)> b, emc2_acc c) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  } else if constexpr (__is_same(T, _Float16)) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+}
+
+// Place along a result tile's rows of value e of fragment m made of its registers.
+template <typename T> __host__ __device__ __forceinline__ constexpr int emc2_hidden_of(int m, int half, int e) {
+  return emc2_tile<T>::kDeep * m + 8 * (e / 4) + 4 * half + e % 4;
+}
+
+// Packed weights: for every slice of 32 hidden units six groups of width / KF fragments (width: C rounded up to 32s, zeros beyond C and F):
+enum emc2_ffn_group {
+  EMC2_FFN_GATE,        // Wg: line = hidden unit, along = channel
+  EMC2_FFN_UP,          // Wu: the same
+  EMC2_FFN_DOWN,        // Wd: line = channel (fragment ct * 32 / KF + m: channels 32 ct ..), along = hidden units in the order of a result tile
+  EMC2_FFN_DOWN_T,      // Wd: line = hidden unit, along = channel
+  EMC2_FFN_GATE_T,      // Wg: line = channel, along = hidden units in the order of a result tile
+  EMC2_FFN_UP_T,        // Wu: the same
+  EMC2_FFN_GROUPS
+};
+
+template <typename T> __device__ __forceinline__ typename emc2_tile<T>::frag emc2_zero_frag() { return typename emc2_tile<T>::frag(T(0)); }
+
+// The fragment of row `row`, along channels kk KF ..; zero beyond the rows and channels.
+template <typename T>
+__device__ __forceinline__ typename emc2_tile<T>::frag emc2_row_frag(const T* p, int64_t ld, int64_t row, int32_t n, int32_t channels, bool wide,
+                                                                      int kk, int half) {
+  typedef emc2_tile<T> M;
+  const int c = kk * M::kDeep + half * M::kPer;
+  typename M::frag f = emc2_zero_frag<T>();
+  if (row < n && c < channels) {
+    const T* q = p + row * ld + c;
+    if (wide) {
+      f = *reinterpret_cast<const typename M::frag*>(q);
+    } else {
+#pragma unroll
+      for (int e = 0; e < M::kPer; ++e)
+        if (c + e < channels) f[e] = q[e];
+    }
+  }
+  return f;
+}
+
+// The fragments of a row: kept in registers, or (wide rows of fp32, which would take half of them) read again for every use.
+template <typename T, int CT> struct emc2_row {
+  typedef emc2_tile<T> M;
+  static constexpr int KK = 32 * CT / M::kDeep;
+  static constexpr bool kKept = sizeof(T) * CT <= 16;
+  typename M::frag f[kKept ? KK : 1];
+  const T* p;
+  int64_t ld, row;
+  int32_t n, channels;
+  int half;
+  bool wide;
+  __device__ __forceinline__ void set(const void* p_, int64_t ld_, int64_t row_, int32_t n_, const bool wide_, int32_t channels_, int half_) {
+    p = (const T*)p_, ld = ld_, row = row_, n = n_, wide = wide_, channels = channels_, half = half_;
+    if constexpr (kKept) {
+#pragma unroll
+      for (int k = 0; k < KK; ++k) f[k] = emc2_row_frag<T>(p, ld, row, n, channels, wide, k, half);
+    }
+  }
+  // before a loop's turn: what is read again is not moved out of the loop
+  __device__ __forceinline__ void again() {
+    if constexpr (!kKept) asm volatile("" : "+v"(p));
+  }
+  __device__ __forceinline__ typename M::frag operator[](int k) const {
+    if constexpr (kKept) return f[k];
+    else return emc2_row_frag<T>(p, ld, row, n, channels, wide, k, half);
+  }
+};
+
+// act(g) of either activation as g s, s = logistic(z): SiLU z = g, GELU (its tanh form) z = sqrt(8 / pi) (g + 0.044715 g^3); and the slope
+// s (1 + g (1 - s) dz/dg).
+template <bool EXACT> __device__ __forceinline__ float emc2_activate(bool gelu, float g) {
+  float s, rest;
+  emc2_logistic<EXACT>(gelu ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g, s, rest);
+  return g * s;
+}
+template <bool EXACT> __device__ __forceinline__ float emc2_activate(bool gelu, float g, float& slope) {
+  float s, rest;
+  emc2_logistic<EXACT>(gelu ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g, s, rest);
+  const float dz = gelu ? 1.5957691216057308f * (1.0f + 0.134145f * g * g) : 1.0f;
+  slope = s + g * s * rest * dz;
+  return g * s;
+}
+
+// Arguments of a launch.
+struct emc2_ffn_args {
+  const void *x, *res, *dy, *packed;
+  void* y;                    // forward: the result; backward: dx
+  float* partial;             // weight gradients of every part of the rows
+  const int32_t* d_n;
+  int64_t ld_x, ld_res, ld_dy, ld_y, capacity;
+  int32_t channels, hidden, slices, parts;
+  bool gelu, wide;
+};
+
+static inline int emc2_ffn_tiles(int32_t channels) {        // 32-wide tiles of channels that the kernels are made for
+  const int t = (channels + 31) / 32;
+  return t <= 4 ? t : t <= 6 ? 6 : 8;
+}
+constexpr int kFfnMaxChannels = 256, kFfnMaxHidden = 1 << 16;
+
+// Calls f with a value of the type and the number of tiles as a constant.
+template <int N> struct emc2_const { static constexpr int value = N; };
+template <typename F> void emc2_ffn_dispatch(emc2_dtype dtype, int tiles, F&& f) {
+  const auto by_tiles = [&](auto type) {
+    switch (tiles) {
+      case 1: return f(type, emc2_const<1>());
+      case 2: return f(type, emc2_const<2>());
+      case 3: return f(type, emc2_const<3>());
+      case 4: return f(type, emc2_const<4>());
+      case 6: return f(type, emc2_const<6>());
+      default: return f(type, emc2_const<8>());
+    }
+  };
+  if (dtype == EMC2_F32) by_tiles(float());
+  else if (dtype == EMC2_F16) by_tiles(_Float16());
+  else by_tiles(__bf16());
+}
+emc2_status emc2_ffn_check(emc2_ctx* ctx, const char* what, emc2_dtype dtype, int32_t activation, int64_t capacity, int32_t channels,
+                           int32_t hidden, const void* packed);

@@ -1,0 +1,348 @@
+// Layer norm over the channels of feature rows, and its gradients.
+//   y = (s - mean) * rstd * gamma + beta,   rstd = 1 / sqrt(var + eps), var the mean of (s - mean)^2, s = x or x + residual
+// A row lies in the registers of L neighbouring lanes, V vectors of 16 bytes each: it is read once, the mean is summed first
+// and the squares about it second (no difference of two large sums), both in fp32 with a butterfly over the L lanes.
+//   dx = rstd (q - mean(q) - xh mean(q xh)) + add,  q = dy gamma, xh = (x - mean) rstd;   dgamma = sum over rows of dy xh, dbeta of dy
+// The backward pass takes mean and rstd from the row again, which it needs in registers anyway: nothing is kept from the forward
+// pass.  The weights' sums stay in each lane's registers while its block walks the rows; the blocks' sums are added by a second
+// launch in a fixed order (fp32 throughout, no atomics: equal inputs give equal bits).
+// Both are bound by memory.
+#include "rows.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxChannels = 1024;
+
+template <int L> __device__ __forceinline__ float lane_sum(float v) {
+#pragma unroll
+  for (int d = 1; d < L; d <<= 1) v += __shfl_xor(v, d, 64);
+  return v;
+}
+
+template <int N, int V> __device__ __forceinline__ float sum_of(const emc2_fvec<N> (&x)[V]) {
+  float s = 0.0f;
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int e = 0; e < N; ++e) s += x[v][e];
+  return s;
+}
+
+struct NormArgs {
+  const void *x, *res, *dy;      // res: forward: the residual; backward: added to dx.  May be null
+  const float *gamma, *beta;
+  const int32_t* d_n;
+  void *y, *sum;                 // y: forward: the result; backward: dx
+  float* partial;                // [blocks][2][channels]
+  int64_t ld_x, ld_res, ld_dy, ld_y, ld_sum, capacity;
+  int32_t channels;
+  float eps, inv_channels;
+};
+
+// N values a vector, L lanes a row, V vectors a lane, U rows of a lane under way together
+template <typename T, int N, int L, int V, int U>
+__global__ void __launch_bounds__(kThreads) k_layernorm(const NormArgs a) {
+  const int32_t n = emc2_row_count(a.d_n, a.capacity);
+  constexpr int kGroups = kThreads / L;
+  const int64_t first = (int64_t)blockIdx.x * (kGroups * U) + threadIdx.x / L;
+  if ((int64_t)blockIdx.x * (kGroups * U) >= n) return;
+  const int sub = threadIdx.x % L;
+  emc2_fvec<N> x[U][V];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t row = first + u * kGroups;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * L + sub) * N;
+      x[u][v] = 0.0f;
+      if (row < n && c < a.channels) x[u][v] = emc2_load<N>((const T*)a.x + row * a.ld_x + c);
+    }
+  }
+  if (a.res) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = first + u * kGroups;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int c = (v * L + sub) * N;
+        if (row < n && c < a.channels) {
+          x[u][v] += emc2_load<N>((const T*)a.res + row * a.ld_res + c);
+          if (a.sum) emc2_store<N>((T*)a.sum + row * a.ld_sum + c, x[u][v]);   // rounded for the caller, not for the norm
+        }
+      }
+    }
+  }
+  emc2_fvec<N> gamma[V], beta[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int c = (v * L + sub) * N;
+    gamma[v] = 0.0f, beta[v] = 0.0f;
+    if (c < a.channels) {
+      gamma[v] = emc2_load_params<N>(a.gamma + c);
+      beta[v] = emc2_load_params<N>(a.beta + c);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t row = first + u * kGroups;
+    const float mean = lane_sum<L>(sum_of<N, V>(x[u])) * a.inv_channels;
+    emc2_fvec<N> sq[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const bool in = (v * L + sub) * N < a.channels;
+      x[u][v] -= mean;
+      sq[v] = in ? x[u][v] * x[u][v] : emc2_fvec<N>(0.0f);
+    }
+    const float rstd = 1.0f / __builtin_sqrtf(lane_sum<L>(sum_of<N, V>(sq)) * a.inv_channels + a.eps);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * L + sub) * N;
+      if (row < n && c < a.channels) emc2_store<N>((T*)a.y + row * a.ld_y + c, x[u][v] * rstd * gamma[v] + beta[v]);
+    }
+  }
+}
+
+template <typename T, int N, int L, int V, int U>
+__global__ void __launch_bounds__(kThreads) k_layernorm_grad(const NormArgs a, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+  const int32_t n = emc2_row_count(a.d_n, a.capacity);
+  constexpr int kGroups = kThreads / L;
+  const int sub = threadIdx.x % L;
+  emc2_fvec<N> gamma[V], sum_g[V], sum_b[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int c = (v * L + sub) * N;
+    gamma[v] = 0.0f, sum_g[v] = 0.0f, sum_b[v] = 0.0f;
+    if (c < a.channels) gamma[v] = emc2_load_params<N>(a.gamma + c);
+  }
+  const int64_t step = (int64_t)gridDim.x * (kGroups * U);
+  for (int64_t first = (int64_t)blockIdx.x * (kGroups * U) + threadIdx.x / L; first < n; first += step) {
+    emc2_fvec<N> x[U][V], dy[U][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = first + u * kGroups;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int c = (v * L + sub) * N;
+        x[u][v] = 0.0f, dy[u][v] = 0.0f;
+        if (row < n && c < a.channels) {
+          x[u][v] = emc2_load<N>((const T*)a.x + row * a.ld_x + c);
+          dy[u][v] = emc2_load<N>((const T*)a.dy + row * a.ld_dy + c);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = first + u * kGroups;
+      const float mean = lane_sum<L>(sum_of<N, V>(x[u])) * a.inv_channels;
+      emc2_fvec<N> t[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        x[u][v] = (v * L + sub) * N < a.channels ? x[u][v] - mean : emc2_fvec<N>(0.0f);
+        t[v] = x[u][v] * x[u][v];
+      }
+      const float var = lane_sum<L>(sum_of<N, V>(t)) * a.inv_channels;
+      const float rstd = row < n ? 1.0f / __builtin_sqrtf(var + a.eps) : 0.0f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        x[u][v] *= rstd;                                   // xh
+        sum_g[v] += dy[u][v] * x[u][v];
+        sum_b[v] += dy[u][v];
+        dy[u][v] *= gamma[v];
+        t[v] = dy[u][v] * x[u][v];
+      }
+      const float mean_q = lane_sum<L>(sum_of<N, V>(dy[u])) * a.inv_channels;
+      const float mean_qx = lane_sum<L>(sum_of<N, V>(t)) * a.inv_channels;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int c = (v * L + sub) * N;
+        if (row < n && c < a.channels) {
+          emc2_fvec<N> dx = (dy[u][v] - mean_q - x[u][v] * mean_qx) * rstd;
+          if (a.res) dx += emc2_load<N>((const T*)a.res + row * a.ld_res + c);
+          emc2_store<N>((T*)a.y + row * a.ld_y + c, dx);
+        }
+      }
+    }
+  }
+  // The block's sums: over a wave's groups by a butterfly, over the waves through LDS, one half of the channels' vectors at a time.
+  __shared__ float part[kThreads / 64][L * N];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      emc2_fvec<N> s = which ? sum_b[v] : sum_g[v];
+#pragma unroll
+      for (int d = L; d < 64; d <<= 1)
+#pragma unroll
+        for (int e = 0; e < N; ++e) s[e] += __shfl_xor(s[e], d, 64);
+      __syncthreads();
+      if (lane < L) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) part[wave][lane * N + e] = s[e];
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < L * N; i += kThreads) {
+        const int c = v * L * N + i;
+        float all = part[0][i];
+#pragma unroll
+        for (int w = 1; w < kThreads / 64; ++w) all += part[w][i];
+        if (c < a.channels) {
+          if (gridDim.x == 1) (which ? dbeta : dgamma)[c] = all;
+          else a.partial[((int64_t)blockIdx.x * 2 + which) * a.channels + c] = all;
+        }
+      }
+    }
+}
+
+// dgamma and dbeta from the blocks' sums: 32 columns a block, 32 threads a column.
+__global__ void __launch_bounds__(1024) k_layernorm_weights(const float* __restrict__ partial, int32_t blocks, int32_t channels,
+                                                            float* __restrict__ dgamma, float* __restrict__ dbeta) {
+  __shared__ float part[32][33];
+  const int col = blockIdx.x * 32 + (threadIdx.x & 31), seg = threadIdx.x >> 5;
+  float s = 0.0f;
+  if (col < 2 * channels) {
+#pragma unroll 8
+    for (int b = seg; b < blocks; b += 32) s += partial[(int64_t)b * 2 * channels + col];
+  }
+  part[seg][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (seg == 0 && col < 2 * channels) {
+    for (int i = 1; i < 32; ++i) s += part[i][threadIdx.x];
+    if (col < channels) dgamma[col] = s;
+    else dbeta[col - channels] = s;
+  }
+}
+
+// How the rows of a call lie over the lanes: 16-byte vectors where all buffers and pitches allow it, else single values.
+struct Shape { bool wide; int lanes, vectors; };
+Shape shape_of(emc2_dtype dtype, int32_t channels, bool wide) {
+  const int per = wide ? (dtype == EMC2_F32 ? 4 : 8) : 1;
+  const int pieces = (channels + per - 1) / per;
+  int lanes = wide ? 8 : 16;
+  while (lanes < 64 && lanes < pieces) lanes *= wide ? 2 : 4;
+  int vectors = 1;
+  while (vectors * lanes < pieces) vectors *= 2;
+  return {wide, lanes, vectors};
+}
+
+// Calls f with the compile-time form (values a vector, lanes, vectors, rows at a time) of a shape.
+template <int N, int L, int V, int U> struct Form { static constexpr int n = N, l = L, v = V, u = U; };
+template <int N, typename F> void with_form(const Shape& s, F&& f) {
+  if constexpr (N == 1) {
+    if (s.lanes == 16) return f(Form<1, 16, 1, 4>());
+    switch (s.vectors) {
+      case 1: return f(Form<1, 64, 1, 4>());
+      case 2: return f(Form<1, 64, 2, 4>());
+      case 4: return f(Form<1, 64, 4, 2>());
+      case 8: return f(Form<1, 64, 8, 1>());
+      default: return f(Form<1, 64, 16, 1>());
+    }
+  } else {
+    switch (s.lanes) {
+      case 8: return f(Form<N, 8, 1, 4>());
+      case 16: return f(Form<N, 16, 1, 4>());
+      case 32: return f(Form<N, 32, 1, 4>());
+    }
+    switch (s.vectors) {
+      case 1: return f(Form<N, 64, 1, 2>());
+      case 2: return f(Form<N, 64, 2, 1>());
+    }
+    if constexpr (N == 4) return f(Form<N, 64, 4, 1>());
+  }
+}
+template <typename F> void with_type(emc2_dtype dtype, const Shape& s, F&& f) {
+  if (dtype == EMC2_F32) {
+    if (s.wide) with_form<4>(s, [&](auto form) { f(form, float()); });
+    else with_form<1>(s, [&](auto form) { f(form, float()); });
+  } else if (dtype == EMC2_F16) {
+    if (s.wide) with_form<8>(s, [&](auto form) { f(form, _Float16()); });
+    else with_form<1>(s, [&](auto form) { f(form, _Float16()); });
+  } else {
+    if (s.wide) with_form<8>(s, [&](auto form) { f(form, __bf16()); });
+    else with_form<1>(s, [&](auto form) { f(form, __bf16()); });
+  }
+}
+
+constexpr int64_t kGradBlocks = 1024;
+
+}  // namespace
+
+extern "C" emc2_status emc2_layernorm(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_res, int64_t ld_res,
+                                      const float* d_gamma, const float* d_beta, float eps, const int32_t* d_n, int64_t capacity,
+                                      int32_t channels, void* d_sum, int64_t ld_sum, void* d_y, int64_t ld_y, void* stream) {
+  if (!ctx) return EMC2_ERR_INVALID_ARG;
+  if (!emc2_is_float(dtype)) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "emc2_layernorm: dtype must be F32, F16 or BF16");
+  if (channels < 1 || channels > kMaxChannels)
+    return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "emc2_layernorm: channels outside [1, %d]", kMaxChannels);
+  if (capacity < 0 || capacity > (1ll << 30)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm: capacity outside [0, 2^30]");
+  if (!(eps >= 0.0f)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm: eps must not be negative");
+  const size_t size = emc2_size_of(dtype);
+  const bool none = capacity == 0;
+  if (!d_gamma || !d_beta || (d_sum && !d_res)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm: null argument");
+  if (!emc2_rows_ok(d_x, ld_x, channels, size, none) || !emc2_rows_ok(d_y, ld_y, channels, size, none) ||
+      !emc2_rows_ok(d_res, ld_res, channels, size, true) || !emc2_rows_ok(d_sum, ld_sum, channels, size, true))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm: null or misaligned rows, or a pitch below the channels");
+  if (none) return EMC2_OK;
+  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_y, ld_y, size) &&
+                    (!d_res || emc2_wide_rows(d_res, ld_res, size)) && (!d_sum || emc2_wide_rows(d_sum, ld_sum, size)) &&
+                    ((uintptr_t)d_gamma & 15) == 0 && ((uintptr_t)d_beta & 15) == 0;
+  NormArgs a = {};
+  a.x = d_x, a.res = d_res, a.gamma = d_gamma, a.beta = d_beta, a.d_n = d_n, a.y = d_y, a.sum = d_sum;
+  a.ld_x = ld_x, a.ld_res = ld_res, a.ld_y = ld_y, a.ld_sum = ld_sum, a.capacity = capacity, a.channels = channels;
+  a.eps = eps, a.inv_channels = 1.0f / (float)channels;
+  with_type(dtype, shape_of(dtype, channels, wide), [&](auto form, auto type) {
+    using F = decltype(form);
+    using T = decltype(type);
+    const int64_t rows = kThreads / F::l * F::u;
+    hipLaunchKernelGGL((k_layernorm<T, F::n, F::l, F::v, F::u>), dim3((unsigned)emc2_div_up(capacity, rows)), dim3(kThreads), 0,
+                       (hipStream_t)stream, a);
+  });
+  return emc2_check_hip(ctx, hipGetLastError(), "emc2_layernorm launch");
+}
+
+extern "C" int64_t emc2_layernorm_work(emc2_dtype dtype, int64_t capacity, int32_t channels) {
+  if (!emc2_is_float(dtype) || channels < 1 || channels > kMaxChannels || capacity < 0 || capacity > (1ll << 30)) return -1;
+  const int64_t blocks = emc2_div_up(capacity, 4);         // a block has four rows at least
+  return (blocks < kGradBlocks ? blocks : kGradBlocks) * 2 * channels * (int64_t)sizeof(float);
+}
+
+extern "C" emc2_status emc2_layernorm_backward(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_dy, int64_t ld_dy,
+                                               const void* d_add, int64_t ld_add, const float* d_gamma, float eps, const int32_t* d_n,
+                                               int64_t capacity, int32_t channels, void* d_dx, int64_t ld_dx, float* d_dgamma,
+                                               float* d_dbeta, void* d_work, int64_t work_bytes, void* stream) {
+  if (!ctx) return EMC2_ERR_INVALID_ARG;
+  if (!emc2_is_float(dtype)) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "emc2_layernorm_backward: dtype must be F32, F16 or BF16");
+  if (channels < 1 || channels > kMaxChannels)
+    return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "emc2_layernorm_backward: channels outside [1, %d]", kMaxChannels);
+  if (capacity < 0 || capacity > (1ll << 30))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm_backward: capacity outside [0, 2^30]");
+  if (!(eps >= 0.0f)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm_backward: eps must not be negative");
+  const size_t size = emc2_size_of(dtype);
+  const bool none = capacity == 0;
+  if (!d_gamma || !d_dgamma || !d_dbeta) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm_backward: null argument");
+  if (!emc2_rows_ok(d_x, ld_x, channels, size, none) || !emc2_rows_ok(d_dy, ld_dy, channels, size, none) ||
+      !emc2_rows_ok(d_dx, ld_dx, channels, size, none) || !emc2_rows_ok(d_add, ld_add, channels, size, true))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm_backward: null or misaligned rows, or a pitch below the channels");
+  if (work_bytes < emc2_layernorm_work(dtype, capacity, channels) || (!none && (!d_work || ((uintptr_t)d_work & 3))))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm_backward: work buffer null, misaligned or smaller than emc2_layernorm_work");
+  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_dy, ld_dy, size) &&
+                    emc2_wide_rows(d_dx, ld_dx, size) && (!d_add || emc2_wide_rows(d_add, ld_add, size)) && ((uintptr_t)d_gamma & 15) == 0;
+  NormArgs a = {};
+  a.x = d_x, a.res = d_add, a.dy = d_dy, a.gamma = d_gamma, a.d_n = d_n, a.y = d_dx, a.partial = (float*)d_work;
+  a.ld_x = ld_x, a.ld_res = ld_add, a.ld_dy = ld_dy, a.ld_y = ld_dx, a.capacity = capacity, a.channels = channels;
+  a.eps = eps, a.inv_channels = 1.0f / (float)channels;
+  hipStream_t s = (hipStream_t)stream;
+  int64_t blocks = 1;
+  with_type(dtype, shape_of(dtype, channels, wide), [&](auto form, auto type) {
+    using F = decltype(form);
+    using T = decltype(type);
+    blocks = emc2_div_up(capacity, kThreads / F::l * F::u * 2);
+    blocks = blocks < 1 ? 1 : blocks < kGradBlocks ? blocks : kGradBlocks;
+    hipLaunchKernelGGL((k_layernorm_grad<T, F::n, F::l, F::v, F::u>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, d_dgamma, d_dbeta);
+  });
+  if (blocks > 1)
+    hipLaunchKernelGGL(k_layernorm_weights, dim3((unsigned)emc2_div_up(2 * channels, 32)), dim3(1024), 0, s, a.partial, (int32_t)blocks,
+                       channels, d_dgamma, d_dbeta);
+  return emc2_check_hip(ctx, hipGetLastError(), "emc2_layernorm_backward launch");
+}

@@ -1,0 +1,747 @@
+// Gated linear recurrence along the rows of packed sequences, its gradients and its form for one row per sequence.
+//   a_t = logistic(gate_t),  h_t = a_t h_{t-1} + (1 - a_t) x_t                 per channel, h_0 given or 0
+//   u_t = dy_t + a_{t+1} u_{t+1} (+ dlast behind the last row);  dx_t = (1 - a_t) u_t,  dgate_t = u_t (h_{t-1} - x_t) a_t (1 - a_t),
+//   dh_0 = a_1 u_1
+// Row t maps the state h -> A h + B, and maps compose: any run of rows is one such pair per channel, so a long sequence is cut into
+// blocks of rows that are worked on side by side.  A first launch reduces every block to its pair (k_recurrence_totals), the second
+// composes the pairs of the blocks before its own into the state that enters it and then walks its rows (k_recurrence).  A sequence's
+// first row begins a new map (A = 0, B = the given state), so sequences of any length share a block and none is padded.
+// The gradients' u runs the other way with the same factors: the first launch reduces both directions at once, the second walks a block's
+// tiles from the last to the first, with the state that enters every tile known from the first launch.
+// Inside a block a thread holds R consecutive rows of N neighbouring channels in registers; maps are composed over a wave's
+// row groups by shuffles, over waves through LDS.  The order of composition is fixed: equal inputs give equal bits.  Maps and states are fp32.
+// A map with A = 0 drops what lies before it, whatever that holds: an infinity or NaN in one sequence never reaches another one.
+// Bound by memory, and close behind by the logistic function's two quarter-rate instructions an element.
+#include "rows.h"
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMaxTiles = 32;        // tiles of a block
+constexpr int kRowsForward = 8, kRowsGrad = 4;
+
+struct Args {
+  const void *x, *gate, *dy;
+  const float *h0, *dlast;           // dlast: gradient of the last states
+  const int32_t* offsets;
+  void *y, *dgate;                   // y: forward: the states; backward: dx
+  float *last, *dh0;
+  float2 *block_f, *block_r, *tile_f;  // maps [blocks or tiles][width]; width: channels rounded up to whole slices
+  int32_t* flags;
+  int64_t ld_x, ld_gate, ld_dy, ld_y, ld_dgate;
+  int32_t capacity, channels, width, n_seq, tiles, backwards;
+  int32_t lane_shift;                // a row group is 2^lane_shift lanes wide
+};
+
+// Rows are counted in the direction of the scan: row r lies at r, or at n - 1 - r when the scan runs backwards; sequence j of the
+// scan is then the caller's sequence n_seq - 1 - j.  Offsets are held within the rows, whatever they say.
+__device__ __forceinline__ int32_t rows_of(const Args& a) {
+  const int32_t n = a.offsets[a.n_seq];
+  return n < 0 ? 0 : n < a.capacity ? n : a.capacity;
+}
+__device__ __forceinline__ int32_t start_of(const Args& a, int32_t n, int32_t j) {   // j in [0, n_seq]
+  const int32_t o = a.offsets[a.backwards ? a.n_seq - j : j];
+  const int32_t in = o < 0 ? 0 : o < n ? o : n;
+  return a.backwards ? n - in : in;
+}
+__device__ __forceinline__ int32_t seq_of(const Args& a, int32_t j) { return a.backwards ? a.n_seq - 1 - j : j; }
+
+// The first j >= `j` whose sequence starts at `row` or later (n_seq if there is none), by the whole wave.
+__device__ __forceinline__ int32_t seek(const Args& a, int32_t n, int32_t j, int32_t row, int lane) {
+  while (true) {
+    const bool below = j + lane < a.n_seq && start_of(a, n, j + lane) < row;
+    const unsigned long long m = ~__ballot(below);
+    if (m) return j + __builtin_ctzll(m);
+    j += 64;
+  }
+}
+__device__ __forceinline__ int32_t seek_far(const Args& a, int32_t n, int32_t row, int lane) {
+  int32_t lo = 0, hi = a.n_seq;
+  while (hi - lo > 64) {                 // the answer lies in [lo, hi]; every turn leaves at most a 64th of that
+    const int32_t step = (hi - lo) / 64;
+    const unsigned long long m = ~__ballot(start_of(a, n, lo + (lane + 1) * step - 1) < row);
+    const int c = m ? __builtin_ctzll(m) : 64;
+    if (c < 64) hi = lo + (c + 1) * step - 1;
+    lo += c * step;
+  }
+  return seek(a, n, lo, row, lane);
+}
+
+// Where sequences start and end within a wave's rows of a tile: per row the caller's number of the sequence that starts or ends there,
+// or -1.  Returns false, and writes nothing, where none does (next: the first start at or after the rows' first, also the end of
+// the sequence that runs there).
+__device__ __forceinline__ bool mark(const Args& a, int32_t n, int32_t row0, int rows, int32_t& j, int32_t& next, int32_t* starts,
+                                     int32_t* ends, int lane) {
+  if (next < row0) {
+    j = seek(a, n, j, row0, lane);
+    next = start_of(a, n, j);
+  }
+  if (next > row0 + rows) return false;
+  for (int i = lane; i < rows; i += 64) starts[i] = ends[i] = -1;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (lane == 0 && j > 0 && next > row0 && next <= row0 + rows) ends[next - 1 - row0] = seq_of(a, j - 1);
+  for (int32_t k = j;; k += 64) {
+    const int32_t s = k + lane;
+    bool here = false;
+    if (s < a.n_seq) {
+      const int32_t p = start_of(a, n, s), q = start_of(a, n, s + 1);
+      here = p >= row0 && p < row0 + rows;
+      if (here && q > p) {
+        starts[p - row0] = seq_of(a, s);
+        if (q <= row0 + rows) ends[q - 1 - row0] = seq_of(a, s);
+      }
+    }
+    if (!__any(here)) break;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  return true;
+}
+
+// A map h -> A h + B of N channels, and what it makes of a state.
+template <int N> struct Map { emc2_fvec<N> A, B; };
+__device__ __forceinline__ float apply(float A, float B, float h) { return A == 0.0f ? B : __builtin_fmaf(A, h, B); }
+template <int N> __device__ __forceinline__ emc2_fvec<N> apply(const Map<N>& m, emc2_fvec<N> h) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) h[e] = apply(m.A[e], m.B[e], h[e]);
+  return h;
+}
+// `second` after `first`.  A second map that drops the state stays one, even if the first one's factor is NaN.
+__device__ __forceinline__ float2 then(float2 first, float2 second) {
+  return make_float2(second.x == 0.0f ? 0.0f : first.x * second.x, apply(second.x, second.y, first.y));
+}
+template <int N> __device__ __forceinline__ Map<N> then(const Map<N>& first, const Map<N>& second) {
+  Map<N> m;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float2 q = then(make_float2(first.A[e], first.B[e]), make_float2(second.A[e], second.B[e]));
+    m.A[e] = q.x, m.B[e] = q.y;
+  }
+  return m;
+}
+template <int N> __device__ __forceinline__ Map<N> nothing() { return {emc2_fvec<N>(1.0f), emc2_fvec<N>(0.0f)}; }
+template <int N> __device__ __forceinline__ Map<N> from_below(const Map<N>& m, int d) {
+  Map<N> o;
+#pragma unroll
+  for (int e = 0; e < N; ++e) o.A[e] = __shfl_up(m.A[e], d, 64), o.B[e] = __shfl_up(m.B[e], d, 64);
+  return o;
+}
+template <int N> __device__ __forceinline__ Map<N> from_above(const Map<N>& m, int d) {
+  Map<N> o;
+#pragma unroll
+  for (int e = 0; e < N; ++e) o.A[e] = __shfl_down(m.A[e], d, 64), o.B[e] = __shfl_down(m.B[e], d, 64);
+  return o;
+}
+
+// What a thread is: its wave, its row group within the wave, its channels.
+struct Place {
+  int lane, wave, group, groups, column;   // column: the first of its channels within the slice
+  int32_t channel;                         // and of all
+  bool in;                                 // it has channels
+};
+template <int N> __device__ __forceinline__ Place place_of(const Args& a) {
+  Place p;
+  p.lane = threadIdx.x & 63;
+  p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  p.group = p.lane >> a.lane_shift;
+  p.groups = 64 >> a.lane_shift;
+  p.column = (p.lane & ((1 << a.lane_shift) - 1)) * N;
+  p.channel = (int32_t)blockIdx.y * (N << a.lane_shift) + p.column;
+  p.in = p.channel < a.channels;
+  return p;
+}
+
+// R consecutive rows of a thread as they lie in memory; rows past the last and channels that are none read valid places.
+template <typename T, int N, int R> struct Rows { emc2_vec<T, N> v[R]; };
+template <typename T, int N, int R>
+__device__ __forceinline__ Rows<T, N, R> fetch(const Args& a, const void* p, int64_t ld, int32_t n, int32_t row, const Place& t) {
+  Rows<T, N, R> r;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int32_t k = row + i < n ? row + i : n - 1;
+    r.v[i] = *reinterpret_cast<const emc2_vec<T, N>*>((const T*)p + (int64_t)(a.backwards ? n - 1 - k : k) * ld + (t.in ? t.channel : 0));
+  }
+  return r;
+}
+
+// a and 1 - a of a gate's row
+template <typename T, int N> __device__ __forceinline__ void open(emc2_vec<T, N> gate, emc2_fvec<N>& keep, emc2_fvec<N>& take) {
+  const emc2_fvec<N> g = __builtin_convertvector(gate, emc2_fvec<N>);
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    float s, r;
+    emc2_logistic<sizeof(T) == 4>(g[e], s, r);
+    keep[e] = s, take[e] = r;
+  }
+}
+
+template <int N> __device__ __forceinline__ emc2_fvec<N> state_or_zero(const float* p, const Args& a, int32_t seq, const Place& t) {
+  return p && t.in ? emc2_load_params<N>(p + (int64_t)seq * a.channels + t.channel) : emc2_fvec<N>(0.0f);
+}
+
+// The map of a thread's rows, first to last, from their factors and offsets.
+template <int N, int R>
+__device__ __forceinline__ Map<N> run_forward(const Args& a, const emc2_fvec<N> (&keep)[R], const emc2_fvec<N> (&add)[R], bool marked,
+                                              const int32_t* starts, const Place& t) {
+  Map<N> m = nothing<N>();
+  if (!marked) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) m.A *= keep[i], m.B = keep[i] * m.B + add[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int32_t s = starts[i];
+      if (s >= 0) m = {emc2_fvec<N>(0.0f), state_or_zero<N>(a.h0, a, s, t)};
+      m.A *= keep[i], m.B = keep[i] * m.B + add[i];
+    }
+  }
+  return m;
+}
+// The map of what flows towards earlier rows (a_t u_t), last to first.
+template <int N, int R>
+__device__ __forceinline__ Map<N> run_backward(const Args& a, const emc2_fvec<N> (&keep)[R], const emc2_fvec<N> (&dy)[R], bool marked,
+                                               const int32_t* ends, const Place& t) {
+  Map<N> m = nothing<N>();
+#pragma unroll
+  for (int i = R - 1; i >= 0; --i) {
+    if (marked) {
+      const int32_t s = ends[i];
+      if (s >= 0) m = {emc2_fvec<N>(0.0f), state_or_zero<N>(a.dlast, a, s, t)};
+    }
+    m.A *= keep[i], m.B = keep[i] * (dy[i] + m.B);
+  }
+  return m;
+}
+
+// Rows past the last change nothing: a = 1, nothing added.
+template <int N, int R> __device__ __forceinline__ void blank(int32_t n, int32_t row, emc2_fvec<N> (&keep)[R], emc2_fvec<N> (&add)[R]) {
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (row + i >= n) keep[i] = 1.0f, add[i] = 0.0f;
+}
+
+// First launch: the maps of every block, and with GRAD of every tile.  Block (b, slice) has `tiles` tiles of rows, a tile a thread's R rows in
+// every row group of the block.
+template <typename T, int N, int R, bool GRAD>
+__global__ void __launch_bounds__(kThreads) k_recurrence_totals(const Args a) {
+  constexpr int kSlice = 64;
+  __shared__ float2 total[2][GRAD ? 2 : 1][kWaves][kSlice];
+  __shared__ int32_t starts[kWaves][64 * R], ends[kWaves][64 * R];
+  const Place t = place_of<N>(a);
+  const int32_t n = rows_of(a);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0 && a.offsets[a.n_seq] > a.capacity) atomicOr(a.flags, EMC2_DEVFLAG_CAPACITY);
+  const int32_t tile_rows = kWaves * t.groups * R;
+  const int64_t first = (int64_t)blockIdx.x * a.tiles * tile_rows;
+  if (first >= n) return;
+  const int slice = N << a.lane_shift;
+  int32_t j = 0, next = -1;
+  if (first > 0) j = seek_far(a, n, (int32_t)first, t.lane);
+  float2 block_f = make_float2(1.0f, 0.0f), block_r = block_f;
+  for (int32_t k = 0; k < a.tiles; ++k) {
+    const int64_t row0 = first + (int64_t)k * tile_rows + t.wave * t.groups * R;
+    if (first + (int64_t)k * tile_rows >= n) break;
+    const int32_t row = (int32_t)row0 + t.group * R;
+    Map<N> f = nothing<N>(), r = nothing<N>();
+    if (row0 < n) {
+      const Rows<T, N, R> x = fetch<T, N, R>(a, a.x, a.ld_x, n, row, t), g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, row, t);
+      Rows<T, N, R> d;
+      if constexpr (GRAD) d = fetch<T, N, R>(a, a.dy, a.ld_dy, n, row, t);
+      const bool marked = mark(a, n, (int32_t)row0, t.groups * R, j, next, starts[t.wave], ends[t.wave], t.lane);
+      emc2_fvec<N> keep[R], add[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        emc2_fvec<N> take;
+        open<T, N>(g.v[i], keep[i], take);
+        add[i] = take * __builtin_convertvector(x.v[i], emc2_fvec<N>);
+      }
+      if (row0 + t.groups * R > n) blank<N, R>(n, row, keep, add);
+      f = run_forward<N, R>(a, keep, add, marked, &starts[t.wave][t.group * R], t);
+      if constexpr (GRAD) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) add[i] = __builtin_convertvector(d.v[i], emc2_fvec<N>);
+        if (row0 + t.groups * R > n) blank<N, R>(n, row, keep, add);
+        r = run_backward<N, R>(a, keep, add, marked, &ends[t.wave][t.group * R], t);
+      }
+      for (int dist = 1 << a.lane_shift; dist < 64; dist <<= 1) {     // the wave's first row group ends with all of them
+        f = then<N>(f, from_above<N>(f, dist));
+        if constexpr (GRAD) r = then<N>(from_above<N>(r, dist), r);
+      }
+    }
+    if (t.group == 0) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        total[k & 1][0][t.wave][t.column + e] = make_float2(f.A[e], f.B[e]);
+        if constexpr (GRAD) total[k & 1][GRAD ? 1 : 0][t.wave][t.column + e] = make_float2(r.A[e], r.B[e]);
+      }
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < slice) {
+      const int c = threadIdx.x;
+      float2 tile = total[k & 1][0][0][c];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) {
+        tile = then(tile, total[k & 1][0][w][c]);
+      }
+      block_f = then(block_f, tile);
+      if constexpr (GRAD) {
+        a.tile_f[((int64_t)blockIdx.x * a.tiles + k) * a.width + blockIdx.y * slice + c] = tile;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {                 // of the flow towards earlier rows, the later rows come first
+          block_r = then(total[k & 1][GRAD ? 1 : 0][w][c], block_r);
+        }
+      }
+    }
+  }
+  if ((int)threadIdx.x < slice) {
+    a.block_f[(int64_t)blockIdx.x * a.width + blockIdx.y * slice + threadIdx.x] = block_f;
+    if constexpr (GRAD) a.block_r[(int64_t)blockIdx.x * a.width + blockIdx.y * slice + threadIdx.x] = block_r;
+  }
+}
+
+// What a run of blocks makes of a state of zeros, per channel of the slice, into enter[]: blocks [lo, hi) in rising order, or (FALLING) from
+// hi - 1 down to lo.  The block's threads take a part of the run each.  Ends with a barrier.
+template <bool FALLING>
+__device__ __forceinline__ void compose(const float2* __restrict__ maps, int32_t width, int32_t column, int slice, int32_t lo, int32_t hi,
+                                        float2* part, float* enter) {
+  const int c = threadIdx.x & (slice - 1), seg = threadIdx.x / slice, segs = kThreads / slice;
+  const int32_t count = hi > lo ? hi - lo : 0, per = (count + segs - 1) / segs;
+  const int32_t from = seg * per < count ? seg * per : count, to = from + per < count ? from + per : count;
+  float2 all = make_float2(1.0f, 0.0f);
+  constexpr int kAtOnce = 8;
+  for (int32_t i = from; i < to; i += kAtOnce) {
+    float2 m[kAtOnce];
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      const int32_t k = i + q < to ? i + q : to - 1;
+      m[q] = maps[(int64_t)(FALLING ? hi - 1 - k : lo + k) * width + column + c];
+    }
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q)
+      if (i + q < to) all = then(all, m[q]);
+  }
+  part[threadIdx.x] = all;
+  __syncthreads();
+  if (seg == 0) {
+    float h = 0.0f;
+    for (int s = 0; s < segs; ++s) h = apply(part[s * slice + c].x, part[s * slice + c].y, h);
+    enter[c] = h;
+  }
+  __syncthreads();
+}
+
+// Sequences without rows leave the state they were given.
+__device__ __forceinline__ void pass_empty(const Args& a, int32_t n, const float* from, float* to, int slice) {
+  if (!to) return;
+  const int32_t per = (int32_t)(((int64_t)a.n_seq + gridDim.x - 1) / gridDim.x);
+  const int64_t lo = (int64_t)blockIdx.x * per, hi = lo + per < a.n_seq ? lo + per : a.n_seq;
+  for (int64_t j = lo + threadIdx.x; j < hi; j += kThreads) {
+    if (start_of(a, n, (int32_t)j + 1) > start_of(a, n, (int32_t)j)) continue;
+    const int64_t s = (int64_t)seq_of(a, (int32_t)j) * a.channels;
+    for (int32_t c = blockIdx.y * slice; c < (int32_t)(blockIdx.y + 1) * slice && c < a.channels; ++c) to[s + c] = from ? from[s + c] : 0.0f;
+  }
+}
+
+template <typename T, int N, int R>
+__global__ void __launch_bounds__(kThreads) k_recurrence(const Args a) {
+  constexpr int kSlice = 64;
+  __shared__ float2 total[2][kWaves][kSlice];
+  __shared__ int32_t starts[kWaves][64 * R], ends[kWaves][64 * R];
+  __shared__ float2 part[kThreads];
+  __shared__ float enter[kSlice];
+  const Place t = place_of<N>(a);
+  const int32_t n = rows_of(a);
+  if (gridDim.x == 1 && blockIdx.y == 0 && threadIdx.x == 0 && a.offsets[a.n_seq] > a.capacity) atomicOr(a.flags, EMC2_DEVFLAG_CAPACITY);
+  const int slice = N << a.lane_shift;
+  const int32_t tile_rows = kWaves * t.groups * R;
+  const int64_t first = (int64_t)blockIdx.x * a.tiles * tile_rows;
+  pass_empty(a, n, a.h0, a.last, slice);
+  if (first >= n) return;
+  emc2_fvec<N> h = emc2_fvec<N>(0.0f);                     // the state that enters the tile
+  int32_t j = 0, next = -1;
+  if (blockIdx.x > 0) {
+    compose<false>(a.block_f, a.width, blockIdx.y * slice, slice, 0, blockIdx.x, part, enter);
+#pragma unroll
+    for (int e = 0; e < N; ++e) h[e] = enter[t.column + e];
+    j = seek_far(a, n, (int32_t)first, t.lane);
+  }
+  for (int32_t k = 0; k < a.tiles; ++k) {
+    if (first + (int64_t)k * tile_rows >= n) break;
+    const int64_t row0 = first + (int64_t)k * tile_rows + t.wave * t.groups * R;
+    const int32_t row = (int32_t)row0 + t.group * R;
+    emc2_fvec<N> keep[R], add[R];
+    Map<N> m = nothing<N>();
+    bool marked = false;
+    if (row0 < n) {
+      const Rows<T, N, R> x = fetch<T, N, R>(a, a.x, a.ld_x, n, row, t), g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, row, t);
+      marked = mark(a, n, (int32_t)row0, t.groups * R, j, next, starts[t.wave], ends[t.wave], t.lane);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        emc2_fvec<N> take;
+        open<T, N>(g.v[i], keep[i], take);
+        add[i] = take * __builtin_convertvector(x.v[i], emc2_fvec<N>);
+      }
+      if (row0 + t.groups * R > n) blank<N, R>(n, row, keep, add);
+      m = run_forward<N, R>(a, keep, add, marked, &starts[t.wave][t.group * R], t);
+    }
+    // maps of all rows of the wave up to the group's last; then of those before its first
+    for (int dist = 1 << a.lane_shift; dist < 64; dist <<= 1) {
+      const Map<N> before = from_below<N>(m, dist);
+      if (t.lane >= dist) m = then<N>(before, m);
+    }
+    if (t.group == t.groups - 1) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) total[k & 1][t.wave][t.column + e] = make_float2(m.A[e], m.B[e]);
+    }
+    m = from_below<N>(m, 1 << a.lane_shift);
+    if (t.group == 0) m = nothing<N>();
+    __syncthreads();
+    emc2_fvec<N> leave = h;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w == t.wave) h = leave;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float2 q = total[k & 1][w][t.column + e];
+        leave[e] = apply(q.x, q.y, leave[e]);
+      }
+    }
+    h = apply<N>(m, h);
+    if (row0 < n) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int32_t r = row + i;
+        if (marked && starts[t.wave][t.group * R + i] >= 0) h = state_or_zero<N>(a.h0, a, starts[t.wave][t.group * R + i], t);
+        h = keep[i] * h + add[i];
+        if (r < n && t.in) {
+          emc2_store<N>((T*)a.y + (int64_t)(a.backwards ? n - 1 - r : r) * a.ld_y + t.channel, h);
+          if (marked && a.last && ends[t.wave][t.group * R + i] >= 0)
+            emc2_store_params<N>(a.last + (int64_t)ends[t.wave][t.group * R + i] * a.channels + t.channel, h);
+        }
+      }
+    }
+    h = leave;
+  }
+}
+
+template <typename T, int N, int R>
+__global__ void __launch_bounds__(kThreads) k_recurrence_grad(const Args a) {
+  constexpr int kSlice = 64;
+  __shared__ float2 total[2][2][kWaves][kSlice];
+  __shared__ int32_t starts[kWaves][64 * R], ends[kWaves][64 * R];
+  __shared__ float2 part[kThreads];
+  __shared__ float enter[kMaxTiles][kSlice], enter_r[kSlice];
+  const Place t = place_of<N>(a);
+  const int32_t n = rows_of(a);
+  if (gridDim.x == 1 && blockIdx.y == 0 && threadIdx.x == 0 && a.offsets[a.n_seq] > a.capacity) atomicOr(a.flags, EMC2_DEVFLAG_CAPACITY);
+  const int slice = N << a.lane_shift;
+  const int32_t tile_rows = kWaves * t.groups * R, block_rows = a.tiles * tile_rows;
+  const int64_t first = (int64_t)blockIdx.x * block_rows;
+  pass_empty(a, n, a.dlast, a.dh0, slice);
+  if (first >= n) return;
+  const int32_t here = (int32_t)((n - first + tile_rows - 1) / tile_rows), tiles = here < a.tiles ? here : a.tiles;
+  emc2_fvec<N> flow = emc2_fvec<N>(0.0f);                  // what flows into the tile from later rows
+  const int32_t blocks = (int32_t)(((int64_t)n + block_rows - 1) / block_rows);
+  if (blocks > 1 || tiles > 1) {
+    compose<false>(a.block_f, a.width, blockIdx.y * slice, slice, 0, blockIdx.x, part, enter[0]);
+    compose<true>(a.block_r, a.width, blockIdx.y * slice, slice, blockIdx.x + 1, blocks, part, enter_r);
+    if ((int)threadIdx.x < slice) {
+      float h = enter[0][threadIdx.x];
+      for (int32_t k = 1; k < tiles; ++k) {
+        const float2 q = a.tile_f[((int64_t)blockIdx.x * a.tiles + k - 1) * a.width + blockIdx.y * slice + threadIdx.x];
+        enter[k][threadIdx.x] = h = apply(q.x, q.y, h);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) flow[e] = enter_r[t.column + e];
+  } else if ((int)threadIdx.x < slice) {
+    enter[0][threadIdx.x] = 0.0f;
+  }
+  for (int32_t k = tiles - 1; k >= 0; --k) {
+    const int64_t row0 = first + (int64_t)k * tile_rows + t.wave * t.groups * R;
+    const int32_t row = (int32_t)row0 + t.group * R;
+    emc2_fvec<N> keep[R], take[R], x[R], dy[R];
+    Map<N> f = nothing<N>(), r = nothing<N>();
+    bool marked = false;
+    if (row0 < n) {
+      const Rows<T, N, R> xv = fetch<T, N, R>(a, a.x, a.ld_x, n, row, t), g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, row, t),
+                          d = fetch<T, N, R>(a, a.dy, a.ld_dy, n, row, t);
+      int32_t j = seek_far(a, n, (int32_t)row0, t.lane), next = -1;
+      marked = mark(a, n, (int32_t)row0, t.groups * R, j, next, starts[t.wave], ends[t.wave], t.lane);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        open<T, N>(g.v[i], keep[i], take[i]);
+        x[i] = __builtin_convertvector(xv.v[i], emc2_fvec<N>);
+        dy[i] = __builtin_convertvector(d.v[i], emc2_fvec<N>);
+      }
+      emc2_fvec<N> add[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) add[i] = take[i] * x[i];
+      if (row0 + t.groups * R > n) blank<N, R>(n, row, keep, add), blank<N, R>(n, row, keep, dy);
+      f = run_forward<N, R>(a, keep, add, marked, &starts[t.wave][t.group * R], t);
+      r = run_backward<N, R>(a, keep, dy, marked, &ends[t.wave][t.group * R], t);
+    }
+    for (int dist = 1 << a.lane_shift; dist < 64; dist <<= 1) {
+      const Map<N> before = from_below<N>(f, dist), after = from_above<N>(r, dist);
+      if (t.lane >= dist) f = then<N>(before, f);
+      if (t.lane + dist < 64) r = then<N>(after, r);
+    }
+    if (t.group == t.groups - 1) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) total[k & 1][0][t.wave][t.column + e] = make_float2(f.A[e], f.B[e]);
+    }
+    if (t.group == 0) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) total[k & 1][1][t.wave][t.column + e] = make_float2(r.A[e], r.B[e]);
+    }
+    f = from_below<N>(f, 1 << a.lane_shift), r = from_above<N>(r, 1 << a.lane_shift);
+    if (t.group == 0) f = nothing<N>();
+    if (t.group == t.groups - 1) r = nothing<N>();
+    __syncthreads();
+    emc2_fvec<N> h, u = flow;
+#pragma unroll
+    for (int e = 0; e < N; ++e) h[e] = enter[k][t.column + e];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      if (w < t.wave) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const float2 q = total[k & 1][0][w][t.column + e];
+          h[e] = apply(q.x, q.y, h[e]);
+        }
+      }
+#pragma unroll
+    for (int w = kWaves - 1; w >= 0; --w) {
+      if (w == t.wave) u = flow;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float2 q = total[k & 1][1][w][t.column + e];
+        flow[e] = apply(q.x, q.y, flow[e]);
+      }
+    }
+    if (row0 < n) {
+      h = apply<N>(f, h), u = apply<N>(r, u);
+      emc2_fvec<N> before[R];                              // h_{t-1}
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        if (marked && starts[t.wave][t.group * R + i] >= 0) h = state_or_zero<N>(a.h0, a, starts[t.wave][t.group * R + i], t);
+        before[i] = h;
+        h = keep[i] * h + take[i] * x[i];
+      }
+#pragma unroll
+      for (int i = R - 1; i >= 0; --i) {
+        const int32_t at = row + i;
+        if (marked && ends[t.wave][t.group * R + i] >= 0) u = state_or_zero<N>(a.dlast, a, ends[t.wave][t.group * R + i], t);
+        const emc2_fvec<N> du = dy[i] + u;
+        if (at < n) u = keep[i] * du;
+        if (at < n && t.in) {
+          const int64_t place = a.backwards ? n - 1 - at : at;
+          emc2_store<N>((T*)a.y + place * a.ld_y + t.channel, take[i] * du);
+          emc2_store<N>((T*)a.dgate + place * a.ld_dgate + t.channel, (before[i] - x[i]) * (keep[i] * take[i]) * du);
+          if (marked && a.dh0 && starts[t.wave][t.group * R + i] >= 0)
+            emc2_store_params<N>(a.dh0 + (int64_t)starts[t.wave][t.group * R + i] * a.channels + t.channel, u);
+        }
+      }
+    }
+  }
+}
+
+// One row per sequence: N channels of a row a thread.
+template <typename T, int N>
+__global__ void __launch_bounds__(kThreads) k_recurrence_step(const T* __restrict__ x, int64_t ld_x, const T* __restrict__ gate, int64_t ld_gate,
+                                                              const float* h_in, float* h_out, T* __restrict__ y, int64_t ld_y, int64_t rows,
+                                                              int32_t channels) {
+  const int32_t pieces = channels / N;
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= rows * pieces) return;
+  const int64_t row = i / pieces;
+  const int32_t c = (int32_t)(i - row * pieces) * N;
+  emc2_fvec<N> keep, take;
+  open<T, N>(*reinterpret_cast<const emc2_vec<T, N>*>(gate + row * ld_gate + c), keep, take);
+  const emc2_fvec<N> h = keep * emc2_load_params<N>(h_in + row * channels + c) + take * emc2_load<N>(x + row * ld_x + c);
+  emc2_store_params<N>(h_out + row * channels + c, h);
+  emc2_store<N>(y + row * ld_y + c, h);
+}
+
+// How a call is cut: row groups, tiles a block, blocks, and the pieces of the work buffer.
+struct Plan {
+  int n, lane_shift, slices;
+  int32_t tiles, blocks, width;
+  bool totals;                       // a first launch is needed
+  int64_t bytes;
+};
+Plan plan_of(emc2_dtype dtype, int64_t capacity, int32_t channels, bool wide, bool grad) {
+  Plan p = {};
+  p.n = wide ? (dtype == EMC2_F32 ? 4 : 8) : 1;
+  const int pieces = (channels + p.n - 1) / p.n, most = wide ? 3 : 6;     // row groups of 8 lanes at most, 64 of single values
+  while (p.lane_shift < most && (1 << p.lane_shift) < pieces) ++p.lane_shift;
+  const int slice = p.n << p.lane_shift;
+  p.slices = (channels + slice - 1) / slice;
+  p.width = p.slices * slice;
+  const int64_t tile_rows = kWaves * (64 >> p.lane_shift) * (grad ? kRowsGrad : kRowsForward), tiles = emc2_div_up(capacity, tile_rows);
+  // A call of a few tiles is one launch of one block a slice, which walks them; others have about 512 blocks, two for every CU.
+  if (tiles <= (grad ? 1 : 4)) {
+    p.tiles = tiles < 1 ? 1 : (int32_t)tiles, p.blocks = 1;
+  } else {
+    const int64_t aim = 512 / p.slices > 1 ? 512 / p.slices : 1, per = emc2_div_up(tiles, aim);
+    p.tiles = (int32_t)(per < kMaxTiles ? per : kMaxTiles);
+    p.blocks = (int32_t)emc2_div_up(tiles, p.tiles);
+    p.totals = true;
+  }
+  p.bytes = p.totals ? (int64_t)p.blocks * p.width * (int64_t)sizeof(float2) * (grad ? 2 + p.tiles : 1) : 0;
+  return p;
+}
+
+template <typename F> void with_type(emc2_dtype dtype, int n, F&& f) {
+  if (dtype == EMC2_F32) {
+    if (n == 4) f(float(), emc2_fvec<4>());
+    else f(float(), emc2_fvec<1>());
+  } else if (dtype == EMC2_F16) {
+    if (n == 8) f(_Float16(), emc2_fvec<8>());
+    else f(_Float16(), emc2_fvec<1>());
+  } else {
+    if (n == 8) f(__bf16(), emc2_fvec<8>());
+    else f(__bf16(), emc2_fvec<1>());
+  }
+}
+template <typename V> constexpr int kLength = sizeof(V) / sizeof(float);
+
+__global__ void __launch_bounds__(kThreads) k_frame_offsets(const int4* __restrict__ coords, const int32_t* __restrict__ d_n, int64_t capacity,
+                                                            int32_t n_batch, int32_t* __restrict__ offsets) {
+  const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (b > n_batch) return;
+  int32_t lo = 0, hi = emc2_row_count(d_n, capacity);
+  if (b == n_batch) lo = hi;                               // every row, also one whose frame id is out of range, belongs to some frame
+  if (b == 0) hi = 0;
+  while (lo < hi) {                                        // the first row of a frame >= b
+    const int32_t mid = lo + (hi - lo) / 2;
+    if (coords[mid].x < b) lo = mid + 1;
+    else hi = mid;
+  }
+  offsets[b] = lo;
+}
+
+emc2_status check(emc2_ctx* ctx, const char* what, emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t n_seq, const void* offsets) {
+  if (!emc2_is_float(dtype)) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "%s: dtype must be F32, F16 or BF16", what);
+  if (channels < 1 || channels > (1 << 16)) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "%s: channels outside [1, 2^16]", what);
+  if (capacity < 0 || capacity > (1ll << 30)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: capacity outside [0, 2^30]", what);
+  if (n_seq < 1 || n_seq > (1 << 30) || !offsets) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: offsets null or n_seq outside [1, 2^30]", what);
+  return EMC2_OK;
+}
+bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+}  // namespace
+
+extern "C" emc2_status emc2_frame_offsets(emc2_ctx* ctx, const int32_t* d_coords, const int32_t* d_n, int64_t capacity, int32_t n_batch,
+                                          int32_t* d_offsets, void* stream) {
+  if (!ctx) return EMC2_ERR_INVALID_ARG;
+  if (!d_offsets || (!d_coords && capacity > 0)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_frame_offsets: null argument");
+  if (capacity < 0 || capacity > (1ll << 30) || n_batch < 1 || n_batch > (1 << 30))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_frame_offsets: capacity outside [0, 2^30] or n_batch outside [1, 2^30]");
+  if (!aligned(d_coords)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_frame_offsets: d_coords must be 16-byte aligned");
+  hipLaunchKernelGGL(k_frame_offsets, dim3((unsigned)emc2_div_up((int64_t)n_batch + 1, kThreads)), dim3(kThreads), 0, (hipStream_t)stream,
+                     (const int4*)d_coords, d_n, capacity, n_batch, d_offsets);
+  return emc2_check_hip(ctx, hipGetLastError(), "emc2_frame_offsets launch");
+}
+
+extern "C" int64_t emc2_recurrence_work(emc2_dtype dtype, int64_t capacity, int32_t channels) {
+  if (!emc2_is_float(dtype) || channels < 1 || channels > (1 << 16) || capacity < 0 || capacity > (1ll << 30)) return -1;
+  int64_t most = 0;
+  for (int i = 0; i < 4; ++i) {
+    const int64_t b = plan_of(dtype, capacity, channels, i & 1, i & 2).bytes;
+    most = b > most ? b : most;
+  }
+  return most;
+}
+
+extern "C" emc2_status emc2_recurrence(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate,
+                                       const int32_t* d_offsets, int32_t n_seq, int64_t capacity, int32_t channels, int32_t backwards,
+                                       const float* d_h0, void* d_y, int64_t ld_y, float* d_last, void* d_work, int64_t work_bytes,
+                                       void* stream) {
+  if (!ctx) return EMC2_ERR_INVALID_ARG;
+  const emc2_status st = check(ctx, "emc2_recurrence", dtype, capacity, channels, n_seq, d_offsets);
+  if (st != EMC2_OK) return st;
+  const size_t size = emc2_size_of(dtype);
+  const bool none = capacity == 0;
+  if (!emc2_rows_ok(d_x, ld_x, channels, size, none) || !emc2_rows_ok(d_gate, ld_gate, channels, size, none) ||
+      !emc2_rows_ok(d_y, ld_y, channels, size, none))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence: null or misaligned rows, or a pitch below the channels");
+  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_gate, ld_gate, size) &&
+                    emc2_wide_rows(d_y, ld_y, size) && aligned(d_h0) && aligned(d_last);
+  const Plan p = plan_of(dtype, capacity, channels, wide, false);
+  if (work_bytes < p.bytes || (p.bytes && (!d_work || !aligned(d_work))))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence: work buffer null, misaligned or smaller than emc2_recurrence_work");
+  Args a = {};
+  a.x = d_x, a.gate = d_gate, a.h0 = d_h0, a.offsets = d_offsets, a.y = d_y, a.last = d_last, a.block_f = (float2*)d_work;
+  a.flags = ctx->dev_words, a.ld_x = ld_x, a.ld_gate = ld_gate, a.ld_y = ld_y, a.capacity = (int32_t)capacity, a.channels = channels;
+  a.width = p.width, a.n_seq = n_seq, a.tiles = p.tiles, a.backwards = backwards != 0, a.lane_shift = p.lane_shift;
+  const dim3 grid((unsigned)p.blocks, (unsigned)p.slices);
+  with_type(dtype, p.n, [&](auto type, auto length) {
+    using T = decltype(type);
+    constexpr int N = kLength<decltype(length)>;
+    if (p.totals) hipLaunchKernelGGL((k_recurrence_totals<T, N, kRowsForward, false>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((k_recurrence<T, N, kRowsForward>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+  });
+  return emc2_check_hip(ctx, hipGetLastError(), "emc2_recurrence launch");
+}
+
+extern "C" emc2_status emc2_recurrence_backward(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_gate,
+                                                int64_t ld_gate, const int32_t* d_offsets, int32_t n_seq, int64_t capacity, int32_t channels,
+                                                int32_t backwards, const float* d_h0, const void* d_dy, int64_t ld_dy, const float* d_dlast,
+                                                void* d_dx, int64_t ld_dx, void* d_dgate, int64_t ld_dgate, float* d_dh0, void* d_work,
+                                                int64_t work_bytes, void* stream) {
+  if (!ctx) return EMC2_ERR_INVALID_ARG;
+  const emc2_status st = check(ctx, "emc2_recurrence_backward", dtype, capacity, channels, n_seq, d_offsets);
+  if (st != EMC2_OK) return st;
+  const size_t size = emc2_size_of(dtype);
+  const bool none = capacity == 0;
+  if (!emc2_rows_ok(d_x, ld_x, channels, size, none) || !emc2_rows_ok(d_gate, ld_gate, channels, size, none) ||
+      !emc2_rows_ok(d_dy, ld_dy, channels, size, none) || !emc2_rows_ok(d_dx, ld_dx, channels, size, none) ||
+      !emc2_rows_ok(d_dgate, ld_dgate, channels, size, none))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_backward: null or misaligned rows, or a pitch below the channels");
+  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_gate, ld_gate, size) &&
+                    emc2_wide_rows(d_dy, ld_dy, size) && emc2_wide_rows(d_dx, ld_dx, size) && emc2_wide_rows(d_dgate, ld_dgate, size) &&
+                    aligned(d_h0) && aligned(d_dlast) && aligned(d_dh0);
+  const Plan p = plan_of(dtype, capacity, channels, wide, true);
+  if (work_bytes < p.bytes || (p.bytes && (!d_work || !aligned(d_work))))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_backward: work buffer null, misaligned or smaller than emc2_recurrence_work");
+  Args a = {};
+  a.x = d_x, a.gate = d_gate, a.dy = d_dy, a.h0 = d_h0, a.dlast = d_dlast, a.offsets = d_offsets, a.y = d_dx, a.dgate = d_dgate, a.dh0 = d_dh0;
+  a.block_f = (float2*)d_work, a.block_r = a.block_f + (int64_t)p.blocks * p.width, a.tile_f = a.block_r + (int64_t)p.blocks * p.width;
+  a.flags = ctx->dev_words, a.ld_x = ld_x, a.ld_gate = ld_gate, a.ld_dy = ld_dy, a.ld_y = ld_dx, a.ld_dgate = ld_dgate;
+  a.capacity = (int32_t)capacity, a.channels = channels, a.width = p.width, a.n_seq = n_seq, a.tiles = p.tiles;
+  a.backwards = backwards != 0, a.lane_shift = p.lane_shift;
+  const dim3 grid((unsigned)p.blocks, (unsigned)p.slices);
+  with_type(dtype, p.n, [&](auto type, auto length) {
+    using T = decltype(type);
+    constexpr int N = kLength<decltype(length)>;
+    if (p.totals) hipLaunchKernelGGL((k_recurrence_totals<T, N, kRowsGrad, true>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((k_recurrence_grad<T, N, kRowsGrad>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+  });
+  return emc2_check_hip(ctx, hipGetLastError(), "emc2_recurrence_backward launch");
+}
+
+extern "C" emc2_status emc2_recurrence_step(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate,
+                                            const float* d_h, int64_t rows, int32_t channels, float* d_h_out, void* d_y, int64_t ld_y,
+                                            void* stream) {
+  if (!ctx) return EMC2_ERR_INVALID_ARG;
+  if (!emc2_is_float(dtype)) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "emc2_recurrence_step: dtype must be F32, F16 or BF16");
+  if (channels < 1 || channels > (1 << 16)) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "emc2_recurrence_step: channels outside [1, 2^16]");
+  if (rows < 0 || rows > (1ll << 30)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_step: rows outside [0, 2^30]");
+  const size_t size = emc2_size_of(dtype);
+  if (rows == 0) return EMC2_OK;
+  if (!d_h || !d_h_out) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_step: null argument");
+  if (!emc2_rows_ok(d_x, ld_x, channels, size, false) || !emc2_rows_ok(d_gate, ld_gate, channels, size, false) ||
+      !emc2_rows_ok(d_y, ld_y, channels, size, false))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_step: null or misaligned rows, or a pitch below the channels");
+  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_gate, ld_gate, size) &&
+                    emc2_wide_rows(d_y, ld_y, size) && aligned(d_h) && aligned(d_h_out);
+  const int n = wide ? (dtype == EMC2_F32 ? 4 : 8) : 1;
+  const int64_t blocks = emc2_div_up(rows * (channels / n), kThreads);
+  if (blocks > 0x7fffffff) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "emc2_recurrence_step: too many rows for one launch");
+  with_type(dtype, n, [&](auto type, auto length) {
+    using T = decltype(type);
+    constexpr int N = kLength<decltype(length)>;
+    hipLaunchKernelGGL((k_recurrence_step<T, N>), dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, (const T*)d_x, ld_x,
+                       (const T*)d_gate, ld_gate, d_h, d_h_out, (T*)d_y, ld_y, rows, channels);
+  });
+  return emc2_check_hip(ctx, hipGetLastError(), "emc2_recurrence_step launch");
+}
