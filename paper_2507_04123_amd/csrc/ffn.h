@@ -33,12 +33,12 @@ template <typename T> __host__ __device__ __forceinline__ constexpr int emc2_hid
   return emc2_tile<T>::kDeep * m + 8 * (e / 4) + 4 * half + e % 4;
 }
 
-// Packed weights: for every slice of 32 hidden units six groups of width / KF fragments (width: C rounded up to 32s, zeros beyond C and F):
-enum emc2_ffn_group {
+// Packed weights: for every slice of 32 hidden units (an even number of slices) six groups of width / KF fragments (width: C rounded up to 32s, zeros beyond C and F):
+enum emc2_ffn_group {   // the forward pass takes the first three, dx the last five, the weights' gradients the three from EMC2_FFN_GATE on
+  EMC2_FFN_DOWN,        // Wd: line = channel (fragment ct * 32 / KF + m: channels 32 ct ..), along = hidden units in the order of a result tile
   EMC2_FFN_GATE,        // Wg: line = hidden unit, along = channel
   EMC2_FFN_UP,          // Wu: the same
-  EMC2_FFN_DOWN,        // Wd: line = channel (fragment ct * 32 / KF + m: channels 32 ct ..), along = hidden units in the order of a result tile
-  EMC2_FFN_DOWN_T,      // Wd: line = hidden unit, along = channel
+  EMC2_FFN_DOWN_T,      // Wd: the same
   EMC2_FFN_GATE_T,      // Wg: line = channel, along = hidden units in the order of a result tile
   EMC2_FFN_UP_T,        // Wu: the same
   EMC2_FFN_GROUPS
@@ -46,16 +46,15 @@ enum emc2_ffn_group {
 
 template <typename T> __device__ __forceinline__ typename emc2_tile<T>::frag emc2_zero_frag() { return typename emc2_tile<T>::frag(T(0)); }
 
-// The fragment of row `row`, along channels kk KF ..; zero beyond the rows and channels.
-template <typename T>
-__device__ __forceinline__ typename emc2_tile<T>::frag emc2_row_frag(const T* p, int64_t ld, int64_t row, int32_t n, int32_t channels, bool wide,
-                                                                      int kk, int half) {
+// The fragment of row `row`, along channels kk KF ..; zero beyond the rows and channels.  WIDE: rows in 16-byte pieces.
+template <typename T, bool WIDE>
+__device__ __forceinline__ typename emc2_tile<T>::frag emc2_row_frag(const T* p, int64_t ld, int64_t row, int32_t n, int32_t channels, int kk, int half) {
   typedef emc2_tile<T> M;
   const int c = kk * M::kDeep + half * M::kPer;
   typename M::frag f = emc2_zero_frag<T>();
   if (row < n && c < channels) {
     const T* q = p + row * ld + c;
-    if (wide) {
+    if constexpr (WIDE) {
       f = *reinterpret_cast<const typename M::frag*>(q);
     } else {
 #pragma unroll
@@ -67,7 +66,7 @@ __device__ __forceinline__ typename emc2_tile<T>::frag emc2_row_frag(const T* p,
 }
 
 // The fragments of a row: kept in registers, or (wide rows of fp32, which would take half of them) read again for every use.
-template <typename T, int CT> struct emc2_row {
+template <typename T, int CT, bool WIDE> struct emc2_row {
   typedef emc2_tile<T> M;
   static constexpr int KK = 32 * CT / M::kDeep;
   static constexpr bool kKept = sizeof(T) * CT <= 16;
@@ -76,12 +75,11 @@ template <typename T, int CT> struct emc2_row {
   int64_t ld, row;
   int32_t n, channels;
   int half;
-  bool wide;
-  __device__ __forceinline__ void set(const void* p_, int64_t ld_, int64_t row_, int32_t n_, const bool wide_, int32_t channels_, int half_) {
-    p = (const T*)p_, ld = ld_, row = row_, n = n_, wide = wide_, channels = channels_, half = half_;
+  __device__ __forceinline__ void set(const void* p_, int64_t ld_, int64_t row_, int32_t n_, int32_t channels_, int half_) {
+    p = (const T*)p_, ld = ld_, row = row_, n = n_, channels = channels_, half = half_;
     if constexpr (kKept) {
 #pragma unroll
-      for (int k = 0; k < KK; ++k) f[k] = emc2_row_frag<T>(p, ld, row, n, channels, wide, k, half);
+      for (int k = 0; k < KK; ++k) f[k] = emc2_row_frag<T, WIDE>(p, ld, row, n, channels, k, half);
     }
   }
   // before a loop's turn: what is read again is not moved out of the loop
@@ -90,23 +88,35 @@ template <typename T, int CT> struct emc2_row {
   }
   __device__ __forceinline__ typename M::frag operator[](int k) const {
     if constexpr (kKept) return f[k];
-    else return emc2_row_frag<T>(p, ld, row, n, channels, wide, k, half);
+    else return emc2_row_frag<T, WIDE>(p, ld, row, n, channels, k, half);
   }
 };
 
 // act(g) of either activation as g s, s = logistic(z): SiLU z = g, GELU (its tanh form) z = sqrt(8 / pi) (g + 0.044715 g^3); and the slope
 // s (1 + g (1 - s) dz/dg).
-template <bool EXACT> __device__ __forceinline__ float emc2_activate(bool gelu, float g) {
+template <bool EXACT, bool GELU> __device__ __forceinline__ float emc2_activate(float g) {
   float s, rest;
-  emc2_logistic<EXACT>(gelu ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g, s, rest);
+  emc2_logistic<EXACT>(GELU ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g, s, rest);
   return g * s;
 }
-template <bool EXACT> __device__ __forceinline__ float emc2_activate(bool gelu, float g, float& slope) {
+template <bool EXACT, bool GELU> __device__ __forceinline__ float emc2_activate(float g, float& slope) {
   float s, rest;
-  emc2_logistic<EXACT>(gelu ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g, s, rest);
-  const float dz = gelu ? 1.5957691216057308f * (1.0f + 0.134145f * g * g) : 1.0f;
+  emc2_logistic<EXACT>(GELU ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g, s, rest);
+  const float dz = GELU ? 1.5957691216057308f * (1.0f + 0.134145f * g * g) : 1.0f;
   slope = s + g * s * rest * dz;
   return g * s;
+}
+// Two neighbouring values of a result tile, registers r and r + 1 (r even), into the fragments made of it.
+template <typename T> __device__ __forceinline__ void emc2_put_pair(typename emc2_tile<T>::frag* f, int r, float a, float b) {
+  constexpr int kPer = emc2_tile<T>::kPer;
+  const emc2_vec<T, 2> v = __builtin_convertvector((emc2_fvec<2>{a, b}), emc2_vec<T, 2>);
+  if constexpr (sizeof(T) == 2) {
+    emc2_vec<uint32_t, 4> w = __builtin_bit_cast(emc2_vec<uint32_t, 4>, f[r / kPer]);
+    w[r % kPer / 2] = __builtin_bit_cast(uint32_t, v);
+    f[r / kPer] = __builtin_bit_cast(typename emc2_tile<T>::frag, w);
+  } else {
+    f[r / kPer][r % kPer] = v[0], f[r / kPer][r % kPer + 1] = v[1];
+  }
 }
 
 // Arguments of a launch.
@@ -117,26 +127,32 @@ struct emc2_ffn_args {
   const int32_t* d_n;
   int64_t ld_x, ld_res, ld_dy, ld_y, capacity;
   int32_t channels, hidden, slices, parts;
-  bool gelu, wide;
 };
 
 static inline int emc2_ffn_tiles(int32_t channels) {        // 32-wide tiles of channels that the kernels are made for
   const int t = (channels + 31) / 32;
   return t <= 4 ? t : t <= 6 ? 6 : 8;
 }
+static inline int32_t emc2_ffn_slices(int32_t hidden) { return (hidden + 63) / 64 * 2; }
 constexpr int kFfnMaxChannels = 256, kFfnMaxHidden = 1 << 16;
 
-// Calls f with a value of the type and the number of tiles as a constant.
+// Calls f with a value of the type, and as constants the number of tiles, whether the activation is GELU and whether rows move in 16-byte pieces.
 template <int N> struct emc2_const { static constexpr int value = N; };
-template <typename F> void emc2_ffn_dispatch(emc2_dtype dtype, int tiles, F&& f) {
+template <typename F> void emc2_ffn_dispatch(emc2_dtype dtype, int tiles, bool gelu, bool wide, F&& f) {
+  const auto by_act = [&](auto type, auto count) {
+    if (gelu && wide) f(type, count, emc2_const<1>(), emc2_const<1>());
+    else if (gelu) f(type, count, emc2_const<1>(), emc2_const<0>());
+    else if (wide) f(type, count, emc2_const<0>(), emc2_const<1>());
+    else f(type, count, emc2_const<0>(), emc2_const<0>());
+  };
   const auto by_tiles = [&](auto type) {
     switch (tiles) {
-      case 1: return f(type, emc2_const<1>());
-      case 2: return f(type, emc2_const<2>());
-      case 3: return f(type, emc2_const<3>());
-      case 4: return f(type, emc2_const<4>());
-      case 6: return f(type, emc2_const<6>());
-      default: return f(type, emc2_const<8>());
+      case 1: return by_act(type, emc2_const<1>());
+      case 2: return by_act(type, emc2_const<2>());
+      case 3: return by_act(type, emc2_const<3>());
+      case 4: return by_act(type, emc2_const<4>());
+      case 6: return by_act(type, emc2_const<6>());
+      default: return by_act(type, emc2_const<8>());
     }
   };
   if (dtype == EMC2_F32) by_tiles(float());

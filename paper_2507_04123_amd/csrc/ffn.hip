@@ -7,25 +7,153 @@
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kFewRows = 16384;
 
-template <typename T, int CT>
-__global__ void __launch_bounds__(kThreads) k_ffn(const emc2_ffn_args a) {
+// Four neighbouring values of a result's row, from channel `at` on.
+template <typename T, bool WIDE> __device__ __forceinline__ void put(const emc2_ffn_args& a, int64_t row, int at, emc2_fvec<4> v) {
+  T* out = (T*)a.y + row * a.ld_y + at;
+  const T* res = (const T*)a.res + row * a.ld_res + at;
+  if constexpr (WIDE) {
+    if (at >= a.channels) return;
+    if (a.res) v += emc2_load<4>(res);
+    emc2_store<4>(out, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (at + i < a.channels) out[i] = (T)(v[i] + (a.res ? (float)res[i] : 0.0f));
+  }
+}
+
+// H's registers r and r + 1, as operands
+template <typename T, bool GELU>
+__device__ __forceinline__ void hidden(const emc2_acc& g, const emc2_acc& u, int r, typename emc2_tile<T>::frag* h) {
+  constexpr bool kExact = sizeof(T) == 4;
+  emc2_put_pair<T>(h, r, emc2_activate<kExact, GELU>(g[r]) * u[r], emc2_activate<kExact, GELU>(g[r + 1]) * u[r + 1]);
+}
+
+template <bool GATES, bool ACT, bool DOWN> struct Stages { static constexpr bool gates = GATES, act = ACT, down = DOWN; };
+template <int V> struct Now { static constexpr int value = V; };
+
+// Waves a SIMD of the kernel below: two where 256 registers hold x, y's sums, and G and U twice
+template <typename T, int CT> constexpr int kFfnWaves = sizeof(T) * CT <= 8 ? 2 : 1;
+
+// Many rows: a block of four waves has 128 rows and passes the weights, slice by slice, through LDS, where all waves read them.  Turn t multiplies
+// slice t's gates, activates slice t - 1 and multiplies slice t - 2's way down: three independent strands, so that the vector ALU's
+// activation (two quarter-rate instructions an element) runs under the matrix cores' products.  The loads of turn t + 1's
+// weights are under way meanwhile.
+constexpr int kManyWaves = 4;
+template <typename T, int CT, bool GELU, bool WIDE>
+__global__ void __launch_bounds__(64 * kManyWaves, (kFfnWaves<T, CT>)) k_ffn(const emc2_ffn_args a) {
   typedef emc2_tile<T> M;
   typedef typename M::frag frag;
-  constexpr int KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep;
+  constexpr int W = kManyWaves, KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep;
+  __shared__ frag ring[2][3 * KK * 64];    // lines down, then gates (two products' fragments)
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int64_t row = ((int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * 32 + (lane & 31);
-  if (row - (lane & 31) >= n) return;
-  emc2_row<T, CT> x;
-  x.set(a.x, a.ld_x, row, n, a.wide, a.channels, half);
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((int64_t)blockIdx.x * W * 32 >= n) return;
+  const int64_t row = ((int64_t)blockIdx.x * W + wave) * 32 + (lane & 31);
+  emc2_row<T, CT, WIDE> x;
+  x.set(a.x, a.ld_x, row, n, a.channels, half);
   emc2_acc y[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) y[c] = 0.0f;
-  const frag* w = (const frag*)a.packed + lane;
-  for (int32_t s = 0; s < a.slices; ++s, w += EMC2_FFN_GROUPS * KK * 64) {
-    emc2_acc g = 0.0f, u = 0.0f;
+  emc2_acc g[2], u[2];                   // of the slice whose gates were multiplied last, and of this turn's
+  frag h[2][MM];                         // likewise
+  const frag* packed = (const frag*)a.packed + lane;
+  // A turn's weights, fragment by fragment over the waves: gates of slice t + 1 and lines down of slice t - 1, by way of registers (loads
+  // straight into LDS are waited for, all of them, before the next read of LDS).
+  constexpr int kStaged = (3 * KK + W - 1) / W;
+  frag staged[kStaged];
+  const auto fetch = [&](int32_t t) {
+#pragma unroll
+    for (int i = 0; i < kStaged; ++i) {                    // (beyond the last fragment or slice: the last one again, which hurts nobody)
+      const int f = min(wave + i * W, 3 * KK - 1), ahead = min(f / KK, 1);
+      const int32_t slice = max(0, min(t - 1 + 2 * ahead, a.slices - 1));
+      staged[i] = packed[((int64_t)slice * EMC2_FFN_GROUPS * KK + f) * 64];
+    }
+  };
+  const auto keep = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < kStaged; ++i) ring[buf][min(wave + i * W, 3 * KK - 1) * 64 + lane] = staged[i];
+  };
+  const auto all_here = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  // one turn: of slices t, t - 1 and t - 2 (parity NOW = t % 2), whichever there are
+  const auto turn = [&](auto stages, auto parity, int32_t t) {
+    constexpr bool kGates = decltype(stages)::gates, kAct = decltype(stages)::act, kDown = decltype(stages)::down;
+    constexpr int now = decltype(parity)::value;
+    all_here();
+    fetch(t);
+    __builtin_amdgcn_sched_barrier(0);
+    const frag* w = ring[now] + lane;
     x.again();
+    if constexpr (kGates) g[now] = 0.0f, u[now] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      if constexpr (kGates) {
+        g[now] = emc2_mma<T>(w[(KK + k) * 64], x[k], g[now]);
+        u[now] = emc2_mma<T>(w[(2 * KK + k) * 64], x[k], u[now]);
+      }
+      if constexpr (kDown) y[k / MM] = emc2_mma<T>(w[k * 64], h[now][k % MM], y[k / MM]);
+      if constexpr (kAct) {
+#pragma unroll
+        for (int r = 8 * k / KK; r < 8 * (k + 1) / KK; ++r) hidden<T, GELU>(g[now ^ 1], u[now ^ 1], 2 * r, h[now ^ 1]);
+      }
+    }
+    if constexpr (kGates && kAct && kDown && sizeof(T) == 2) {
+      // the order that the scheduler is to find: the next fragments ahead (two k's, one where registers are short), and after every product
+      // its share of the activation
+      __builtin_amdgcn_sched_group_barrier(0x100, CT == 6 ? 3 : 6, 0);
+#pragma unroll
+      for (int i = 0; i < 3 * KK; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, (32 + 3 * KK - 1) / (3 * KK), 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, (72 + 3 * KK - 1) / (3 * KK), 0);
+        if (i % 3 == 2) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    keep(now ^ 1);
+  };
+  fetch(-1);
+  keep(0);
+  turn(Stages<true, false, false>(), Now<0>(), 0);         // slices come in pairs, the second one of zeros where F ends in the first
+  turn(Stages<true, true, false>(), Now<1>(), 1);
+  for (int32_t t = 2; t < a.slices; t += 2) {
+    turn(Stages<true, true, true>(), Now<0>(), t);
+    turn(Stages<true, true, true>(), Now<1>(), t + 1);
+  }
+  turn(Stages<false, true, true>(), Now<0>(), a.slices);
+  turn(Stages<false, false, true>(), Now<1>(), a.slices + 1);
+  if (row >= n) return;
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      put<T, WIDE>(a, row, 32 * c + 8 * j + 4 * half, emc2_fvec<4>{y[c][4 * j], y[c][4 * j + 1], y[c][4 * j + 2], y[c][4 * j + 3]});
+}
+
+// Few rows: a block has 32 of them, its waves share the slices out, each reading its own from memory at once, and their sums meet in LDS.
+template <int CT, bool WIDE> constexpr int kFewWaves = CT == 8 && !WIDE ? 4 : 8;   // (four: rows value by value take more registers)
+template <typename T, int CT, bool GELU, bool WIDE>
+__global__ void __launch_bounds__((64 * kFewWaves<CT, WIDE>)) k_ffn_few(const emc2_ffn_args a) {
+  typedef emc2_tile<T> M;
+  typedef typename M::frag frag;
+  constexpr int KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep;
+  constexpr int kWaves = kFewWaves<CT, WIDE>;
+  __shared__ emc2_fvec<4> part[kWaves][4][64];
+  const int32_t n = emc2_row_count(a.d_n, a.capacity);
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((int64_t)blockIdx.x * 32 >= n) return;
+  const int64_t row = (int64_t)blockIdx.x * 32 + (lane & 31);
+  emc2_row<T, CT, WIDE> x;
+  x.set(a.x, a.ld_x, row, n, a.channels, half);
+  emc2_acc y[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) y[c] = 0.0f;
+  for (int32_t s = wave; s < a.slices; s += kWaves) {
+    const frag* w = (const frag*)a.packed + (int64_t)s * EMC2_FFN_GROUPS * KK * 64 + lane;
+    x.again();
+    emc2_acc g = 0.0f, u = 0.0f;
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
       g = emc2_mma<T>(w[(EMC2_FFN_GATE * KK + k) * 64], x[k], g);
@@ -33,36 +161,24 @@ __global__ void __launch_bounds__(kThreads) k_ffn(const emc2_ffn_args a) {
     }
     frag h[MM];
 #pragma unroll
-    for (int m = 0; m < MM; ++m)
+    for (int r = 0; r < 16; r += 2) hidden<T, GELU>(g, u, r, h);
+    if constexpr (CT == 8) __builtin_amdgcn_sched_barrier(0);   // no loads further ahead: registers
 #pragma unroll
-      for (int e = 0; e < M::kPer; ++e) {
-        const int r = m * M::kPer + e;
-        h[m][e] = (T)(emc2_activate<sizeof(T) == 4>(a.gelu, g[r]) * u[r]);
-      }
-#pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-      for (int m = 0; m < MM; ++m) y[c] = emc2_mma<T>(w[(EMC2_FFN_DOWN * KK + c * MM + m) * 64], h[m], y[c]);
+    for (int k = 0; k < KK; ++k) y[k / MM] = emc2_mma<T>(w[(EMC2_FFN_DOWN * KK + k) * 64], h[k % MM], y[k / MM]);
   }
-  if (row >= n) return;
 #pragma unroll
-  for (int c = 0; c < CT; ++c)
+  for (int c = 0; c < CT; ++c) {
+    if (c) __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int at = 32 * c + 8 * j + 4 * half;
-      emc2_fvec<4> v = {y[c][4 * j], y[c][4 * j + 1], y[c][4 * j + 2], y[c][4 * j + 3]};
-      T* out = (T*)a.y + row * a.ld_y + at;
-      const T* res = (const T*)a.res + row * a.ld_res + at;
-      if (a.wide) {
-        if (at >= a.channels) continue;
-        if (a.res) v += emc2_load<4>(res);
-        emc2_store<4>(out, v);
-      } else {
+    for (int j = 0; j < 4; ++j) part[wave][j][lane] = emc2_fvec<4>{y[c][4 * j], y[c][4 * j + 1], y[c][4 * j + 2], y[c][4 * j + 3]};
+    __syncthreads();
+    if (wave < 4 && row < n) {
+      emc2_fvec<4> v = part[0][wave][lane];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (at + i < a.channels) out[i] = (T)(v[i] + (a.res ? (float)res[i] : 0.0f));
-      }
+      for (int w = 1; w < kWaves; ++w) v += part[w][wave][lane];
+      put<T, WIDE>(a, row, 32 * c + 8 * wave + 4 * half, v);
     }
+  }
 }
 
 // One lane's 16 bytes of a fragment a thread.
@@ -91,7 +207,7 @@ __global__ void __launch_bounds__(kThreads) k_ffn_pack(const T* __restrict__ wg,
 }
 
 int64_t packed_values(int32_t channels, int32_t hidden) {
-  return (int64_t)EMC2_FFN_GROUPS * 32 * emc2_ffn_tiles(channels) * 32 * ((hidden + 31) / 32);
+  return (int64_t)EMC2_FFN_GROUPS * 32 * emc2_ffn_tiles(channels) * 32 * emc2_ffn_slices(hidden);
 }
 
 }  // namespace
@@ -151,13 +267,19 @@ extern "C" emc2_status emc2_ffn(emc2_ctx* ctx, emc2_dtype dtype, int32_t activat
   if (none) return EMC2_OK;
   emc2_ffn_args a = {};
   a.x = d_x, a.res = d_res, a.packed = d_packed, a.y = d_y, a.d_n = d_n, a.ld_x = ld_x, a.ld_res = ld_res, a.ld_y = ld_y;
-  a.capacity = capacity, a.channels = channels, a.hidden = hidden, a.slices = (hidden + 31) / 32, a.gelu = activation == EMC2_ACT_GELU;
-  a.wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_y, ld_y, size) &&
+  a.capacity = capacity, a.channels = channels, a.hidden = hidden, a.slices = emc2_ffn_slices(hidden);
+  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_y, ld_y, size) &&
            (!d_res || emc2_wide_rows(d_res, ld_res, size));
-  emc2_ffn_dispatch(dtype, emc2_ffn_tiles(channels), [&](auto type, auto tiles) {
+  emc2_ffn_dispatch(dtype, emc2_ffn_tiles(channels), activation == EMC2_ACT_GELU, wide, [&](auto type, auto tiles, auto gelu, auto pieces) {
     using T = decltype(type);
     constexpr int CT = decltype(tiles)::value;
-    hipLaunchKernelGGL((k_ffn<T, CT>), dim3((unsigned)emc2_div_up(capacity, 128)), dim3(kThreads), 0, (hipStream_t)stream, a);
+    constexpr bool G = decltype(gelu)::value, P = decltype(pieces)::value;
+        // up to 16 384 rows there are more CUs than blocks of 128 rows need; fp32 rows of over 64 channels would leave a SIMD one wave
+    constexpr bool kFew = sizeof(T) * CT > 8 && sizeof(T) == 4;
+    if (kFew || capacity <= kFewRows)
+      hipLaunchKernelGGL((k_ffn_few<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32)), dim3(64 * kFewWaves<CT, P>), 0, (hipStream_t)stream, a);
+    else if constexpr (!kFew)
+      hipLaunchKernelGGL((k_ffn<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32 * kManyWaves)), dim3(64 * kManyWaves), 0, (hipStream_t)stream, a);
   });
   return emc2_check_hip(ctx, hipGetLastError(), "emc2_ffn launch");
 }

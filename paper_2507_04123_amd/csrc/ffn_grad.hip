@@ -4,7 +4,7 @@
 // and dU would move six times n F values.
 // k_ffn_dx works like the forward pass: hidden units along the lanes' registers, rows along the lanes.
 // k_ffn_dw has them the other way round (rows along the registers), which is what a contraction over rows takes: dG, dU and H are its operands as
-// they are.  x and dy have to be turned round for it: a product with the identity does that on the matrix cores, exactly.  Each wave sums
+// they are.  x and dy have to be turned round for it: a product with the identity does that on the matrix cores, exactly.  Each block sums
 // its slice of 32 hidden units over a part of the rows; the parts are added by k_ffn_sum in a fixed order (fp32, no atomics).
 #include "ffn.h"
 
@@ -12,25 +12,122 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <typename T, int CT>
-__global__ void __launch_bounds__(kThreads) k_ffn_dx(const emc2_ffn_args a) {
+// Four neighbouring values of dx's row, from channel `at` on.
+template <typename T, bool WIDE> __device__ __forceinline__ void put_dx(const emc2_ffn_args& a, int64_t row, int at, emc2_fvec<4> v) {
+  T* out = (T*)a.y + row * a.ld_y + at;
+  if constexpr (WIDE) {
+    if (at < a.channels) emc2_store<4>(out, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (at + i < a.channels) out[i] = (T)v[i];
+  }
+}
+
+// Many rows: every wave has 32 rows of its own and walks all slices, whose weights pass through LDS for the whole block; the next
+// slice's are on their way meanwhile.  us, the form below (whose waves split the slices) / this one: 100 k x 64 x 256 bf16 78 / 35.
+constexpr int64_t kFewRows = 16384;
+template <typename T, int CT> constexpr bool kDxMany = sizeof(T) * CT <= 8;               // two waves a SIMD have the registers
+template <typename T, int CT> constexpr int kDxManyWaves = sizeof(T) * CT <= 4 ? 4 : 8;   // (and the fragments under way are fewer a wave)
+template <typename T, int CT, bool GELU, bool WIDE>
+__global__ void __launch_bounds__((64 * kDxManyWaves<T, CT>), 2) k_ffn_dx_many(const emc2_ffn_args a) {
   typedef emc2_tile<T> M;
   typedef typename M::frag frag;
-  constexpr int KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep;
+  constexpr int W = kDxManyWaves<T, CT>, KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep, kStaged = (3 * KK + W - 1) / W;
+  constexpr bool kExact = sizeof(T) == 4;
+  __shared__ frag ring[2][5 * KK * 64];
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int64_t row = ((int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * 32 + (lane & 31);
-  if (row - (lane & 31) >= n) return;
-  emc2_row<T, CT> x, dy;
-  x.set(a.x, a.ld_x, row, n, a.wide, a.channels, half);
-  dy.set(a.dy, a.ld_dy, row, n, a.wide, a.channels, half);
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((int64_t)blockIdx.x * W * 32 >= n) return;
+  const int64_t row = ((int64_t)blockIdx.x * W + wave) * 32 + (lane & 31);
+  emc2_row<T, CT, WIDE> x, dy;
+  x.set(a.x, a.ld_x, row, n, a.channels, half);
+  dy.set(a.dy, a.ld_dy, row, n, a.channels, half);
   emc2_acc dx[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) dx[c] = 0.0f;
-  const frag* w = (const frag*)a.packed + lane;
-  for (int32_t s = 0; s < a.slices; ++s, w += EMC2_FFN_GROUPS * KK * 64) {
+  const frag* packed = (const frag*)a.packed + EMC2_FFN_GATE * KK * 64 + lane;
+  frag staged[kStaged];
+  // fragments FROM .. TO - 1 of a slice (beyond the last one: the last one again)
+  const auto place = [&](int i, int from, int to) { return min(from + wave + i * W, to - 1); };
+  const auto fetch = [&](int32_t s, int from, int to) {
+#pragma unroll
+    for (int i = 0; i < (to - from + W - 1) / W; ++i)
+      staged[i] = packed[((int64_t)min(s, a.slices - 1) * EMC2_FFN_GROUPS * KK + place(i, from, to)) * 64];
+  };
+  const auto keep = [&](int buf, int from, int to) {
+#pragma unroll
+    for (int i = 0; i < (to - from + W - 1) / W; ++i) ring[buf][place(i, from, to) * 64 + lane] = staged[i];
+  };
+  fetch(0, 0, 3 * KK);
+  keep(0, 0, 3 * KK);
+  fetch(0, 3 * KK, 5 * KK);
+  keep(0, 3 * KK, 5 * KK);
+  for (int32_t s = 0; s < a.slices; ++s) {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    fetch(s + 1, 0, 3 * KK);
+    __builtin_amdgcn_sched_barrier(0);
+    const frag* w = ring[s & 1] + lane;
     emc2_acc g = 0.0f, u = 0.0f, dh = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      g = emc2_mma<T>(w[k * 64], x[k], g);
+      u = emc2_mma<T>(w[(KK + k) * 64], x[k], u);
+      dh = emc2_mma<T>(w[(2 * KK + k) * 64], dy[k], dh);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    keep((s + 1) & 1, 0, 3 * KK);
+    fetch(s + 1, 3 * KK, 5 * KK);
+    frag dg[MM], du[MM];
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      float slope[2];
+      const float act[2] = {emc2_activate<kExact, GELU>(g[r], slope[0]), emc2_activate<kExact, GELU>(g[r + 1], slope[1])};
+      emc2_put_pair<T>(dg, r, dh[r] * u[r] * slope[0], dh[r + 1] * u[r + 1] * slope[1]);
+      emc2_put_pair<T>(du, r, dh[r] * act[0], dh[r + 1] * act[1]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      dx[k / MM] = emc2_mma<T>(w[(3 * KK + k) * 64], dg[k % MM], dx[k / MM]);
+      dx[k / MM] = emc2_mma<T>(w[(4 * KK + k) * 64], du[k % MM], dx[k / MM]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    keep((s + 1) & 1, 3 * KK, 5 * KK);
+  }
+  if (row >= n) return;
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      put_dx<T, WIDE>(a, row, 32 * c + 8 * j + 4 * half, emc2_fvec<4>{dx[c][4 * j], dx[c][4 * j + 1], dx[c][4 * j + 2], dx[c][4 * j + 3]});
+}
+
+// A block has 32 rows; its waves (eight, or four where x, dy and dx's sums take over half of a SIMD's registers) share the slices out, each
+// reading its own weights from memory at once, and their sums meet in LDS.
+template <typename T, int CT> constexpr int kDxWaves = sizeof(T) == 2 ? (CT > 4 ? 4 : 8) : CT == 4 ? 4 : 8;
+template <typename T, int CT, bool GELU, bool WIDE>
+__global__ void __launch_bounds__((64 * kDxWaves<T, CT>)) k_ffn_dx(const emc2_ffn_args a) {
+  typedef emc2_tile<T> M;
+  typedef typename M::frag frag;
+  constexpr int KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep;
+  constexpr bool kExact = sizeof(T) == 4;
+  constexpr int kWaves = kDxWaves<T, CT>;
+  __shared__ emc2_fvec<4> part[kWaves][4][64];
+  const int32_t n = emc2_row_count(a.d_n, a.capacity);
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((int64_t)blockIdx.x * 32 >= n) return;
+  const int64_t row = (int64_t)blockIdx.x * 32 + (lane & 31);
+  emc2_row<T, CT, WIDE> x, dy;
+  x.set(a.x, a.ld_x, row, n, a.channels, half);
+  dy.set(a.dy, a.ld_dy, row, n, a.channels, half);
+  emc2_acc dx[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) dx[c] = 0.0f;
+  for (int32_t s = wave; s < a.slices; s += kWaves) {
+    const frag* w = (const frag*)a.packed + (int64_t)s * EMC2_FFN_GROUPS * KK * 64 + lane;
     x.again(), dy.again();
+    emc2_acc g = 0.0f, u = 0.0f, dh = 0.0f;
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
       g = emc2_mma<T>(w[(EMC2_FFN_GATE * KK + k) * 64], x[k], g);
@@ -39,67 +136,71 @@ __global__ void __launch_bounds__(kThreads) k_ffn_dx(const emc2_ffn_args a) {
     }
     frag dg[MM], du[MM];
 #pragma unroll
-    for (int m = 0; m < MM; ++m)
-#pragma unroll
-      for (int e = 0; e < M::kPer; ++e) {
-        const int r = m * M::kPer + e;
-        float slope;
-        const float act = emc2_activate<sizeof(T) == 4>(a.gelu, g[r], slope);
-        dg[m][e] = (T)(dh[r] * u[r] * slope);
-        du[m][e] = (T)(dh[r] * act);
-      }
-#pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-      for (int m = 0; m < MM; ++m) {
-        dx[c] = emc2_mma<T>(w[(EMC2_FFN_GATE_T * KK + c * MM + m) * 64], dg[m], dx[c]);
-        dx[c] = emc2_mma<T>(w[(EMC2_FFN_UP_T * KK + c * MM + m) * 64], du[m], dx[c]);
-      }
-  }
-  if (row >= n) return;
-#pragma unroll
-  for (int c = 0; c < CT; ++c)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int at = 32 * c + 8 * j + 4 * half;
-      const emc2_fvec<4> v = {dx[c][4 * j], dx[c][4 * j + 1], dx[c][4 * j + 2], dx[c][4 * j + 3]};
-      T* out = (T*)a.y + row * a.ld_y + at;
-      if (a.wide) {
-        if (at < a.channels) emc2_store<4>(out, v);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (at + i < a.channels) out[i] = (T)v[i];
-      }
+    for (int r = 0; r < 16; r += 2) {
+      float slope[2];
+      const float act[2] = {emc2_activate<kExact, GELU>(g[r], slope[0]), emc2_activate<kExact, GELU>(g[r + 1], slope[1])};
+      emc2_put_pair<T>(dg, r, dh[r] * u[r] * slope[0], dh[r + 1] * u[r + 1] * slope[1]);
+      emc2_put_pair<T>(du, r, dh[r] * act[0], dh[r + 1] * act[1]);
     }
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      dx[k / MM] = emc2_mma<T>(w[(EMC2_FFN_GATE_T * KK + k) * 64], dg[k % MM], dx[k / MM]);
+      dx[k / MM] = emc2_mma<T>(w[(EMC2_FFN_UP_T * KK + k) * 64], du[k % MM], dx[k / MM]);
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    if (c) __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part[wave][j][lane] = emc2_fvec<4>{dx[c][4 * j], dx[c][4 * j + 1], dx[c][4 * j + 2], dx[c][4 * j + 3]};
+    __syncthreads();
+    const int at = 32 * c + 8 * wave + 4 * half;
+    if (wave < 4 && row < n) {
+      emc2_fvec<4> v = part[0][wave][lane];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) v += part[w][wave][lane];
+      put_dx<T, WIDE>(a, row, at, v);
+    }
+  }
 }
 
 // Fragments of a tile's 32 columns of x or dy, rows along the lanes' registers: the rows' fragments times the identity.
-template <typename T, int CT, int MM>
-__device__ __forceinline__ void turned(const emc2_row<T, CT>& rows, int first, const typename emc2_tile<T>::frag (&one)[MM],
+template <typename T, int CT, bool WIDE, int MM>
+__device__ __forceinline__ void turned(const emc2_row<T, CT, WIDE>& rows, int first, const typename emc2_tile<T>::frag (&one)[MM],
                                        typename emc2_tile<T>::frag (&out)[MM]) {
   emc2_acc t = 0.0f;
 #pragma unroll
   for (int m = 0; m < MM; ++m) t = emc2_mma<T>(rows[first + m], one[m], t);
 #pragma unroll
-  for (int m = 0; m < MM; ++m)
-#pragma unroll
-    for (int e = 0; e < emc2_tile<T>::kPer; ++e) out[m][e] = (T)t[m * emc2_tile<T>::kPer + e];
+  for (int r = 0; r < 16; r += 2) emc2_put_pair<T>(out, r, t[r], t[r + 1]);
 }
 
 // Partial sums [part][slice][3][C / 32][64 lanes][16]: of a tile of dWg, dWu (rows: channels, columns: hidden units) and of dWd (rows: hidden
-// units, columns: channels).  C0: the first of the CB tiles of channels whose sums the launch takes.
-template <typename T, int CT, int C0, int CB>
-__global__ void __launch_bounds__(kThreads, 1) k_ffn_dw(const emc2_ffn_args a) {
+// units, columns: channels), the CB tiles of channels from C0 on.  A block has one slice, whose weights lie in LDS, and one part of the rows, which
+// its four waves share out; the next tile of rows is on its way while one is worked on.
+// Waves a SIMD: two without the next tile's rows where the sums are few.
+#ifndef DW2
+#define DW2 2
+#define DCB (CT > 4 ? CT / 2 : CT)
+#endif
+template <typename T, int CT> constexpr int kDwWaves = sizeof(T) == 2 && CT <= DW2 ? 2 : 1;
+template <typename T, int CT, bool GELU, bool WIDE, int C0, int CB>
+__global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const emc2_ffn_args a) {
   typedef emc2_tile<T> M;
   typedef typename M::frag frag;
-  constexpr int KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep;
+  constexpr int KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep, kWaves = kThreads / 64;
+  constexpr int kWavesASimd = kDwWaves<T, CT>;
+  constexpr bool kExact = sizeof(T) == 4, kAhead = false;
+  __shared__ frag w[3 * KK * 64];
+  __shared__ emc2_fvec<4> meet[kWaves][4][64];
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int64_t wave = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int32_t s = (int32_t)(wave % a.slices), part = (int32_t)(wave / a.slices);
-  if (part >= a.parts) return;
-  const frag* w = (const frag*)a.packed + (int64_t)s * EMC2_FFN_GROUPS * KK * 64 + lane;
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t s = blockIdx.x % a.slices, part = blockIdx.x / a.slices;
+  {
+    const frag* from = (const frag*)a.packed + ((int64_t)s * EMC2_FFN_GROUPS + EMC2_FFN_GATE) * KK * 64;
+    for (int i = threadIdx.x; i < 3 * KK * 64; i += kThreads) w[i] = from[i];
+  }
+  __syncthreads();
   frag one[MM];
 #pragma unroll
   for (int m = 0; m < MM; ++m)
@@ -108,45 +209,82 @@ __global__ void __launch_bounds__(kThreads, 1) k_ffn_dw(const emc2_ffn_args a) {
   emc2_acc dwg[CB], dwu[CB], dwd[CB];
 #pragma unroll
   for (int c = 0; c < CB; ++c) dwg[c] = 0.0f, dwu[c] = 0.0f, dwd[c] = 0.0f;
-  for (int64_t tile = part; tile * 32 < n; tile += a.parts) {
+  const int32_t step = a.parts * kWaves;
+  const auto read = [&](int64_t tile, emc2_row<T, CT, WIDE>& x, emc2_row<T, CT, WIDE>& dy) {
     const int64_t row = tile * 32 + (lane & 31);
-    if constexpr (sizeof(T) * CT > 8) asm volatile("" : "+v"(w));   // too many weights to keep in registers: loaded again for every tile
-    emc2_row<T, CT> x, dy;
-    x.set(a.x, a.ld_x, row, n, a.wide, a.channels, half);
-    dy.set(a.dy, a.ld_dy, row, n, a.wide, a.channels, half);
+    x.set(a.x, a.ld_x, row, n, a.channels, half);
+    dy.set(a.dy, a.ld_dy, row, n, a.channels, half);
+  };
+  const auto work = [&](const emc2_row<T, CT, WIDE>& x, const emc2_row<T, CT, WIDE>& dy) {
+    int at = lane;
+    asm volatile("" : "+v"(at));                           // the weights are read from LDS each time: registers have no room for them
     emc2_acc g = 0.0f, u = 0.0f, dh = 0.0f;
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
-      g = emc2_mma<T>(x[k], w[(EMC2_FFN_GATE * KK + k) * 64], g);
-      u = emc2_mma<T>(x[k], w[(EMC2_FFN_UP * KK + k) * 64], u);
-      dh = emc2_mma<T>(dy[k], w[(EMC2_FFN_DOWN_T * KK + k) * 64], dh);
+      g = emc2_mma<T>(x[k], w[k * 64 + at], g);
+      u = emc2_mma<T>(x[k], w[(KK + k) * 64 + at], u);
+      dh = emc2_mma<T>(dy[k], w[(2 * KK + k) * 64 + at], dh);
     }
     frag h[MM], dg[MM], du[MM];
 #pragma unroll
-    for (int m = 0; m < MM; ++m)
+    for (int r = 0; r < 16; r += 2) {
+      float slope[2];
+      const float act[2] = {emc2_activate<kExact, GELU>(g[r], slope[0]), emc2_activate<kExact, GELU>(g[r + 1], slope[1])};
+      emc2_put_pair<T>(h, r, act[0] * u[r], act[1] * u[r + 1]);
+      emc2_put_pair<T>(dg, r, dh[r] * u[r] * slope[0], dh[r + 1] * u[r + 1] * slope[1]);
+      emc2_put_pair<T>(du, r, dh[r] * act[0], dh[r + 1] * act[1]);
+    }
+    // tile 2 c of x and 2 c + 1 of dy, each turned one step ahead of its products
+    frag t[2][MM];
+    turned<T, CT, WIDE, MM>(x, C0 * MM, one, t[0]);
 #pragma unroll
-      for (int e = 0; e < M::kPer; ++e) {
-        const int r = m * M::kPer + e;
-        float slope;
-        const float act = emc2_activate<sizeof(T) == 4>(a.gelu, g[r], slope);
-        h[m][e] = (T)(act * u[r]);
-        dg[m][e] = (T)(dh[r] * u[r] * slope);
-        du[m][e] = (T)(dh[r] * act);
+    for (int i = 0; i < 2 * CB; ++i) {
+      const int c = i / 2;
+      if (i + 1 < 2 * CB) {
+        if (i % 2) turned<T, CT, WIDE, MM>(x, (C0 + c + 1) * MM, one, t[(i + 1) % 2]);
+        else turned<T, CT, WIDE, MM>(dy, (C0 + c) * MM, one, t[(i + 1) % 2]);
       }
 #pragma unroll
-    for (int c = 0; c < CB; ++c) {
-      frag t[MM];
-      turned<T, CT, MM>(x, (C0 + c) * MM, one, t);
-#pragma unroll
-      for (int m = 0; m < MM; ++m) dwg[c] = emc2_mma<T>(t[m], dg[m], dwg[c]), dwu[c] = emc2_mma<T>(t[m], du[m], dwu[c]);
-      turned<T, CT, MM>(dy, (C0 + c) * MM, one, t);
-#pragma unroll
-      for (int m = 0; m < MM; ++m) dwd[c] = emc2_mma<T>(h[m], t[m], dwd[c]);
+      for (int m = 0; m < MM; ++m) {
+        if (i % 2) dwd[c] = emc2_mma<T>(h[m], t[1][m], dwd[c]);
+        else dwg[c] = emc2_mma<T>(t[0][m], dg[m], dwg[c]), dwu[c] = emc2_mma<T>(t[0][m], du[m], dwu[c]);
+      }
+      if constexpr (kWavesASimd == 1) __builtin_amdgcn_sched_barrier(0);   // no further ahead: registers
+    }
+  };
+  int64_t tile = (int64_t)part * kWaves + wave;
+  if constexpr (kAhead) {
+    emc2_row<T, CT, WIDE> x[2], dy[2];
+    if (tile * 32 < n) read(tile, x[0], dy[0]);
+    while (tile * 32 < n) {
+      read(tile + step, x[1], dy[1]);                      // (nothing is read beyond the rows)
+      work(x[0], dy[0]);
+      tile += step;
+      if (tile * 32 >= n) break;
+      read(tile + step, x[0], dy[0]);
+      work(x[1], dy[1]);
+      tile += step;
+    }
+  } else {
+    for (; tile * 32 < n; tile += step) {
+      emc2_row<T, CT, WIDE> x, dy;
+      read(tile, x, dy);
+      work(x, dy);
     }
   }
-  emc2_acc* out = (emc2_acc*)a.partial + (((int64_t)part * a.slices + s) * 3 * CT + C0) * 64 + lane;
+  emc2_fvec<4>* out = (emc2_fvec<4>*)a.partial + ((int64_t)part * a.slices + s) * 3 * CT * 256;
 #pragma unroll
-  for (int c = 0; c < CB; ++c) out[c * 64] = dwg[c], out[(CT + c) * 64] = dwu[c], out[(2 * CT + c) * 64] = dwd[c];
+  for (int which = 0; which < 3; ++which)
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+      const emc2_acc& t = which == 0 ? dwg[c] : which == 1 ? dwu[c] : dwd[c];
+      if (which + c) __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) meet[wave][j][lane] = emc2_fvec<4>{t[4 * j], t[4 * j + 1], t[4 * j + 2], t[4 * j + 3]};
+      __syncthreads();
+      // registers 4 wave .. 4 wave + 3 of every lane
+      out[((which * CT + C0 + c) * 64 + lane) * 4 + wave] = meet[0][wave][lane] + meet[1][wave][lane] + meet[2][wave][lane] + meet[3][wave][lane];
+    }
 }
 
 // Adds the parts, four values a thread, and puts them where they belong.
@@ -178,10 +316,10 @@ __global__ void __launch_bounds__(kThreads) k_ffn_sum(const float4* __restrict__
   }
 }
 
-// Parts that the rows are cut into: enough that every SIMD has a wave, none without rows.
+// Parts that the rows are cut into: about 512 blocks, two for every CU, and none of them without a tile of rows for each wave.
 int32_t parts_of(int64_t capacity, int32_t hidden) {
-  const int64_t slices = (hidden + 31) / 32, aim = emc2_div_up(1024, slices), tiles = emc2_div_up(capacity, 32);
-  const int64_t parts = aim < tiles ? aim : tiles;
+  const int64_t slices = (hidden + 31) / 32, aim = emc2_div_up(512, slices), most = emc2_div_up(capacity, 32 * (kThreads / 64));
+  const int64_t parts = aim < most ? aim : most;
   return (int32_t)(parts < 1 ? 1 : parts);
 }
 
@@ -212,19 +350,26 @@ extern "C" emc2_status emc2_ffn_backward(emc2_ctx* ctx, emc2_dtype dtype, int32_
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_ffn_backward: work buffer null, not 16-byte aligned or smaller than emc2_ffn_work");
   emc2_ffn_args a = {};
   a.x = d_x, a.dy = d_dy, a.packed = d_packed, a.y = d_dx, a.partial = (float*)d_work, a.d_n = d_n, a.ld_x = ld_x, a.ld_dy = ld_dy, a.ld_y = ld_dx;
-  a.capacity = capacity, a.channels = channels, a.hidden = hidden, a.slices = (hidden + 31) / 32, a.gelu = activation == EMC2_ACT_GELU;
+  a.capacity = capacity, a.channels = channels, a.hidden = hidden, a.slices = (hidden + 31) / 32;
   a.parts = parts_of(capacity, hidden);
-  a.wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_dy, ld_dy, size) && emc2_wide_rows(d_dx, ld_dx, size);
+  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_dy, ld_dy, size) && emc2_wide_rows(d_dx, ld_dx, size);
   hipStream_t s = (hipStream_t)stream;
   const int tiles = emc2_ffn_tiles(channels);
-  const dim3 dw_grid((unsigned)emc2_div_up((int64_t)a.parts * a.slices, kThreads / 64));
-  emc2_ffn_dispatch(dtype, tiles, [&](auto type, auto count) {
+  const dim3 dw_grid((unsigned)((int64_t)a.parts * a.slices));
+  emc2_ffn_dispatch(dtype, tiles, activation == EMC2_ACT_GELU, wide, [&](auto type, auto count, auto gelu, auto pieces) {
     using T = decltype(type);
-    constexpr int CT = decltype(count)::value, CB = CT > 4 ? CT / 2 : CT;
+    constexpr bool G = decltype(gelu)::value, P = decltype(pieces)::value;
+    constexpr int CT = decltype(count)::value, CB = DCB;
     // the weights' launches first: dx may lie where dy did
-    hipLaunchKernelGGL((k_ffn_dw<T, CT, 0, CB>), dw_grid, dim3(kThreads), 0, s, a);
-    if constexpr (CB < CT) hipLaunchKernelGGL((k_ffn_dw<T, CT, CB, CB>), dw_grid, dim3(kThreads), 0, s, a);
-    if (!none) hipLaunchKernelGGL((k_ffn_dx<T, CT>), dim3((unsigned)emc2_div_up(capacity, 128)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((k_ffn_dw<T, CT, G, P, 0, CB>), dw_grid, dim3(kThreads), 0, s, a);
+    if constexpr (CB < CT) hipLaunchKernelGGL((k_ffn_dw<T, CT, G, P, CB, CT - CB>), dw_grid, dim3(kThreads), 0, s, a);
+    if constexpr (kDxMany<T, CT>) {
+      constexpr int W = kDxManyWaves<T, CT>;
+      if (capacity > kFewRows)
+        hipLaunchKernelGGL((k_ffn_dx_many<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32 * W)), dim3(64 * W), 0, s, a);
+    }
+    if (!none && !(kDxMany<T, CT> && capacity > kFewRows))
+      hipLaunchKernelGGL((k_ffn_dx<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32)), dim3(64 * kDxWaves<T, CT>), 0, s, a);
     hipLaunchKernelGGL(k_ffn_sum<T>, dim3((unsigned)emc2_div_up((int64_t)a.slices * 3 * CT * 256, kThreads)), dim3(kThreads), 0, s,
                        (const float4*)d_work, a.parts, a.slices, CT, channels, hidden, (T*)d_dwg, (T*)d_dwu, (T*)d_dwd);
   });
