@@ -8,17 +8,22 @@
 // first row begins a new map (A = 0, B = the given state), so sequences of any length share a block and none is padded.
 // The gradients' u runs the other way with the same factors: the first launch reduces both directions at once, the second walks a block's
 // tiles from the last to the first, with the state that enters every tile known from the first launch.
-// Inside a block a thread holds R consecutive rows of N neighbouring channels in registers; maps are composed over a wave's
+// A thread holds R consecutive rows of N neighbouring channels in registers; maps are composed over a wave's
 // row groups by shuffles, over waves through LDS.  The order of composition is fixed: equal inputs give equal bits.  Maps and states are fp32.
 // A map with A = 0 drops what lies before it, whatever that holds: an infinity or NaN in one sequence never reaches another one.
-// Bound by memory, and close behind by the logistic function's two quarter-rate instructions an element.
+// Bound by memory, and close behind by the logistic function's two slow instructions an element.
 #include "rows.h"
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kMaxTiles = 32;        // tiles of a block
-constexpr int kRowsForward = 8, kRowsGrad = 4;
+constexpr int kMaxTiles = 32;        // tiles of a wave's run (forward) or of a block (gradients)
+constexpr int kSlice = 64;           // channels of a block at most
+// Waves of a block, rows of a thread and blocks aimed at, as measured (us, 613 k x 64 f16 forward; 200 k x 128 bf16 gradients): the second launch's
+// blocks compose the maps of all others, which costs 1024 of them 20 us; blocks of eight waves need half as many.
+//   forward, 8 waves, 4 rows: 512 blocks 102, 256 blocks 108; 8 rows, 256 blocks 102 (fp32 over 96 channels 82, 93, 91); 4 waves, 8 rows: 1024, 512,
+//   256 blocks 125, 111, 124.  gradients with the forward pass, 4 waves, 4 rows: 1024, 512, 256 blocks 220, 187, 241; 8 rows 274; 8 waves: 512, 256 blocks 211, 195
+constexpr int kStepThreads = 256;    // of the kernels of one value or piece a thread
+constexpr int kWavesForward = 8, kWavesGrad = 4, kRowsForward = 4, kRowsGrad = 4, kBlocks = 512;
 
 struct Args {
   const void *x, *gate, *dy;
@@ -46,6 +51,11 @@ __device__ __forceinline__ int32_t start_of(const Args& a, int32_t n, int32_t j)
 }
 __device__ __forceinline__ int32_t seq_of(const Args& a, int32_t j) { return a.backwards ? a.n_seq - 1 - j : j; }
 
+// More rows than the buffers hold are left out and reported.
+__device__ __forceinline__ void report(const Args& a) {
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0 && a.offsets[a.n_seq] > a.capacity) atomicOr(a.flags, EMC2_DEVFLAG_CAPACITY);
+}
+
 // The first j >= `j` whose sequence starts at `row` or later (n_seq if there is none), by the whole wave.
 __device__ __forceinline__ int32_t seek(const Args& a, int32_t n, int32_t j, int32_t row, int lane) {
   while (true) {
@@ -66,6 +76,17 @@ __device__ __forceinline__ int32_t seek_far(const Args& a, int32_t n, int32_t ro
   }
   return seek(a, n, lo, row, lane);
 }
+
+// The first sequence from a tile's first row on, for tiles in falling order.
+struct Falling {
+  int32_t j = 0, next = -1, before = 0x7fffffff;           // its number and start; the start of the one before it
+  __device__ __forceinline__ void move(const Args& a, int32_t n, int32_t row0, int lane) {
+    if (before < row0) return;
+    j = row0 > 0 ? seek_far(a, n, row0, lane) : 0;
+    next = start_of(a, n, j);
+    before = j > 0 ? start_of(a, n, j - 1) : -1;
+  }
+};
 
 // Where sequences start and end within a wave's rows of a tile: per row the caller's number of the sequence that starts or ends there,
 // or -1.  Returns false, and writes nothing, where none does (next: the first start at or after the rows' first, also the end of
@@ -153,12 +174,12 @@ template <int N> __device__ __forceinline__ Place place_of(const Args& a) {
 // R consecutive rows of a thread as they lie in memory; rows past the last and channels that are none read valid places.
 template <typename T, int N, int R> struct Rows { emc2_vec<T, N> v[R]; };
 template <typename T, int N, int R>
-__device__ __forceinline__ Rows<T, N, R> fetch(const Args& a, const void* p, int64_t ld, int32_t n, int32_t row, const Place& t) {
+__device__ __forceinline__ Rows<T, N, R> fetch(const Args& a, const void* p, int64_t ld, int32_t n, int64_t row, const Place& t) {
   Rows<T, N, R> r;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    const int32_t k = row + i < n ? row + i : n - 1;
-    r.v[i] = *reinterpret_cast<const emc2_vec<T, N>*>((const T*)p + (int64_t)(a.backwards ? n - 1 - k : k) * ld + (t.in ? t.channel : 0));
+    const int64_t k = row + i < n ? row + i : n - 1;
+    r.v[i] = *reinterpret_cast<const emc2_vec<T, N>*>((const T*)p + (a.backwards ? n - 1 - k : k) * ld + (t.in ? t.channel : 0));
   }
   return r;
 }
@@ -219,20 +240,83 @@ template <int N, int R> __device__ __forceinline__ void blank(int32_t n, int32_t
     if (row + i >= n) keep[i] = 1.0f, add[i] = 0.0f;
 }
 
-// First launch: the maps of every block, and with GRAD of every tile.  Block (b, slice) has `tiles` tiles of rows, a tile a thread's R rows in
-// every row group of the block.
-template <typename T, int N, int R, bool GRAD>
-__global__ void __launch_bounds__(kThreads) k_recurrence_totals(const Args a) {
-  constexpr int kSlice = 64;
-  __shared__ float2 total[2][GRAD ? 2 : 1][kWaves][kSlice];
+// First launch of the forward pass: the maps of every wave's run of rows and of every block.  A wave walks `tiles` tiles, a tile being R rows in every
+// row group of the wave, from the last to the first: the second launch, whose blocks lie on the same XCDs, begins with what was read
+// last.  The next tile's rows are on their way while one is worked on.
+template <typename T, int N, int R>
+__global__ void __launch_bounds__(64 * kWavesForward) k_recurrence_totals(const Args a) {
+  constexpr int kWaves = kWavesForward;
+  __shared__ float2 total[kWaves][kSlice];
+  __shared__ int32_t starts[kWaves][64 * R], ends[kWaves][64 * R];
+  const Place t = place_of<N>(a);
+  const int32_t n = rows_of(a), rows = t.groups * R;
+  report(a);
+  const int64_t first = ((int64_t)blockIdx.x * kWaves + t.wave) * a.tiles * rows;
+  if ((int64_t)blockIdx.x * kWaves * a.tiles * rows >= n) return;
+  const int slice = N << a.lane_shift;
+  Map<N> run = nothing<N>();
+  if (first < n) {
+    const int32_t here = (int32_t)((n - first + rows - 1) / rows), tiles = here < a.tiles ? here : a.tiles;
+    const int64_t mine = first + (int64_t)(tiles - 1) * rows + t.group * R;
+    Rows<T, N, R> x = fetch<T, N, R>(a, a.x, a.ld_x, n, mine, t), g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, mine, t);
+    Falling at;
+    for (int32_t k = tiles - 1; k >= 0; --k) {
+      const int64_t row0 = first + (int64_t)k * rows;
+      const int32_t row = (int32_t)row0 + t.group * R;
+      emc2_fvec<N> keep[R], add[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        emc2_fvec<N> take;
+        open<T, N>(g.v[i], keep[i], take);
+        add[i] = take * __builtin_convertvector(x.v[i], emc2_fvec<N>);
+      }
+      if (k > 0) {
+        x = fetch<T, N, R>(a, a.x, a.ld_x, n, (int64_t)row - rows, t);
+        g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, (int64_t)row - rows, t);
+      }
+      at.move(a, n, (int32_t)row0, t.lane);
+      const bool marked = mark(a, n, (int32_t)row0, rows, at.j, at.next, starts[t.wave], ends[t.wave], t.lane);
+      if (row0 + rows > n) blank<N, R>(n, row, keep, add);
+      Map<N> m = run_forward<N, R>(a, keep, add, marked, &starts[t.wave][t.group * R], t);
+      for (int dist = 1 << a.lane_shift; dist < 64; dist <<= 1) m = then<N>(m, from_above<N>(m, dist));
+      run = then<N>(m, run);                               // (of the first row group; the others' are not used)
+    }
+  }
+  if (t.group == 0) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) total[t.wave][t.column + e] = make_float2(run.A[e], run.B[e]);
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < slice) {
+    const int64_t place = (int64_t)blockIdx.y * slice + threadIdx.x;
+    float2 block = make_float2(1.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float2 m = total[w][threadIdx.x];
+      a.tile_f[((int64_t)blockIdx.x * kWaves + w) * a.width + place] = m;
+      block = then(block, m);
+    }
+    a.block_f[(int64_t)blockIdx.x * a.width + place] = block;
+  }
+}
+
+// First launch of the gradients: the maps of every block in both directions, and the forward one of every tile.  Block (b, slice) has `tiles` tiles
+// of rows, a tile being R rows in every row group of the block.
+template <typename T, int N, int R>
+__global__ void __launch_bounds__(64 * kWavesGrad) k_recurrence_grad_totals(const Args a) {
+  constexpr int kWaves = kWavesGrad;
+  __shared__ float2 total[2][2][kWaves][kSlice];
   __shared__ int32_t starts[kWaves][64 * R], ends[kWaves][64 * R];
   const Place t = place_of<N>(a);
   const int32_t n = rows_of(a);
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0 && a.offsets[a.n_seq] > a.capacity) atomicOr(a.flags, EMC2_DEVFLAG_CAPACITY);
+  report(a);
   const int32_t tile_rows = kWaves * t.groups * R;
   const int64_t first = (int64_t)blockIdx.x * a.tiles * tile_rows;
   if (first >= n) return;
   const int slice = N << a.lane_shift;
+  const int64_t mine = first + (t.wave * t.groups + t.group) * R;
+  Rows<T, N, R> x = fetch<T, N, R>(a, a.x, a.ld_x, n, mine, t), g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, mine, t),
+                d = fetch<T, N, R>(a, a.dy, a.ld_dy, n, mine, t);
   int32_t j = 0, next = -1;
   if (first > 0) j = seek_far(a, n, (int32_t)first, t.lane);
   float2 block_f = make_float2(1.0f, 0.0f), block_r = block_f;
@@ -241,36 +325,34 @@ __global__ void __launch_bounds__(kThreads) k_recurrence_totals(const Args a) {
     if (first + (int64_t)k * tile_rows >= n) break;
     const int32_t row = (int32_t)row0 + t.group * R;
     Map<N> f = nothing<N>(), r = nothing<N>();
+    emc2_fvec<N> keep[R], add[R], dy[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      emc2_fvec<N> take;
+      open<T, N>(g.v[i], keep[i], take);
+      add[i] = take * __builtin_convertvector(x.v[i], emc2_fvec<N>);
+      dy[i] = __builtin_convertvector(d.v[i], emc2_fvec<N>);
+    }
+    if (k + 1 < a.tiles && first + (int64_t)(k + 1) * tile_rows < n) {
+      x = fetch<T, N, R>(a, a.x, a.ld_x, n, (int64_t)row + tile_rows, t);
+      g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, (int64_t)row + tile_rows, t);
+      d = fetch<T, N, R>(a, a.dy, a.ld_dy, n, (int64_t)row + tile_rows, t);
+    }
     if (row0 < n) {
-      const Rows<T, N, R> x = fetch<T, N, R>(a, a.x, a.ld_x, n, row, t), g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, row, t);
-      Rows<T, N, R> d;
-      if constexpr (GRAD) d = fetch<T, N, R>(a, a.dy, a.ld_dy, n, row, t);
       const bool marked = mark(a, n, (int32_t)row0, t.groups * R, j, next, starts[t.wave], ends[t.wave], t.lane);
-      emc2_fvec<N> keep[R], add[R];
-#pragma unroll
-      for (int i = 0; i < R; ++i) {
-        emc2_fvec<N> take;
-        open<T, N>(g.v[i], keep[i], take);
-        add[i] = take * __builtin_convertvector(x.v[i], emc2_fvec<N>);
-      }
-      if (row0 + t.groups * R > n) blank<N, R>(n, row, keep, add);
+      if (row0 + t.groups * R > n) blank<N, R>(n, row, keep, add), blank<N, R>(n, row, keep, dy);
       f = run_forward<N, R>(a, keep, add, marked, &starts[t.wave][t.group * R], t);
-      if constexpr (GRAD) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) add[i] = __builtin_convertvector(d.v[i], emc2_fvec<N>);
-        if (row0 + t.groups * R > n) blank<N, R>(n, row, keep, add);
-        r = run_backward<N, R>(a, keep, add, marked, &ends[t.wave][t.group * R], t);
-      }
+      r = run_backward<N, R>(a, keep, dy, marked, &ends[t.wave][t.group * R], t);
       for (int dist = 1 << a.lane_shift; dist < 64; dist <<= 1) {     // the wave's first row group ends with all of them
         f = then<N>(f, from_above<N>(f, dist));
-        if constexpr (GRAD) r = then<N>(from_above<N>(r, dist), r);
+        r = then<N>(from_above<N>(r, dist), r);
       }
     }
     if (t.group == 0) {
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         total[k & 1][0][t.wave][t.column + e] = make_float2(f.A[e], f.B[e]);
-        if constexpr (GRAD) total[k & 1][GRAD ? 1 : 0][t.wave][t.column + e] = make_float2(r.A[e], r.B[e]);
+        total[k & 1][1][t.wave][t.column + e] = make_float2(r.A[e], r.B[e]);
       }
     }
     __syncthreads();
@@ -278,35 +360,29 @@ __global__ void __launch_bounds__(kThreads) k_recurrence_totals(const Args a) {
       const int c = threadIdx.x;
       float2 tile = total[k & 1][0][0][c];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) {
-        tile = then(tile, total[k & 1][0][w][c]);
-      }
+      for (int w = 1; w < kWaves; ++w) tile = then(tile, total[k & 1][0][w][c]);
       block_f = then(block_f, tile);
-      if constexpr (GRAD) {
-        a.tile_f[((int64_t)blockIdx.x * a.tiles + k) * a.width + blockIdx.y * slice + c] = tile;
+      a.tile_f[((int64_t)blockIdx.x * a.tiles + k) * a.width + blockIdx.y * slice + c] = tile;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {                 // of the flow towards earlier rows, the later rows come first
-          block_r = then(total[k & 1][GRAD ? 1 : 0][w][c], block_r);
-        }
-      }
+      for (int w = 0; w < kWaves; ++w) block_r = then(total[k & 1][1][w][c], block_r);   // of the flow towards earlier rows, the later rows come first
     }
   }
   if ((int)threadIdx.x < slice) {
     a.block_f[(int64_t)blockIdx.x * a.width + blockIdx.y * slice + threadIdx.x] = block_f;
-    if constexpr (GRAD) a.block_r[(int64_t)blockIdx.x * a.width + blockIdx.y * slice + threadIdx.x] = block_r;
+    a.block_r[(int64_t)blockIdx.x * a.width + blockIdx.y * slice + threadIdx.x] = block_r;
   }
 }
 
 // What a run of blocks makes of a state of zeros, per channel of the slice, into enter[]: blocks [lo, hi) in rising order, or (FALLING) from
 // hi - 1 down to lo.  The block's threads take a part of the run each.  Ends with a barrier.
-template <bool FALLING>
+template <bool FALLING, int WAVES>
 __device__ __forceinline__ void compose(const float2* __restrict__ maps, int32_t width, int32_t column, int slice, int32_t lo, int32_t hi,
                                         float2* part, float* enter) {
-  const int c = threadIdx.x & (slice - 1), seg = threadIdx.x / slice, segs = kThreads / slice;
+  const int c = threadIdx.x & (slice - 1), seg = threadIdx.x / slice, segs = 64 * WAVES / slice;
   const int32_t count = hi > lo ? hi - lo : 0, per = (count + segs - 1) / segs;
   const int32_t from = seg * per < count ? seg * per : count, to = from + per < count ? from + per : count;
   float2 all = make_float2(1.0f, 0.0f);
-  constexpr int kAtOnce = 8;
+  constexpr int kAtOnce = 16;
   for (int32_t i = from; i < to; i += kAtOnce) {
     float2 m[kAtOnce];
 #pragma unroll
@@ -333,116 +409,111 @@ __device__ __forceinline__ void pass_empty(const Args& a, int32_t n, const float
   if (!to) return;
   const int32_t per = (int32_t)(((int64_t)a.n_seq + gridDim.x - 1) / gridDim.x);
   const int64_t lo = (int64_t)blockIdx.x * per, hi = lo + per < a.n_seq ? lo + per : a.n_seq;
-  for (int64_t j = lo + threadIdx.x; j < hi; j += kThreads) {
+  for (int64_t j = lo + threadIdx.x; j < hi; j += blockDim.x) {
     if (start_of(a, n, (int32_t)j + 1) > start_of(a, n, (int32_t)j)) continue;
     const int64_t s = (int64_t)seq_of(a, (int32_t)j) * a.channels;
     for (int32_t c = blockIdx.y * slice; c < (int32_t)(blockIdx.y + 1) * slice && c < a.channels; ++c) to[s + c] = from ? from[s + c] : 0.0f;
   }
 }
 
+// Second launch: the rows.  A block of one wave (calls of a few tiles) needs no first launch.
 template <typename T, int N, int R>
-__global__ void __launch_bounds__(kThreads) k_recurrence(const Args a) {
-  constexpr int kSlice = 64;
-  __shared__ float2 total[2][kWaves][kSlice];
+__global__ void __launch_bounds__(64 * kWavesForward) k_recurrence(const Args a) {
+  constexpr int kWaves = kWavesForward;
   __shared__ int32_t starts[kWaves][64 * R], ends[kWaves][64 * R];
-  __shared__ float2 part[kThreads];
+  __shared__ float2 part[64 * kWaves];
   __shared__ float enter[kSlice];
   const Place t = place_of<N>(a);
-  const int32_t n = rows_of(a);
-  if (gridDim.x == 1 && blockIdx.y == 0 && threadIdx.x == 0 && a.offsets[a.n_seq] > a.capacity) atomicOr(a.flags, EMC2_DEVFLAG_CAPACITY);
+  const int32_t n = rows_of(a), rows = t.groups * R, waves = blockDim.x >> 6;
+  if (waves == 1) report(a);
   const int slice = N << a.lane_shift;
-  const int32_t tile_rows = kWaves * t.groups * R;
-  const int64_t first = (int64_t)blockIdx.x * a.tiles * tile_rows;
+  const int64_t first = ((int64_t)blockIdx.x * waves + t.wave) * a.tiles * rows;
   pass_empty(a, n, a.h0, a.last, slice);
-  if (first >= n) return;
+  if ((int64_t)blockIdx.x * waves * a.tiles * rows >= n) return;
+  const int64_t mine = first + t.group * R;
+  Rows<T, N, R> x = fetch<T, N, R>(a, a.x, a.ld_x, n, mine, t), g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, mine, t);
   emc2_fvec<N> h = emc2_fvec<N>(0.0f);                     // the state that enters the tile
   int32_t j = 0, next = -1;
-  if (blockIdx.x > 0) {
-    compose<false>(a.block_f, a.width, blockIdx.y * slice, slice, 0, blockIdx.x, part, enter);
+  if (first > 0 && first < n) j = seek_far(a, n, (int32_t)first, t.lane);
+  if (waves > 1) {
+    compose<false, kWaves>(a.block_f, a.width, blockIdx.y * slice, slice, 0, blockIdx.x, part, enter);
 #pragma unroll
-    for (int e = 0; e < N; ++e) h[e] = enter[t.column + e];
-    j = seek_far(a, n, (int32_t)first, t.lane);
+    for (int e = 0; e < N; ++e) {
+      h[e] = enter[t.column + e];
+      float2 m[kWaves - 1];
+#pragma unroll
+      for (int w = 0; w < kWaves - 1; ++w) m[w] = a.tile_f[((int64_t)blockIdx.x * kWaves + w) * a.width + blockIdx.y * slice + t.column + e];
+#pragma unroll
+      for (int w = 0; w < kWaves - 1; ++w)
+        if (w < t.wave) h[e] = apply(m[w].x, m[w].y, h[e]);
+    }
   }
   for (int32_t k = 0; k < a.tiles; ++k) {
-    if (first + (int64_t)k * tile_rows >= n) break;
-    const int64_t row0 = first + (int64_t)k * tile_rows + t.wave * t.groups * R;
+    const int64_t row0 = first + (int64_t)k * rows;
+    if (row0 >= n) break;
     const int32_t row = (int32_t)row0 + t.group * R;
     emc2_fvec<N> keep[R], add[R];
-    Map<N> m = nothing<N>();
-    bool marked = false;
-    if (row0 < n) {
-      const Rows<T, N, R> x = fetch<T, N, R>(a, a.x, a.ld_x, n, row, t), g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, row, t);
-      marked = mark(a, n, (int32_t)row0, t.groups * R, j, next, starts[t.wave], ends[t.wave], t.lane);
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        emc2_fvec<N> take;
-        open<T, N>(g.v[i], keep[i], take);
-        add[i] = take * __builtin_convertvector(x.v[i], emc2_fvec<N>);
-      }
-      if (row0 + t.groups * R > n) blank<N, R>(n, row, keep, add);
-      m = run_forward<N, R>(a, keep, add, marked, &starts[t.wave][t.group * R], t);
+    for (int i = 0; i < R; ++i) {
+      emc2_fvec<N> take;
+      open<T, N>(g.v[i], keep[i], take);
+      add[i] = take * __builtin_convertvector(x.v[i], emc2_fvec<N>);
     }
+    if (k + 1 < a.tiles && row0 + rows < n) {
+      x = fetch<T, N, R>(a, a.x, a.ld_x, n, (int64_t)row + rows, t);
+      g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, (int64_t)row + rows, t);
+    }
+    const bool marked = mark(a, n, (int32_t)row0, rows, j, next, starts[t.wave], ends[t.wave], t.lane);
+    if (row0 + rows > n) blank<N, R>(n, row, keep, add);
+    Map<N> m = run_forward<N, R>(a, keep, add, marked, &starts[t.wave][t.group * R], t);
     // maps of all rows of the wave up to the group's last; then of those before its first
     for (int dist = 1 << a.lane_shift; dist < 64; dist <<= 1) {
       const Map<N> before = from_below<N>(m, dist);
       if (t.lane >= dist) m = then<N>(before, m);
     }
-    if (t.group == t.groups - 1) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) total[k & 1][t.wave][t.column + e] = make_float2(m.A[e], m.B[e]);
-    }
     m = from_below<N>(m, 1 << a.lane_shift);
-    if (t.group == 0) m = nothing<N>();
-    __syncthreads();
-    emc2_fvec<N> leave = h;
+    if (t.group > 0) h = apply<N>(m, h);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      if (w == t.wave) h = leave;
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float2 q = total[k & 1][w][t.column + e];
-        leave[e] = apply(q.x, q.y, leave[e]);
+    for (int i = 0; i < R; ++i) {
+      const int32_t r = row + i;
+      if (marked && starts[t.wave][t.group * R + i] >= 0) h = state_or_zero<N>(a.h0, a, starts[t.wave][t.group * R + i], t);
+      h = keep[i] * h + add[i];
+      if (r < n && t.in) {
+        emc2_store<N>((T*)a.y + (int64_t)(a.backwards ? n - 1 - r : r) * a.ld_y + t.channel, h);
+        if (marked && a.last && ends[t.wave][t.group * R + i] >= 0)
+          emc2_store_params<N>(a.last + (int64_t)ends[t.wave][t.group * R + i] * a.channels + t.channel, h);
       }
     }
-    h = apply<N>(m, h);
-    if (row0 < n) {
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const int32_t r = row + i;
-        if (marked && starts[t.wave][t.group * R + i] >= 0) h = state_or_zero<N>(a.h0, a, starts[t.wave][t.group * R + i], t);
-        h = keep[i] * h + add[i];
-        if (r < n && t.in) {
-          emc2_store<N>((T*)a.y + (int64_t)(a.backwards ? n - 1 - r : r) * a.ld_y + t.channel, h);
-          if (marked && a.last && ends[t.wave][t.group * R + i] >= 0)
-            emc2_store_params<N>(a.last + (int64_t)ends[t.wave][t.group * R + i] * a.channels + t.channel, h);
-        }
-      }
-    }
-    h = leave;
+    for (int e = 0; e < N; ++e) h[e] = __shfl(h[e], t.lane | (64 - (1 << a.lane_shift)), 64);   // the last row group's: enters the next tile
   }
 }
 
 template <typename T, int N, int R>
-__global__ void __launch_bounds__(kThreads) k_recurrence_grad(const Args a) {
-  constexpr int kSlice = 64;
+__global__ void __launch_bounds__(64 * kWavesGrad) k_recurrence_grad(const Args a) {
+  constexpr int kWaves = kWavesGrad;
   __shared__ float2 total[2][2][kWaves][kSlice];
   __shared__ int32_t starts[kWaves][64 * R], ends[kWaves][64 * R];
-  __shared__ float2 part[kThreads];
+  __shared__ float2 part[64 * kWaves];
   __shared__ float enter[kMaxTiles][kSlice], enter_r[kSlice];
   const Place t = place_of<N>(a);
   const int32_t n = rows_of(a);
-  if (gridDim.x == 1 && blockIdx.y == 0 && threadIdx.x == 0 && a.offsets[a.n_seq] > a.capacity) atomicOr(a.flags, EMC2_DEVFLAG_CAPACITY);
+  if (gridDim.x == 1) report(a);
   const int slice = N << a.lane_shift;
   const int32_t tile_rows = kWaves * t.groups * R, block_rows = a.tiles * tile_rows;
   const int64_t first = (int64_t)blockIdx.x * block_rows;
   pass_empty(a, n, a.dlast, a.dh0, slice);
   if (first >= n) return;
   const int32_t here = (int32_t)((n - first + tile_rows - 1) / tile_rows), tiles = here < a.tiles ? here : a.tiles;
+  const int64_t mine = first + (int64_t)(tiles - 1) * tile_rows + (t.wave * t.groups + t.group) * R;
+  Rows<T, N, R> xv = fetch<T, N, R>(a, a.x, a.ld_x, n, mine, t), g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, mine, t),
+                d = fetch<T, N, R>(a, a.dy, a.ld_dy, n, mine, t);
+  Falling at;
   emc2_fvec<N> flow = emc2_fvec<N>(0.0f);                  // what flows into the tile from later rows
   const int32_t blocks = (int32_t)(((int64_t)n + block_rows - 1) / block_rows);
   if (blocks > 1 || tiles > 1) {
-    compose<false>(a.block_f, a.width, blockIdx.y * slice, slice, 0, blockIdx.x, part, enter[0]);
-    compose<true>(a.block_r, a.width, blockIdx.y * slice, slice, blockIdx.x + 1, blocks, part, enter_r);
+    compose<false, kWaves>(a.block_f, a.width, blockIdx.y * slice, slice, 0, blockIdx.x, part, enter[0]);
+    compose<true, kWaves>(a.block_r, a.width, blockIdx.y * slice, slice, blockIdx.x + 1, blocks, part, enter_r);
     if ((int)threadIdx.x < slice) {
       float h = enter[0][threadIdx.x];
       for (int32_t k = 1; k < tiles; ++k) {
@@ -461,17 +532,20 @@ __global__ void __launch_bounds__(kThreads) k_recurrence_grad(const Args a) {
     emc2_fvec<N> keep[R], take[R], x[R], dy[R];
     Map<N> f = nothing<N>(), r = nothing<N>();
     bool marked = false;
-    if (row0 < n) {
-      const Rows<T, N, R> xv = fetch<T, N, R>(a, a.x, a.ld_x, n, row, t), g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, row, t),
-                          d = fetch<T, N, R>(a, a.dy, a.ld_dy, n, row, t);
-      int32_t j = seek_far(a, n, (int32_t)row0, t.lane), next = -1;
-      marked = mark(a, n, (int32_t)row0, t.groups * R, j, next, starts[t.wave], ends[t.wave], t.lane);
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        open<T, N>(g.v[i], keep[i], take[i]);
-        x[i] = __builtin_convertvector(xv.v[i], emc2_fvec<N>);
-        dy[i] = __builtin_convertvector(d.v[i], emc2_fvec<N>);
-      }
+    for (int i = 0; i < R; ++i) {
+      open<T, N>(g.v[i], keep[i], take[i]);
+      x[i] = __builtin_convertvector(xv.v[i], emc2_fvec<N>);
+      dy[i] = __builtin_convertvector(d.v[i], emc2_fvec<N>);
+    }
+    if (k > 0) {
+      xv = fetch<T, N, R>(a, a.x, a.ld_x, n, (int64_t)row - tile_rows, t);
+      g = fetch<T, N, R>(a, a.gate, a.ld_gate, n, (int64_t)row - tile_rows, t);
+      d = fetch<T, N, R>(a, a.dy, a.ld_dy, n, (int64_t)row - tile_rows, t);
+    }
+    if (row0 < n) {
+      at.move(a, n, (int32_t)row0, t.lane);
+      marked = mark(a, n, (int32_t)row0, t.groups * R, at.j, at.next, starts[t.wave], ends[t.wave], t.lane);
       emc2_fvec<N> add[R];
 #pragma unroll
       for (int i = 0; i < R; ++i) add[i] = take[i] * x[i];
@@ -480,9 +554,9 @@ __global__ void __launch_bounds__(kThreads) k_recurrence_grad(const Args a) {
       r = run_backward<N, R>(a, keep, dy, marked, &ends[t.wave][t.group * R], t);
     }
     for (int dist = 1 << a.lane_shift; dist < 64; dist <<= 1) {
-      const Map<N> before = from_below<N>(f, dist), after = from_above<N>(r, dist);
-      if (t.lane >= dist) f = then<N>(before, f);
-      if (t.lane + dist < 64) r = then<N>(after, r);
+      const Map<N> below = from_below<N>(f, dist), above = from_above<N>(r, dist);
+      if (t.lane >= dist) f = then<N>(below, f);
+      if (t.lane + dist < 64) r = then<N>(above, r);
     }
     if (t.group == t.groups - 1) {
 #pragma unroll
@@ -496,7 +570,7 @@ __global__ void __launch_bounds__(kThreads) k_recurrence_grad(const Args a) {
     if (t.group == 0) f = nothing<N>();
     if (t.group == t.groups - 1) r = nothing<N>();
     __syncthreads();
-    emc2_fvec<N> h, u = flow;
+    emc2_fvec<N> h, u = flow;                              // what enters the thread's rows from either side
 #pragma unroll
     for (int e = 0; e < N; ++e) h[e] = enter[k][t.column + e];
 #pragma unroll
@@ -519,11 +593,11 @@ __global__ void __launch_bounds__(kThreads) k_recurrence_grad(const Args a) {
     }
     if (row0 < n) {
       h = apply<N>(f, h), u = apply<N>(r, u);
-      emc2_fvec<N> before[R];                              // h_{t-1}
+      emc2_fvec<N> prev[R];                                // h_{t-1}
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         if (marked && starts[t.wave][t.group * R + i] >= 0) h = state_or_zero<N>(a.h0, a, starts[t.wave][t.group * R + i], t);
-        before[i] = h;
+        prev[i] = h;
         h = keep[i] * h + take[i] * x[i];
       }
 #pragma unroll
@@ -535,7 +609,7 @@ __global__ void __launch_bounds__(kThreads) k_recurrence_grad(const Args a) {
         if (at < n && t.in) {
           const int64_t place = a.backwards ? n - 1 - at : at;
           emc2_store<N>((T*)a.y + place * a.ld_y + t.channel, take[i] * du);
-          emc2_store<N>((T*)a.dgate + place * a.ld_dgate + t.channel, (before[i] - x[i]) * (keep[i] * take[i]) * du);
+          emc2_store<N>((T*)a.dgate + place * a.ld_dgate + t.channel, (prev[i] - x[i]) * (keep[i] * take[i]) * du);
           if (marked && a.dh0 && starts[t.wave][t.group * R + i] >= 0)
             emc2_store_params<N>(a.dh0 + (int64_t)starts[t.wave][t.group * R + i] * a.channels + t.channel, u);
         }
@@ -546,11 +620,11 @@ __global__ void __launch_bounds__(kThreads) k_recurrence_grad(const Args a) {
 
 // One row per sequence: N channels of a row a thread.
 template <typename T, int N>
-__global__ void __launch_bounds__(kThreads) k_recurrence_step(const T* __restrict__ x, int64_t ld_x, const T* __restrict__ gate, int64_t ld_gate,
+__global__ void __launch_bounds__(kStepThreads) k_recurrence_step(const T* __restrict__ x, int64_t ld_x, const T* __restrict__ gate, int64_t ld_gate,
                                                               const float* h_in, float* h_out, T* __restrict__ y, int64_t ld_y, int64_t rows,
                                                               int32_t channels) {
   const int32_t pieces = channels / N;
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t i = (int64_t)blockIdx.x * kStepThreads + threadIdx.x;
   if (i >= rows * pieces) return;
   const int64_t row = i / pieces;
   const int32_t c = (int32_t)(i - row * pieces) * N;
@@ -570,43 +644,42 @@ struct Plan {
 };
 Plan plan_of(emc2_dtype dtype, int64_t capacity, int32_t channels, bool wide, bool grad) {
   Plan p = {};
-  p.n = wide ? (dtype == EMC2_F32 ? 4 : 8) : 1;
-  const int pieces = (channels + p.n - 1) / p.n, most = wide ? 3 : 6;     // row groups of 8 lanes at most, 64 of single values
+  p.n = wide ? 4 : 1;
+  const int pieces = (channels + p.n - 1) / p.n, most = wide ? (dtype == EMC2_F32 ? 3 : 4) : 6;     // row groups of 128 bytes at most
   while (p.lane_shift < most && (1 << p.lane_shift) < pieces) ++p.lane_shift;
-  const int slice = p.n << p.lane_shift;
+  const int slice = p.n << p.lane_shift, groups = 64 >> p.lane_shift;
   p.slices = (channels + slice - 1) / slice;
   p.width = p.slices * slice;
-  const int64_t tile_rows = kWaves * (64 >> p.lane_shift) * (grad ? kRowsGrad : kRowsForward), tiles = emc2_div_up(capacity, tile_rows);
-  // A call of a few tiles is one launch of one block a slice, which walks them; others have about 512 blocks, two for every CU.
-  if (tiles <= (grad ? 1 : 4)) {
-    p.tiles = tiles < 1 ? 1 : (int32_t)tiles, p.blocks = 1;
-  } else {
-    const int64_t aim = 512 / p.slices > 1 ? 512 / p.slices : 1, per = emc2_div_up(tiles, aim);
-    p.tiles = (int32_t)(per < kMaxTiles ? per : kMaxTiles);
-    p.blocks = (int32_t)emc2_div_up(tiles, p.tiles);
-    p.totals = true;
+  // A call of a few tiles is one launch: the forward pass's of one wave, which walks them, the gradients' of one block and one tile.
+  const int64_t small = emc2_div_up(capacity, grad ? kWavesGrad * groups * kRowsGrad : groups * kRowsForward);
+  if (small <= (grad ? 1 : 4)) {
+    p.tiles = small < 1 ? 1 : (int32_t)small, p.blocks = 1;
+    return p;
   }
-  p.bytes = p.totals ? (int64_t)p.blocks * p.width * (int64_t)sizeof(float2) * (grad ? 2 + p.tiles : 1) : 0;
+  // Others have about 512 blocks, two for every CU, each with a whole number of tiles for every wave.
+  const int64_t tiles = emc2_div_up(capacity, groups * (grad ? kWavesGrad * kRowsGrad : kWavesForward * kRowsForward));
+  const int64_t aim = kBlocks / p.slices > 1 ? kBlocks / p.slices : 1, per = emc2_div_up(tiles, aim);
+  p.tiles = (int32_t)(per < kMaxTiles ? per : kMaxTiles);
+  p.blocks = (int32_t)emc2_div_up(tiles, p.tiles);
+  p.totals = true;
+  p.bytes = (int64_t)p.blocks * p.width * (int64_t)sizeof(float2) * (grad ? 2 + p.tiles : 1 + kWavesForward);
   return p;
 }
 
 template <typename F> void with_type(emc2_dtype dtype, int n, F&& f) {
-  if (dtype == EMC2_F32) {
-    if (n == 4) f(float(), emc2_fvec<4>());
-    else f(float(), emc2_fvec<1>());
-  } else if (dtype == EMC2_F16) {
-    if (n == 8) f(_Float16(), emc2_fvec<8>());
-    else f(_Float16(), emc2_fvec<1>());
-  } else {
-    if (n == 8) f(__bf16(), emc2_fvec<8>());
-    else f(__bf16(), emc2_fvec<1>());
-  }
+  const auto by_length = [&](auto type) {
+    if (n == 4) f(type, emc2_fvec<4>());
+    else f(type, emc2_fvec<1>());
+  };
+  if (dtype == EMC2_F32) by_length(float());
+  else if (dtype == EMC2_F16) by_length(_Float16());
+  else by_length(__bf16());
 }
 template <typename V> constexpr int kLength = sizeof(V) / sizeof(float);
 
-__global__ void __launch_bounds__(kThreads) k_frame_offsets(const int4* __restrict__ coords, const int32_t* __restrict__ d_n, int64_t capacity,
+__global__ void __launch_bounds__(kStepThreads) k_frame_offsets(const int4* __restrict__ coords, const int32_t* __restrict__ d_n, int64_t capacity,
                                                             int32_t n_batch, int32_t* __restrict__ offsets) {
-  const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t b = (int64_t)blockIdx.x * kStepThreads + threadIdx.x;
   if (b > n_batch) return;
   int32_t lo = 0, hi = emc2_row_count(d_n, capacity);
   if (b == n_batch) lo = hi;                               // every row, also one whose frame id is out of range, belongs to some frame
@@ -627,6 +700,8 @@ emc2_status check(emc2_ctx* ctx, const char* what, emc2_dtype dtype, int64_t cap
   return EMC2_OK;
 }
 bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// True if the rows at p can be moved in pieces of four values.
+bool whole_pieces(const void* p, int64_t pitch, size_t size) { return (uintptr_t)p % (4 * size) == 0 && pitch % 4 == 0; }
 
 }  // namespace
 
@@ -637,7 +712,7 @@ extern "C" emc2_status emc2_frame_offsets(emc2_ctx* ctx, const int32_t* d_coords
   if (capacity < 0 || capacity > (1ll << 30) || n_batch < 1 || n_batch > (1 << 30))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_frame_offsets: capacity outside [0, 2^30] or n_batch outside [1, 2^30]");
   if (!aligned(d_coords)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_frame_offsets: d_coords must be 16-byte aligned");
-  hipLaunchKernelGGL(k_frame_offsets, dim3((unsigned)emc2_div_up((int64_t)n_batch + 1, kThreads)), dim3(kThreads), 0, (hipStream_t)stream,
+  hipLaunchKernelGGL(k_frame_offsets, dim3((unsigned)emc2_div_up((int64_t)n_batch + 1, kStepThreads)), dim3(kStepThreads), 0, (hipStream_t)stream,
                      (const int4*)d_coords, d_n, capacity, n_batch, d_offsets);
   return emc2_check_hip(ctx, hipGetLastError(), "emc2_frame_offsets launch");
 }
@@ -664,21 +739,22 @@ extern "C" emc2_status emc2_recurrence(emc2_ctx* ctx, emc2_dtype dtype, const vo
   if (!emc2_rows_ok(d_x, ld_x, channels, size, none) || !emc2_rows_ok(d_gate, ld_gate, channels, size, none) ||
       !emc2_rows_ok(d_y, ld_y, channels, size, none))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence: null or misaligned rows, or a pitch below the channels");
-  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_gate, ld_gate, size) &&
-                    emc2_wide_rows(d_y, ld_y, size) && aligned(d_h0) && aligned(d_last);
+  const bool wide = channels % 4 == 0 && whole_pieces(d_x, ld_x, size) && whole_pieces(d_gate, ld_gate, size) &&
+                    whole_pieces(d_y, ld_y, size) && aligned(d_h0) && aligned(d_last);
   const Plan p = plan_of(dtype, capacity, channels, wide, false);
   if (work_bytes < p.bytes || (p.bytes && (!d_work || !aligned(d_work))))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence: work buffer null, misaligned or smaller than emc2_recurrence_work");
   Args a = {};
   a.x = d_x, a.gate = d_gate, a.h0 = d_h0, a.offsets = d_offsets, a.y = d_y, a.last = d_last, a.block_f = (float2*)d_work;
+  a.tile_f = a.block_f + (int64_t)p.blocks * p.width;
   a.flags = ctx->dev_words, a.ld_x = ld_x, a.ld_gate = ld_gate, a.ld_y = ld_y, a.capacity = (int32_t)capacity, a.channels = channels;
   a.width = p.width, a.n_seq = n_seq, a.tiles = p.tiles, a.backwards = backwards != 0, a.lane_shift = p.lane_shift;
   const dim3 grid((unsigned)p.blocks, (unsigned)p.slices);
   with_type(dtype, p.n, [&](auto type, auto length) {
     using T = decltype(type);
     constexpr int N = kLength<decltype(length)>;
-    if (p.totals) hipLaunchKernelGGL((k_recurrence_totals<T, N, kRowsForward, false>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
-    hipLaunchKernelGGL((k_recurrence<T, N, kRowsForward>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+    if (p.totals) hipLaunchKernelGGL((k_recurrence_totals<T, N, kRowsForward>), grid, dim3(64 * kWavesForward), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((k_recurrence<T, N, kRowsForward>), grid, dim3(p.totals ? 64 * kWavesForward : 64), 0, (hipStream_t)stream, a);
   });
   return emc2_check_hip(ctx, hipGetLastError(), "emc2_recurrence launch");
 }
@@ -697,8 +773,8 @@ extern "C" emc2_status emc2_recurrence_backward(emc2_ctx* ctx, emc2_dtype dtype,
       !emc2_rows_ok(d_dy, ld_dy, channels, size, none) || !emc2_rows_ok(d_dx, ld_dx, channels, size, none) ||
       !emc2_rows_ok(d_dgate, ld_dgate, channels, size, none))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_backward: null or misaligned rows, or a pitch below the channels");
-  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_gate, ld_gate, size) &&
-                    emc2_wide_rows(d_dy, ld_dy, size) && emc2_wide_rows(d_dx, ld_dx, size) && emc2_wide_rows(d_dgate, ld_dgate, size) &&
+  const bool wide = channels % 4 == 0 && whole_pieces(d_x, ld_x, size) && whole_pieces(d_gate, ld_gate, size) &&
+                    whole_pieces(d_dy, ld_dy, size) && whole_pieces(d_dx, ld_dx, size) && whole_pieces(d_dgate, ld_dgate, size) &&
                     aligned(d_h0) && aligned(d_dlast) && aligned(d_dh0);
   const Plan p = plan_of(dtype, capacity, channels, wide, true);
   if (work_bytes < p.bytes || (p.bytes && (!d_work || !aligned(d_work))))
@@ -713,8 +789,8 @@ extern "C" emc2_status emc2_recurrence_backward(emc2_ctx* ctx, emc2_dtype dtype,
   with_type(dtype, p.n, [&](auto type, auto length) {
     using T = decltype(type);
     constexpr int N = kLength<decltype(length)>;
-    if (p.totals) hipLaunchKernelGGL((k_recurrence_totals<T, N, kRowsGrad, true>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
-    hipLaunchKernelGGL((k_recurrence_grad<T, N, kRowsGrad>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+    if (p.totals) hipLaunchKernelGGL((k_recurrence_grad_totals<T, N, kRowsGrad>), grid, dim3(64 * kWavesGrad), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((k_recurrence_grad<T, N, kRowsGrad>), grid, dim3(64 * kWavesGrad), 0, (hipStream_t)stream, a);
   });
   return emc2_check_hip(ctx, hipGetLastError(), "emc2_recurrence_backward launch");
 }
@@ -732,15 +808,15 @@ extern "C" emc2_status emc2_recurrence_step(emc2_ctx* ctx, emc2_dtype dtype, con
   if (!emc2_rows_ok(d_x, ld_x, channels, size, false) || !emc2_rows_ok(d_gate, ld_gate, channels, size, false) ||
       !emc2_rows_ok(d_y, ld_y, channels, size, false))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_step: null or misaligned rows, or a pitch below the channels");
-  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_gate, ld_gate, size) &&
-                    emc2_wide_rows(d_y, ld_y, size) && aligned(d_h) && aligned(d_h_out);
-  const int n = wide ? (dtype == EMC2_F32 ? 4 : 8) : 1;
-  const int64_t blocks = emc2_div_up(rows * (channels / n), kThreads);
+  const bool wide = channels % 4 == 0 && whole_pieces(d_x, ld_x, size) && whole_pieces(d_gate, ld_gate, size) &&
+                    whole_pieces(d_y, ld_y, size) && aligned(d_h) && aligned(d_h_out);
+  const int n = wide ? 4 : 1;
+  const int64_t blocks = emc2_div_up(rows * (channels / n), kStepThreads);
   if (blocks > 0x7fffffff) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "emc2_recurrence_step: too many rows for one launch");
   with_type(dtype, n, [&](auto type, auto length) {
     using T = decltype(type);
     constexpr int N = kLength<decltype(length)>;
-    hipLaunchKernelGGL((k_recurrence_step<T, N>), dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, (const T*)d_x, ld_x,
+    hipLaunchKernelGGL((k_recurrence_step<T, N>), dim3((unsigned)blocks), dim3(kStepThreads), 0, (hipStream_t)stream, (const T*)d_x, ld_x,
                        (const T*)d_gate, ld_gate, d_h, d_h_out, (T*)d_y, ld_y, rows, channels);
   });
   return emc2_check_hip(ctx, hipGetLastError(), "emc2_recurrence_step launch");
