@@ -197,23 +197,42 @@ def _dev_check(t: torch.Tensor, dtype: torch.dtype, name: str) -> None:
         raise ValueError(f"{name}: need a contiguous {dtype} device tensor, got {t.dtype} on {t.device}")
 
 
-def _rows_check(t: torch.Tensor, dtype: torch.dtype, like: Tuple[int, int], name: str) -> int:
-    """Rows of a sequence operator: [n][channels] with neighbouring channels, rows any distance apart; returns that distance."""
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or tuple(t.shape) != like:
-        raise ValueError(f"{name}: need a {dtype} device tensor {like}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    if t.numel() == 0:
-        return like[1]
+_PLACE_TYPE_SHAPE = operator.attrgetter("is_cuda", "dtype", "shape")
+
+
+def _rows_of(x: torch.Tensor, dtype: int, name: str = "x") -> Tuple[tuple, int, int]:
+    """What the rows of a sequence operator must look like (those of its first operand): (place, type, shape), rows, channels."""
+    like = _PLACE_TYPE_SHAPE(x)
+    if like[:2] != (True, _TORCH_DTYPE[dtype]) or len(like[2]) != 2:
+        raise ValueError(f"{name}: need {_TORCH_DTYPE[dtype]} rows [n][channels] on the device, got {x.dtype} {tuple(x.shape)} on {x.device}")
+    return like, like[2][0], like[2][1]
+
+
+def _pitch(t: Optional[torch.Tensor], like: tuple, name: str) -> int:
+    """Distance of the rows of `t`: as many as `like` says, any distance apart, channels neighbours."""
+    if t is None:
+        return 0
+    if _PLACE_TYPE_SHAPE(t) != like:
+        raise ValueError(f"{name}: need {like[1]} rows {tuple(like[2])} on the device, got {t.dtype} {tuple(t.shape)} on {t.device}")
     ld, step = t.stride()
-    if (step != 1 and like[1] > 1) or (ld < like[1] and like[0] > 1):
+    n, c = like[2]
+    if (step != 1 and c > 1 and n > 0) or (ld < c and n > 1):
         raise ValueError(f"{name}: channels of a row must be neighbours and rows must not overlap, got strides {t.stride()}")
-    return max(ld, like[1])
+    return ld if ld > c else c
 
 
 def _params_check(t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...], name: str) -> None:
-    if t is not None:
-        _dev_check(t, dtype, name)
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name}: need {shape}, got {tuple(t.shape)}")
+    if t is not None and (_PLACE_TYPE_SHAPE(t) != (True, dtype, shape) or not t.is_contiguous()):
+        raise ValueError(f"{name}: need a contiguous {dtype} device tensor {tuple(shape)}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _at(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream() -> int:
+    """torch's current stream, without the object around it."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _count_check(n: Optional[torch.Tensor]) -> None:
@@ -681,14 +700,13 @@ class Context:
     def layernorm(self, dtype: int, x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float, y: torch.Tensor,
                   residual: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None) -> None:
         """y = layer norm of x (+ residual, the sum going to `total` if it is given); n: device count of the rows present."""
-        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
-        ld = [_rows_check(t, td, like, nm) if t is not None else 0
-              for t, nm in ((x, "x"), (residual, "residual"), (total, "total"), (y, "y"))]
-        _params_check(gamma, torch.float32, like[1:], "gamma")
-        _params_check(beta, torch.float32, like[1:], "beta")
+        like, rows, c = _rows_of(x, dtype)
+        ld = _pitch(x, like, "x"), _pitch(residual, like, "residual"), _pitch(total, like, "total"), _pitch(y, like, "y")
+        _params_check(gamma, torch.float32, (c,), "gamma")
+        _params_check(beta, torch.float32, (c,), "beta")
         _count_check(n)
-        self._chk(self.lib.emc2_layernorm(self.h, dtype, _ptr(x), ld[0], _ptr(residual), ld[1], _ptr(gamma), _ptr(beta), eps, _ptr(n), like[0],
-                                          like[1], _ptr(total), ld[2], _ptr(y), ld[3], _stream()))
+        self._chk(self.lib.emc2_layernorm(self.h, dtype, _at(x), ld[0], _at(residual), ld[1], _at(gamma), _at(beta), eps, _at(n), rows, c,
+                                          _at(total), ld[2], _at(y), ld[3], _raw_stream()))
 
     def layernorm_work(self, dtype: int, capacity: int, channels: int) -> int:
         return self.lib.emc2_layernorm_work(dtype, capacity, channels)
@@ -697,14 +715,14 @@ class Context:
                            dgamma: torch.Tensor, dbeta: torch.Tensor, work: torch.Tensor, add: Optional[torch.Tensor] = None,
                            n: Optional[torch.Tensor] = None) -> None:
         """dx (+ add), dgamma, dbeta of a layer norm of x for dy."""
-        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
-        ld = [_rows_check(t, td, like, nm) if t is not None else 0 for t, nm in ((x, "x"), (dy, "dy"), (add, "add"), (dx, "dx"))]
+        like, rows, c = _rows_of(x, dtype)
+        ld = _pitch(x, like, "x"), _pitch(dy, like, "dy"), _pitch(add, like, "add"), _pitch(dx, like, "dx")
         for t, nm in ((gamma, "gamma"), (dgamma, "dgamma"), (dbeta, "dbeta")):
-            _params_check(t, torch.float32, like[1:], nm)
+            _params_check(t, torch.float32, (c,), nm)
         _count_check(n)
-        size = _work_check(work, self.lib.emc2_layernorm_work(dtype, *like))
-        self._chk(self.lib.emc2_layernorm_backward(self.h, dtype, _ptr(x), ld[0], _ptr(dy), ld[1], _ptr(add), ld[2], _ptr(gamma), eps, _ptr(n),
-                                                   like[0], like[1], _ptr(dx), ld[3], _ptr(dgamma), _ptr(dbeta), _ptr(work), size, _stream()))
+        size = _work_check(work, self.lib.emc2_layernorm_work(dtype, rows, c))
+        self._chk(self.lib.emc2_layernorm_backward(self.h, dtype, _at(x), ld[0], _at(dy), ld[1], _at(add), ld[2], _at(gamma), eps, _at(n),
+                                                   rows, c, _at(dx), ld[3], _at(dgamma), _at(dbeta), _at(work), size, _raw_stream()))
 
     def recurrence_work(self, dtype: int, capacity: int, channels: int) -> int:
         return self.lib.emc2_recurrence_work(dtype, capacity, channels)
@@ -712,39 +730,39 @@ class Context:
     def recurrence(self, dtype: int, x: torch.Tensor, gate: torch.Tensor, offsets: torch.Tensor, y: torch.Tensor, work: torch.Tensor,
                    backwards: bool = False, h0: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None) -> None:
         """y_t = h_t = a_t h_{t-1} + (1 - a_t) x_t along every sequence, a = sigmoid(gate); offsets [sequences + 1] device int32."""
-        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
-        ld = [_rows_check(t, td, like, nm) for t, nm in ((x, "x"), (gate, "gate"), (y, "y"))]
+        like, rows, c = _rows_of(x, dtype)
+        ld = _pitch(x, like, "x"), _pitch(gate, like, "gate"), _pitch(y, like, "y")
         _dev_check(offsets, torch.int32, "offsets")
         n_seq = offsets.numel() - 1
-        _params_check(h0, torch.float32, (n_seq, like[1]), "h0")
-        _params_check(last, torch.float32, (n_seq, like[1]), "last")
-        size = _work_check(work, self.lib.emc2_recurrence_work(dtype, *like))
-        self._chk(self.lib.emc2_recurrence(self.h, dtype, _ptr(x), ld[0], _ptr(gate), ld[1], _ptr(offsets), n_seq, like[0], like[1],
-                                           int(bool(backwards)), _ptr(h0), _ptr(y), ld[2], _ptr(last), _ptr(work), size, _stream()))
+        _params_check(h0, torch.float32, (n_seq, c), "h0")
+        _params_check(last, torch.float32, (n_seq, c), "last")
+        size = _work_check(work, self.lib.emc2_recurrence_work(dtype, rows, c))
+        self._chk(self.lib.emc2_recurrence(self.h, dtype, _at(x), ld[0], _at(gate), ld[1], _at(offsets), n_seq, rows, c,
+                                           int(bool(backwards)), _at(h0), _at(y), ld[2], _at(last), _at(work), size, _raw_stream()))
 
     def recurrence_backward(self, dtype: int, x: torch.Tensor, gate: torch.Tensor, offsets: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor,
                             dgate: torch.Tensor, work: torch.Tensor, backwards: bool = False, h0: Optional[torch.Tensor] = None,
                             dlast: Optional[torch.Tensor] = None, dh0: Optional[torch.Tensor] = None) -> None:
         """dx, dgate and dh0 of a recurrence over x and gate, for dy and the gradient of the last states."""
-        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
-        ld = [_rows_check(t, td, like, nm) for t, nm in ((x, "x"), (gate, "gate"), (dy, "dy"), (dx, "dx"), (dgate, "dgate"))]
+        like, rows, c = _rows_of(x, dtype)
+        ld = _pitch(x, like, "x"), _pitch(gate, like, "gate"), _pitch(dy, like, "dy"), _pitch(dx, like, "dx"), _pitch(dgate, like, "dgate")
         _dev_check(offsets, torch.int32, "offsets")
         n_seq = offsets.numel() - 1
         for t, nm in ((h0, "h0"), (dlast, "dlast"), (dh0, "dh0")):
-            _params_check(t, torch.float32, (n_seq, like[1]), nm)
-        size = _work_check(work, self.lib.emc2_recurrence_work(dtype, *like))
-        self._chk(self.lib.emc2_recurrence_backward(self.h, dtype, _ptr(x), ld[0], _ptr(gate), ld[1], _ptr(offsets), n_seq, like[0], like[1],
-                                                    int(bool(backwards)), _ptr(h0), _ptr(dy), ld[2], _ptr(dlast), _ptr(dx), ld[3], _ptr(dgate),
-                                                    ld[4], _ptr(dh0), _ptr(work), size, _stream()))
+            _params_check(t, torch.float32, (n_seq, c), nm)
+        size = _work_check(work, self.lib.emc2_recurrence_work(dtype, rows, c))
+        self._chk(self.lib.emc2_recurrence_backward(self.h, dtype, _at(x), ld[0], _at(gate), ld[1], _at(offsets), n_seq, rows, c,
+                                                    int(bool(backwards)), _at(h0), _at(dy), ld[2], _at(dlast), _at(dx), ld[3], _at(dgate),
+                                                    ld[4], _at(dh0), _at(work), size, _raw_stream()))
 
     def recurrence_step(self, dtype: int, x: torch.Tensor, gate: torch.Tensor, h: torch.Tensor, h_out: torch.Tensor, y: torch.Tensor) -> None:
         """One row per sequence: h_out = a h + (1 - a) x (h_out may be h), y the same rounded."""
-        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
-        ld = [_rows_check(t, td, like, nm) for t, nm in ((x, "x"), (gate, "gate"), (y, "y"))]
-        _params_check(h, torch.float32, like, "h")
-        _params_check(h_out, torch.float32, like, "h_out")
-        self._chk(self.lib.emc2_recurrence_step(self.h, dtype, _ptr(x), ld[0], _ptr(gate), ld[1], _ptr(h), like[0], like[1], _ptr(h_out), _ptr(y),
-                                                ld[2], _stream()))
+        like, rows, c = _rows_of(x, dtype)
+        ld = _pitch(x, like, "x"), _pitch(gate, like, "gate"), _pitch(y, like, "y")
+        _params_check(h, torch.float32, (rows, c), "h")
+        _params_check(h_out, torch.float32, (rows, c), "h_out")
+        self._chk(self.lib.emc2_recurrence_step(self.h, dtype, _at(x), ld[0], _at(gate), ld[1], _at(h), rows, c, _at(h_out), _at(y),
+                                                ld[2], _raw_stream()))
 
     def ffn_packed_size(self, dtype: int, channels: int, hidden: int) -> int:
         """Values of the packed weights of a gated feed-forward network."""
@@ -756,7 +774,7 @@ class Context:
         for t, shape, nm in ((wg, (c, f), "wg"), (wu, (c, f), "wu"), (wd, (f, c), "wd")):
             _params_check(t, td, shape, nm)
         self._packed_check(packed, dtype, c, f)
-        self._chk(self.lib.emc2_ffn_pack(self.h, dtype, _ptr(wg), _ptr(wu), _ptr(wd), c, f, _ptr(packed), _stream()))
+        self._chk(self.lib.emc2_ffn_pack(self.h, dtype, _at(wg), _at(wu), _at(wd), c, f, _at(packed), _raw_stream()))
 
     def _packed_check(self, packed: torch.Tensor, dtype: int, c: int, f: int) -> None:
         _dev_check(packed, _TORCH_DTYPE[dtype], "packed")
@@ -766,12 +784,12 @@ class Context:
     def ffn(self, dtype: int, activation: int, x: torch.Tensor, packed: torch.Tensor, hidden: int, y: torch.Tensor,
             residual: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None) -> None:
         """y = (act(x wg) * (x wu)) wd (+ residual); packed: ffn_pack's; n: device count of the rows present."""
-        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
-        ld = [_rows_check(t, td, like, nm) if t is not None else 0 for t, nm in ((x, "x"), (residual, "residual"), (y, "y"))]
+        like, rows, c = _rows_of(x, dtype)
+        ld = _pitch(x, like, "x"), _pitch(residual, like, "residual"), _pitch(y, like, "y")
         _count_check(n)
-        self._packed_check(packed, dtype, like[1], hidden)
-        self._chk(self.lib.emc2_ffn(self.h, dtype, activation, _ptr(x), ld[0], _ptr(packed), _ptr(residual), ld[1], _ptr(n), like[0], like[1],
-                                    hidden, _ptr(y), ld[2], _stream()))
+        self._packed_check(packed, dtype, c, hidden)
+        self._chk(self.lib.emc2_ffn(self.h, dtype, activation, _at(x), ld[0], _at(packed), _at(residual), ld[1], _at(n), rows, c,
+                                    hidden, _at(y), ld[2], _raw_stream()))
 
     def ffn_work(self, dtype: int, capacity: int, channels: int, hidden: int) -> int:
         return self.lib.emc2_ffn_work(dtype, capacity, channels, hidden)
@@ -779,13 +797,13 @@ class Context:
     def ffn_backward(self, dtype: int, activation: int, x: torch.Tensor, packed: torch.Tensor, hidden: int, dy: torch.Tensor, dx: torch.Tensor,
                      dwg: torch.Tensor, dwu: torch.Tensor, dwd: torch.Tensor, work: torch.Tensor, n: Optional[torch.Tensor] = None) -> None:
         """dx and the weights' gradients of ffn for dy."""
-        td, like = _TORCH_DTYPE[dtype], tuple(x.shape)
-        ld = [_rows_check(t, td, like, nm) for t, nm in ((x, "x"), (dy, "dy"), (dx, "dx"))]
-        c = like[1]
+        like, rows, c = _rows_of(x, dtype)
+        td = like[1]
+        ld = _pitch(x, like, "x"), _pitch(dy, like, "dy"), _pitch(dx, like, "dx")
         for t, shape, nm in ((dwg, (c, hidden), "dwg"), (dwu, (c, hidden), "dwu"), (dwd, (hidden, c), "dwd")):
             _params_check(t, td, shape, nm)
         _count_check(n)
         self._packed_check(packed, dtype, c, hidden)
-        size = _work_check(work, self.lib.emc2_ffn_work(dtype, like[0], c, hidden))
-        self._chk(self.lib.emc2_ffn_backward(self.h, dtype, activation, _ptr(x), ld[0], _ptr(packed), _ptr(dy), ld[1], _ptr(n), like[0], c, hidden,
-                                             _ptr(dx), ld[2], _ptr(dwg), _ptr(dwu), _ptr(dwd), _ptr(work), size, _stream()))
+        size = _work_check(work, self.lib.emc2_ffn_work(dtype, rows, c, hidden))
+        self._chk(self.lib.emc2_ffn_backward(self.h, dtype, activation, _at(x), ld[0], _at(packed), _at(dy), ld[1], _at(n), rows, c, hidden,
+                                             _at(dx), ld[2], _at(dwg), _at(dwu), _at(dwd), _at(work), size, _raw_stream()))

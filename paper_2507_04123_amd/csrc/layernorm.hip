@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kThreads) k_layernorm(const NormArgs a) {
   }
 }
 
-template <typename T, int N, int L, int V, int U>
+template <typename T, int N, int L, int V>
 __global__ void __launch_bounds__(kThreads) k_layernorm_grad(const NormArgs a, float* __restrict__ dgamma, float* __restrict__ dbeta) {
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
   constexpr int kGroups = kThreads / L;
@@ -115,52 +115,42 @@ __global__ void __launch_bounds__(kThreads) k_layernorm_grad(const NormArgs a, f
     gamma[v] = 0.0f, sum_g[v] = 0.0f, sum_b[v] = 0.0f;
     if (c < a.channels) gamma[v] = emc2_load_params<N>(a.gamma + c);
   }
-  const int64_t step = (int64_t)gridDim.x * (kGroups * U);
-  for (int64_t first = (int64_t)blockIdx.x * (kGroups * U) + threadIdx.x / L; first < n; first += step) {
-    emc2_fvec<N> x[U][V], dy[U][V];
+  const int64_t step = (int64_t)gridDim.x * kGroups;
+  for (int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / L; row < n; row += step) {
+    emc2_fvec<N> x[V], dy[V], t[V];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t row = first + u * kGroups;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int c = (v * L + sub) * N;
-        x[u][v] = 0.0f, dy[u][v] = 0.0f;
-        if (row < n && c < a.channels) {
-          x[u][v] = emc2_load<N>((const T*)a.x + row * a.ld_x + c);
-          dy[u][v] = emc2_load<N>((const T*)a.dy + row * a.ld_dy + c);
-        }
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * L + sub) * N;
+      x[v] = 0.0f, dy[v] = 0.0f;
+      if (c < a.channels) {
+        x[v] = emc2_load<N>((const T*)a.x + row * a.ld_x + c);
+        dy[v] = emc2_load<N>((const T*)a.dy + row * a.ld_dy + c);
       }
     }
+    const float mean = lane_sum<L>(sum_of<N, V>(x)) * a.inv_channels;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t row = first + u * kGroups;
-      const float mean = lane_sum<L>(sum_of<N, V>(x[u])) * a.inv_channels;
-      emc2_fvec<N> t[V];
+    for (int v = 0; v < V; ++v) {
+      x[v] = (v * L + sub) * N < a.channels ? x[v] - mean : emc2_fvec<N>(0.0f);
+      t[v] = x[v] * x[v];
+    }
+    const float rstd = 1.0f / __builtin_sqrtf(lane_sum<L>(sum_of<N, V>(t)) * a.inv_channels + a.eps);
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        x[u][v] = (v * L + sub) * N < a.channels ? x[u][v] - mean : emc2_fvec<N>(0.0f);
-        t[v] = x[u][v] * x[u][v];
-      }
-      const float var = lane_sum<L>(sum_of<N, V>(t)) * a.inv_channels;
-      const float rstd = row < n ? 1.0f / __builtin_sqrtf(var + a.eps) : 0.0f;
+    for (int v = 0; v < V; ++v) {
+      x[v] *= rstd;                                        // xh
+      sum_g[v] += dy[v] * x[v];
+      sum_b[v] += dy[v];
+      dy[v] *= gamma[v];
+      t[v] = dy[v] * x[v];
+    }
+    const float mean_q = lane_sum<L>(sum_of<N, V>(dy)) * a.inv_channels;
+    const float mean_qx = lane_sum<L>(sum_of<N, V>(t)) * a.inv_channels;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        x[u][v] *= rstd;                                   // xh
-        sum_g[v] += dy[u][v] * x[u][v];
-        sum_b[v] += dy[u][v];
-        dy[u][v] *= gamma[v];
-        t[v] = dy[u][v] * x[u][v];
-      }
-      const float mean_q = lane_sum<L>(sum_of<N, V>(dy[u])) * a.inv_channels;
-      const float mean_qx = lane_sum<L>(sum_of<N, V>(t)) * a.inv_channels;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int c = (v * L + sub) * N;
-        if (row < n && c < a.channels) {
-          emc2_fvec<N> dx = (dy[u][v] - mean_q - x[u][v] * mean_qx) * rstd;
-          if (a.res) dx += emc2_load<N>((const T*)a.res + row * a.ld_res + c);
-          emc2_store<N>((T*)a.y + row * a.ld_y + c, dx);
-        }
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * L + sub) * N;
+      if (c < a.channels) {
+        emc2_fvec<N> dx = (dy[v] - mean_q - x[v] * mean_qx) * rstd;
+        if (a.res) dx += emc2_load<N>((const T*)a.res + row * a.ld_res + c);
+        emc2_store<N>((T*)a.y + row * a.ld_y + c, dx);
       }
     }
   }
@@ -264,7 +254,11 @@ template <typename F> void with_type(emc2_dtype dtype, const Shape& s, F&& f) {
   }
 }
 
-constexpr int64_t kGradBlocks = 1024;
+// Blocks of the backward pass, each walking the rows in steps of all blocks: about as many as the chip holds at once (a lane's sums and one row of 16
+// bytes leave room for five or six a CU, two rows' worth for four), one row a lane at a time.  us with the forward pass, 240 k x 128 bf16 / 600 k x 64 f16 /
+// 30 k x 1024 bf16: 1280 or 1536 blocks 69 / 81 / 74, 1024 of two rows at a time 76 / 85 / 65, 1024 of four 94 / 106 / 67.
+constexpr int64_t kGradBlocks = 1280;
+constexpr int64_t grad_blocks(int vectors) { return vectors == 1 ? kGradBlocks : 1024; }
 
 }  // namespace
 
@@ -303,7 +297,7 @@ extern "C" emc2_status emc2_layernorm(emc2_ctx* ctx, emc2_dtype dtype, const voi
 
 extern "C" int64_t emc2_layernorm_work(emc2_dtype dtype, int64_t capacity, int32_t channels) {
   if (!emc2_is_float(dtype) || channels < 1 || channels > kMaxChannels || capacity < 0 || capacity > (1ll << 30)) return -1;
-  const int64_t blocks = emc2_div_up(capacity, 4);         // a block has four rows at least
+  const int64_t blocks = emc2_div_up(capacity, 8);         // a block has eight rows at least
   return (blocks < kGradBlocks ? blocks : kGradBlocks) * 2 * channels * (int64_t)sizeof(float);
 }
 
@@ -337,9 +331,9 @@ extern "C" emc2_status emc2_layernorm_backward(emc2_ctx* ctx, emc2_dtype dtype, 
   with_type(dtype, shape_of(dtype, channels, wide), [&](auto form, auto type) {
     using F = decltype(form);
     using T = decltype(type);
-    blocks = emc2_div_up(capacity, kThreads / F::l * F::u * 2);
-    blocks = blocks < 1 ? 1 : blocks < kGradBlocks ? blocks : kGradBlocks;
-    hipLaunchKernelGGL((k_layernorm_grad<T, F::n, F::l, F::v, F::u>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, d_dgamma, d_dbeta);
+    blocks = emc2_div_up(capacity, kThreads / F::l * 2);
+    blocks = blocks < 1 ? 1 : blocks < grad_blocks(F::v) ? blocks : grad_blocks(F::v);
+    hipLaunchKernelGGL((k_layernorm_grad<T, F::n, F::l, F::v>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, d_dgamma, d_dbeta);
   });
   if (blocks > 1)
     hipLaunchKernelGGL(k_layernorm_weights, dim3((unsigned)emc2_div_up(2 * channels, 32)), dim3(1024), 0, s, a.partial, (int32_t)blocks,

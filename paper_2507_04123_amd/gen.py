@@ -208,6 +208,17 @@ def make_layer_params(layer: Layer, seed: int, layer_id: int) -> Dict[str, np.nd
     return {"w": w, "scale": scale, "shift": shift}
 
 
+def make_sequence_params(channels: int, hidden: int, seed: int, block_id: int = 0) -> Dict[str, np.ndarray]:
+    """Parameters of a sequence block in fp32: wg, wu [C][F] and wd [F][C] ~ N(0, 1 / rows); the scales of both layer norms ~ U[0.8, 1.2], their
+    shifts ~ U[-0.1, 0.1], the gates' moved up by 2, so that a new block remembers about eight voxels."""
+    st = Stream(seed, 4000 + block_id)
+    p = {k: st.normal(r * c, 1.0 / math.sqrt(r)).astype(np.float32).reshape(r, c)
+         for k, r, c in (("wg", channels, hidden), ("wu", channels, hidden), ("wd", hidden, channels))}
+    for k, lo, hi in (("gamma", 0.8, 1.2), ("beta", -0.1, 0.1), ("gate_gamma", 0.8, 1.2), ("gate_beta", 1.9, 2.1)):
+        p[k] = st.uniform(channels, lo, hi).astype(np.float32)
+    return p
+
+
 def make_camera(seed: int) -> np.ndarray:
     """Seeded 3x4 pinhole matrix P = K [R | t], row-major float32[12].
 
