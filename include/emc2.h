@@ -479,8 +479,7 @@ emc2_status emc2_project_gather(emc2_ctx* ctx, const float* d_points, int32_t st
  * 27 cells; these mix along a frame's whole list of voxels.  The operators are the library's own addition): layer norm, a gated linear
  * recurrence and a gated feed-forward network, each with its gradients, of F32, F16 or BF16 rows.
  *   - Rows lie `ld_*` elements apart (>= channels), so that a slice of wider rows can be an operand; pointers must be aligned to their
- *     element.  Where all rows of a call begin at multiples of 16 bytes and hold a multiple of 16 bytes, rows move in 16-byte pieces,
- *     else value by value.
+ *     element.  Any length and pitch moves in pieces of up to 16 bytes; rows that begin at multiples of 16 bytes are fastest.
  *   - `d_n` (device int32, or NULL): rows present, of `capacity` at most; rows beyond are neither read nor written.
  *   - Parameters and states of float* are fp32 whatever the rows' type; sums are fp32; each result is rounded once, to nearest even.
  *   - Results may lie where inputs of the same call do, if pointer and pitch are the same; otherwise they must not overlap.

@@ -46,7 +46,7 @@ enum emc2_ffn_group {   // the forward pass takes the first three, dx the last f
 
 template <typename T> __device__ __forceinline__ typename emc2_tile<T>::frag emc2_zero_frag() { return typename emc2_tile<T>::frag(T(0)); }
 
-// The fragment of row `row`, along channels kk KF ..; zero beyond the rows and channels.  WIDE: rows in 16-byte pieces.
+// The fragment of row `row`, along channels kk KF ..; zero beyond the rows and channels.  WIDE: rows are whole pieces of 16 bytes.
 template <typename T, bool WIDE>
 __device__ __forceinline__ typename emc2_tile<T>::frag emc2_row_frag(const T* p, int64_t ld, int64_t row, int32_t n, int32_t channels, int kk, int half) {
   typedef emc2_tile<T> M;
@@ -54,8 +54,8 @@ __device__ __forceinline__ typename emc2_tile<T>::frag emc2_row_frag(const T* p,
   typename M::frag f = emc2_zero_frag<T>();
   if (row < n && c < channels) {
     const T* q = p + row * ld + c;
-    if constexpr (WIDE) {
-      f = *reinterpret_cast<const typename M::frag*>(q);
+    if (WIDE || c + M::kPer <= channels) {
+      f = emc2_piece<M::kPer>(q);
     } else {
 #pragma unroll
       for (int e = 0; e < M::kPer; ++e)
@@ -136,7 +136,7 @@ static inline int emc2_ffn_tiles(int32_t channels) {        // 32-wide tiles of 
 static inline int32_t emc2_ffn_slices(int32_t hidden) { return (hidden + 63) / 64 * 2; }
 constexpr int kFfnMaxChannels = 256, kFfnMaxHidden = 1 << 16;
 
-// Calls f with a value of the type, and as constants the number of tiles, whether the activation is GELU and whether rows move in 16-byte pieces.
+// Calls f with a value of the type, and as constants the number of tiles, whether the activation is GELU and whether rows are whole pieces of 16 bytes.
 template <int N> struct emc2_const { static constexpr int value = N; };
 template <typename F> void emc2_ffn_dispatch(emc2_dtype dtype, int tiles, bool gelu, bool wide, F&& f) {
   const auto by_act = [&](auto type, auto count) {

@@ -13,11 +13,10 @@ constexpr int64_t kFewRows = 16384;
 template <typename T, bool WIDE> __device__ __forceinline__ void put(const emc2_ffn_args& a, int64_t row, int at, emc2_fvec<4> v) {
   T* out = (T*)a.y + row * a.ld_y + at;
   const T* res = (const T*)a.res + row * a.ld_res + at;
-  if constexpr (WIDE) {
-    if (at >= a.channels) return;
+  if (at + 4 <= a.channels) {
     if (a.res) v += emc2_load<4>(res);
     emc2_store<4>(out, v);
-  } else {
+  } else if constexpr (!WIDE) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (at + i < a.channels) out[i] = (T)(v[i] + (a.res ? (float)res[i] : 0.0f));
@@ -268,8 +267,7 @@ extern "C" emc2_status emc2_ffn(emc2_ctx* ctx, emc2_dtype dtype, int32_t activat
   emc2_ffn_args a = {};
   a.x = d_x, a.res = d_res, a.packed = d_packed, a.y = d_y, a.d_n = d_n, a.ld_x = ld_x, a.ld_res = ld_res, a.ld_y = ld_y;
   a.capacity = capacity, a.channels = channels, a.hidden = hidden, a.slices = emc2_ffn_slices(hidden);
-  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_y, ld_y, size) &&
-           (!d_res || emc2_wide_rows(d_res, ld_res, size));
+  const bool wide = channels % (16 / size) == 0;
   emc2_ffn_dispatch(dtype, emc2_ffn_tiles(channels), activation == EMC2_ACT_GELU, wide, [&](auto type, auto tiles, auto gelu, auto pieces) {
     using T = decltype(type);
     constexpr int CT = decltype(tiles)::value;

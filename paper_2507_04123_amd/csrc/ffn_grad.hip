@@ -15,9 +15,9 @@ constexpr int kThreads = 256;
 // Four neighbouring values of dx's row, from channel `at` on.
 template <typename T, bool WIDE> __device__ __forceinline__ void put_dx(const emc2_ffn_args& a, int64_t row, int at, emc2_fvec<4> v) {
   T* out = (T*)a.y + row * a.ld_y + at;
-  if constexpr (WIDE) {
-    if (at < a.channels) emc2_store<4>(out, v);
-  } else {
+  if (at + 4 <= a.channels) {
+    emc2_store<4>(out, v);
+  } else if constexpr (!WIDE) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (at + i < a.channels) out[i] = (T)v[i];
@@ -352,7 +352,7 @@ extern "C" emc2_status emc2_ffn_backward(emc2_ctx* ctx, emc2_dtype dtype, int32_
   a.x = d_x, a.dy = d_dy, a.packed = d_packed, a.y = d_dx, a.partial = (float*)d_work, a.d_n = d_n, a.ld_x = ld_x, a.ld_dy = ld_dy, a.ld_y = ld_dx;
   a.capacity = capacity, a.channels = channels, a.hidden = hidden, a.slices = (hidden + 31) / 32;
   a.parts = parts_of(capacity, hidden);
-  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_dy, ld_dy, size) && emc2_wide_rows(d_dx, ld_dx, size);
+  const bool wide = channels % (16 / size) == 0;
   hipStream_t s = (hipStream_t)stream;
   const int tiles = emc2_ffn_tiles(channels);
   const dim3 dw_grid((unsigned)((int64_t)a.parts * a.slices));

@@ -20,14 +20,28 @@ template <int L> __device__ __forceinline__ float lane_sum(float v) {
   return v;
 }
 
-template <int N, int V> __device__ __forceinline__ float sum_of(const emc2_fvec<N> (&x)[V]) {
-  float s = 0.0f;
+// A lane's vectors: vector v begins at channel at[v] (-1: there is none).  A row whose length is no multiple of N (MOVED) ends with a vector moved
+// back over its neighbour: the first twice[v] of its values are that one's too, computed alike by both and counted by one.
+template <int N, int L, int V, bool MOVED> struct Places {
+  int32_t at[V], twice[V];
+  __device__ __forceinline__ Places(int32_t channels, int sub) {
 #pragma unroll
-  for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v) {
+      const int32_t c = (v * L + sub) * N;
+      at[v] = c >= channels ? -1 : !MOVED || c + N <= channels ? c : channels - N;
+      twice[v] = at[v] >= 0 ? c - at[v] : 0;
+    }
+  }
+  // The sum of the values that the lane counts.
+  __device__ __forceinline__ float sum(const emc2_fvec<N> (&x)[V]) const {
+    float s = 0.0f;
 #pragma unroll
-    for (int e = 0; e < N; ++e) s += x[v][e];
-  return s;
-}
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += MOVED && e < twice[v] ? 0.0f : x[v][e];
+    return s;
+  }
+};
 
 struct NormArgs {
   const void *x, *res, *dy;      // res: forward: the residual; backward: added to dx.  May be null
@@ -41,99 +55,90 @@ struct NormArgs {
 };
 
 // N values a vector, L lanes a row, V vectors a lane, U rows of a lane under way together
-template <typename T, int N, int L, int V, int U>
-__global__ void __launch_bounds__(kThreads) k_layernorm(const NormArgs a) {
+template <typename T, int N, int L, int V, int U, bool MOVED>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) k_layernorm(const NormArgs a) {
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
   constexpr int kGroups = kThreads / L;
   const int64_t first = (int64_t)blockIdx.x * (kGroups * U) + threadIdx.x / L;
   if ((int64_t)blockIdx.x * (kGroups * U) >= n) return;
-  const int sub = threadIdx.x % L;
+  const Places<N, L, V, MOVED> p(a.channels, threadIdx.x % L);
   emc2_fvec<N> x[U][V];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t row = first + u * kGroups;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = (v * L + sub) * N;
       x[u][v] = 0.0f;
-      if (row < n && c < a.channels) x[u][v] = emc2_load<N>((const T*)a.x + row * a.ld_x + c);
+      if (row < n && p.at[v] >= 0) x[u][v] = emc2_load<N>((const T*)a.x + row * a.ld_x + p.at[v]);
     }
   }
   if (a.res) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t row = first + u * kGroups;
+      if (row >= n) break;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int c = (v * L + sub) * N;
-        if (row < n && c < a.channels) {
-          x[u][v] += emc2_load<N>((const T*)a.res + row * a.ld_res + c);
-          if (a.sum) emc2_store<N>((T*)a.sum + row * a.ld_sum + c, x[u][v]);   // rounded for the caller, not for the norm
-        }
+      for (int v = 0; v < V; ++v)
+        if (p.at[v] >= 0) x[u][v] += emc2_load<N>((const T*)a.res + row * a.ld_res + p.at[v]);
+      if (a.sum) {                                         // rounded for the caller, not for the norm; after all of the row's loads
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (p.at[v] >= 0) emc2_store<N>((T*)a.sum + row * a.ld_sum + p.at[v], x[u][v]);
       }
     }
   }
   emc2_fvec<N> gamma[V], beta[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int c = (v * L + sub) * N;
     gamma[v] = 0.0f, beta[v] = 0.0f;
-    if (c < a.channels) {
-      gamma[v] = emc2_load_params<N>(a.gamma + c);
-      beta[v] = emc2_load_params<N>(a.beta + c);
-    }
+    if (p.at[v] >= 0) gamma[v] = emc2_load<N>(a.gamma + p.at[v]), beta[v] = emc2_load<N>(a.beta + p.at[v]);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t row = first + u * kGroups;
-    const float mean = lane_sum<L>(sum_of<N, V>(x[u])) * a.inv_channels;
+    const float mean = lane_sum<L>(p.sum(x[u])) * a.inv_channels;
     emc2_fvec<N> sq[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const bool in = (v * L + sub) * N < a.channels;
       x[u][v] -= mean;
-      sq[v] = in ? x[u][v] * x[u][v] : emc2_fvec<N>(0.0f);
+      sq[v] = p.at[v] >= 0 ? x[u][v] * x[u][v] : emc2_fvec<N>(0.0f);
     }
-    const float rstd = 1.0f / __builtin_sqrtf(lane_sum<L>(sum_of<N, V>(sq)) * a.inv_channels + a.eps);
+    const float rstd = 1.0f / __builtin_sqrtf(lane_sum<L>(p.sum(sq)) * a.inv_channels + a.eps);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (v * L + sub) * N;
-      if (row < n && c < a.channels) emc2_store<N>((T*)a.y + row * a.ld_y + c, x[u][v] * rstd * gamma[v] + beta[v]);
-    }
+    for (int v = 0; v < V; ++v)
+      if (row < n && p.at[v] >= 0) emc2_store<N>((T*)a.y + row * a.ld_y + p.at[v], x[u][v] * rstd * gamma[v] + beta[v]);
   }
 }
 
-template <typename T, int N, int L, int V>
-__global__ void __launch_bounds__(kThreads) k_layernorm_grad(const NormArgs a, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+template <typename T, int N, int L, int V, bool MOVED>
+__global__ void __launch_bounds__(kThreads, V == 1 ? 5 : 2) k_layernorm_grad(const NormArgs a, float* __restrict__ dgamma, float* __restrict__ dbeta) {
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
   constexpr int kGroups = kThreads / L;
-  const int sub = threadIdx.x % L;
+  const Places<N, L, V, MOVED> p(a.channels, threadIdx.x % L);
   emc2_fvec<N> gamma[V], sum_g[V], sum_b[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int c = (v * L + sub) * N;
     gamma[v] = 0.0f, sum_g[v] = 0.0f, sum_b[v] = 0.0f;
-    if (c < a.channels) gamma[v] = emc2_load_params<N>(a.gamma + c);
+    if (p.at[v] >= 0) gamma[v] = emc2_load<N>(a.gamma + p.at[v]);
   }
   const int64_t step = (int64_t)gridDim.x * kGroups;
   for (int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / L; row < n; row += step) {
     emc2_fvec<N> x[V], dy[V], t[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = (v * L + sub) * N;
       x[v] = 0.0f, dy[v] = 0.0f;
-      if (c < a.channels) {
-        x[v] = emc2_load<N>((const T*)a.x + row * a.ld_x + c);
-        dy[v] = emc2_load<N>((const T*)a.dy + row * a.ld_dy + c);
+      if (p.at[v] >= 0) {
+        x[v] = emc2_load<N>((const T*)a.x + row * a.ld_x + p.at[v]);
+        dy[v] = emc2_load<N>((const T*)a.dy + row * a.ld_dy + p.at[v]);
       }
     }
-    const float mean = lane_sum<L>(sum_of<N, V>(x)) * a.inv_channels;
+    const float mean = lane_sum<L>(p.sum(x)) * a.inv_channels;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      x[v] = (v * L + sub) * N < a.channels ? x[v] - mean : emc2_fvec<N>(0.0f);
+      x[v] = p.at[v] >= 0 ? x[v] - mean : emc2_fvec<N>(0.0f);
       t[v] = x[v] * x[v];
     }
-    const float rstd = 1.0f / __builtin_sqrtf(lane_sum<L>(sum_of<N, V>(t)) * a.inv_channels + a.eps);
+    const float rstd = 1.0f / __builtin_sqrtf(lane_sum<L>(p.sum(t)) * a.inv_channels + a.eps);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       x[v] *= rstd;                                        // xh
@@ -142,17 +147,16 @@ __global__ void __launch_bounds__(kThreads) k_layernorm_grad(const NormArgs a, f
       dy[v] *= gamma[v];
       t[v] = dy[v] * x[v];
     }
-    const float mean_q = lane_sum<L>(sum_of<N, V>(dy)) * a.inv_channels;
-    const float mean_qx = lane_sum<L>(sum_of<N, V>(t)) * a.inv_channels;
+    const float mean_q = lane_sum<L>(p.sum(dy)) * a.inv_channels;
+    const float mean_qx = lane_sum<L>(p.sum(t)) * a.inv_channels;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = (v * L + sub) * N;
-      if (c < a.channels) {
-        emc2_fvec<N> dx = (dy[v] - mean_q - x[v] * mean_qx) * rstd;
-        if (a.res) dx += emc2_load<N>((const T*)a.res + row * a.ld_res + c);
-        emc2_store<N>((T*)a.y + row * a.ld_y + c, dx);
-      }
+      t[v] = (dy[v] - mean_q - x[v] * mean_qx) * rstd;
+      if (a.res && p.at[v] >= 0) t[v] += emc2_load<N>((const T*)a.res + row * a.ld_res + p.at[v]);
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (p.at[v] >= 0) emc2_store<N>((T*)a.y + row * a.ld_y + p.at[v], t[v]);
   }
   // The block's sums: over a wave's groups by a butterfly, over the waves through LDS, one half of the channels' vectors at a time.
   __shared__ float part[kThreads / 64][L * N];
@@ -173,11 +177,11 @@ __global__ void __launch_bounds__(kThreads) k_layernorm_grad(const NormArgs a, f
       }
       __syncthreads();
       for (int i = threadIdx.x; i < L * N; i += kThreads) {
-        const int c = v * L * N + i;
+        const int32_t from = (v * L + i / N) * N, at = from + N <= a.channels ? from : a.channels - N, c = at + i % N;
         float all = part[0][i];
 #pragma unroll
         for (int w = 1; w < kThreads / 64; ++w) all += part[w][i];
-        if (c < a.channels) {
+        if (from < a.channels && c >= from) {                // a vector moved back leaves its neighbour's channels to that one
           if (gridDim.x == 1) (which ? dbeta : dgamma)[c] = all;
           else a.partial[((int64_t)blockIdx.x * 2 + which) * a.channels + c] = all;
         }
@@ -204,61 +208,54 @@ __global__ void __launch_bounds__(1024) k_layernorm_weights(const float* __restr
   }
 }
 
-// How the rows of a call lie over the lanes: 16-byte vectors where all buffers and pitches allow it, else single values.
-struct Shape { bool wide; int lanes, vectors; };
-Shape shape_of(emc2_dtype dtype, int32_t channels, bool wide) {
-  const int per = wide ? (dtype == EMC2_F32 ? 4 : 8) : 1;
+// How the rows of a call lie over the lanes: vectors of 16 bytes, single values where a row has not even one.
+struct Shape { bool wide, moved; int lanes, vectors; };
+Shape shape_of(emc2_dtype dtype, int32_t channels) {
+  const int whole = dtype == EMC2_F32 ? 4 : 8, per = channels >= whole ? whole : 1;
   const int pieces = (channels + per - 1) / per;
-  int lanes = wide ? 8 : 16;
-  while (lanes < 64 && lanes < pieces) lanes *= wide ? 2 : 4;
+  int lanes = 8;
+  while (lanes < 64 && lanes < pieces) lanes *= 2;
   int vectors = 1;
   while (vectors * lanes < pieces) vectors *= 2;
-  return {wide, lanes, vectors};
+  return {per > 1, channels % per != 0, lanes, vectors};
 }
 
-// Calls f with the compile-time form (values a vector, lanes, vectors, rows at a time) of a shape.
-template <int N, int L, int V, int U> struct Form { static constexpr int n = N, l = L, v = V, u = U; };
-template <int N, typename F> void with_form(const Shape& s, F&& f) {
-  if constexpr (N == 1) {
-    if (s.lanes == 16) return f(Form<1, 16, 1, 4>());
-    switch (s.vectors) {
-      case 1: return f(Form<1, 64, 1, 4>());
-      case 2: return f(Form<1, 64, 2, 4>());
-      case 4: return f(Form<1, 64, 4, 2>());
-      case 8: return f(Form<1, 64, 8, 1>());
-      default: return f(Form<1, 64, 16, 1>());
-    }
-  } else {
-    switch (s.lanes) {
-      case 8: return f(Form<N, 8, 1, 4>());
-      case 16: return f(Form<N, 16, 1, 4>());
-      case 32: return f(Form<N, 32, 1, 4>());
-    }
-    switch (s.vectors) {
-      case 1: return f(Form<N, 64, 1, 2>());
-      case 2: return f(Form<N, 64, 2, 1>());
-    }
-    if constexpr (N == 4) return f(Form<N, 64, 4, 1>());
+// Calls f with the compile-time form (values a vector, lanes, vectors, rows at a time) of a shape.  Against one value a lane where rows are not whole
+// vectors: 200 k x 47 f16 forward and backward 94 us, 32 with a last vector moved back.
+template <int N, int L, int V, int U, bool MOVED = false> struct Form {
+  static constexpr int n = N, l = L, v = V, u = U;
+  static constexpr bool moved = MOVED;
+};
+template <int N, bool MOVED, typename F> void with_form(const Shape& s, F&& f) {
+  switch (s.lanes) {
+    case 8: return f(Form<N, 8, 1, 4, MOVED>());
+    case 16: return f(Form<N, 16, 1, 4, MOVED>());
+    case 32: return f(Form<N, 32, 1, 4, MOVED>());
   }
+  switch (s.vectors) {
+    case 1: return f(Form<N, 64, 1, 2, MOVED>());
+    case 2: return f(Form<N, 64, 2, 1, MOVED>());
+  }
+  if constexpr (N == 4) return f(Form<N, 64, 4, 1, MOVED>());
+}
+template <typename T, typename F> void with_type(const Shape& s, F&& f) {
+  constexpr int N = 16 / sizeof(T);
+  const auto with_T = [&](auto form) { f(form, T()); };
+  if (!s.wide) with_T(Form<1, 8, 1, 4>());
+  else if (s.moved) with_form<N, true>(s, with_T);
+  else with_form<N, false>(s, with_T);
 }
 template <typename F> void with_type(emc2_dtype dtype, const Shape& s, F&& f) {
-  if (dtype == EMC2_F32) {
-    if (s.wide) with_form<4>(s, [&](auto form) { f(form, float()); });
-    else with_form<1>(s, [&](auto form) { f(form, float()); });
-  } else if (dtype == EMC2_F16) {
-    if (s.wide) with_form<8>(s, [&](auto form) { f(form, _Float16()); });
-    else with_form<1>(s, [&](auto form) { f(form, _Float16()); });
-  } else {
-    if (s.wide) with_form<8>(s, [&](auto form) { f(form, __bf16()); });
-    else with_form<1>(s, [&](auto form) { f(form, __bf16()); });
-  }
+  if (dtype == EMC2_F32) with_type<float>(s, f);
+  else if (dtype == EMC2_F16) with_type<_Float16>(s, f);
+  else with_type<__bf16>(s, f);
 }
 
 // Blocks of the backward pass, each walking the rows in steps of all blocks: about as many as the chip holds at once (a lane's sums and one row of 16
-// bytes leave room for five or six a CU, two rows' worth for four), one row a lane at a time.  us with the forward pass, 240 k x 128 bf16 / 600 k x 64 f16 /
+// bytes leave room for five or six a CU, several vectors a lane for three), one row a lane at a time.  us with the forward pass, 240 k x 128 bf16 / 600 k x 64 f16 /
 // 30 k x 1024 bf16: 1280 or 1536 blocks 69 / 81 / 74, 1024 of two rows at a time 76 / 85 / 65, 1024 of four 94 / 106 / 67.
 constexpr int64_t kGradBlocks = 1280;
-constexpr int64_t grad_blocks(int vectors) { return vectors == 1 ? kGradBlocks : 1024; }
+constexpr int64_t grad_blocks(int vectors) { return vectors == 1 ? kGradBlocks : 768; }
 
 }  // namespace
 
@@ -278,18 +275,15 @@ extern "C" emc2_status emc2_layernorm(emc2_ctx* ctx, emc2_dtype dtype, const voi
       !emc2_rows_ok(d_res, ld_res, channels, size, true) || !emc2_rows_ok(d_sum, ld_sum, channels, size, true))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm: null or misaligned rows, or a pitch below the channels");
   if (none) return EMC2_OK;
-  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_y, ld_y, size) &&
-                    (!d_res || emc2_wide_rows(d_res, ld_res, size)) && (!d_sum || emc2_wide_rows(d_sum, ld_sum, size)) &&
-                    ((uintptr_t)d_gamma & 15) == 0 && ((uintptr_t)d_beta & 15) == 0;
   NormArgs a = {};
   a.x = d_x, a.res = d_res, a.gamma = d_gamma, a.beta = d_beta, a.d_n = d_n, a.y = d_y, a.sum = d_sum;
   a.ld_x = ld_x, a.ld_res = ld_res, a.ld_y = ld_y, a.ld_sum = ld_sum, a.capacity = capacity, a.channels = channels;
   a.eps = eps, a.inv_channels = 1.0f / (float)channels;
-  with_type(dtype, shape_of(dtype, channels, wide), [&](auto form, auto type) {
+  with_type(dtype, shape_of(dtype, channels), [&](auto form, auto type) {
     using F = decltype(form);
     using T = decltype(type);
     const int64_t rows = kThreads / F::l * F::u;
-    hipLaunchKernelGGL((k_layernorm<T, F::n, F::l, F::v, F::u>), dim3((unsigned)emc2_div_up(capacity, rows)), dim3(kThreads), 0,
+    hipLaunchKernelGGL((k_layernorm<T, F::n, F::l, F::v, F::u, F::moved>), dim3((unsigned)emc2_div_up(capacity, rows)), dim3(kThreads), 0,
                        (hipStream_t)stream, a);
   });
   return emc2_check_hip(ctx, hipGetLastError(), "emc2_layernorm launch");
@@ -320,20 +314,18 @@ extern "C" emc2_status emc2_layernorm_backward(emc2_ctx* ctx, emc2_dtype dtype, 
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm_backward: null or misaligned rows, or a pitch below the channels");
   if (work_bytes < emc2_layernorm_work(dtype, capacity, channels) || (!none && (!d_work || ((uintptr_t)d_work & 3))))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_layernorm_backward: work buffer null, misaligned or smaller than emc2_layernorm_work");
-  const bool wide = channels % (16 / size) == 0 && emc2_wide_rows(d_x, ld_x, size) && emc2_wide_rows(d_dy, ld_dy, size) &&
-                    emc2_wide_rows(d_dx, ld_dx, size) && (!d_add || emc2_wide_rows(d_add, ld_add, size)) && ((uintptr_t)d_gamma & 15) == 0;
   NormArgs a = {};
   a.x = d_x, a.res = d_add, a.dy = d_dy, a.gamma = d_gamma, a.d_n = d_n, a.y = d_dx, a.partial = (float*)d_work;
   a.ld_x = ld_x, a.ld_res = ld_add, a.ld_dy = ld_dy, a.ld_y = ld_dx, a.capacity = capacity, a.channels = channels;
   a.eps = eps, a.inv_channels = 1.0f / (float)channels;
   hipStream_t s = (hipStream_t)stream;
   int64_t blocks = 1;
-  with_type(dtype, shape_of(dtype, channels, wide), [&](auto form, auto type) {
+  with_type(dtype, shape_of(dtype, channels), [&](auto form, auto type) {
     using F = decltype(form);
     using T = decltype(type);
     blocks = emc2_div_up(capacity, kThreads / F::l * 2);
     blocks = blocks < 1 ? 1 : blocks < grad_blocks(F::v) ? blocks : grad_blocks(F::v);
-    hipLaunchKernelGGL((k_layernorm_grad<T, F::n, F::l, F::v>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, d_dgamma, d_dbeta);
+    hipLaunchKernelGGL((k_layernorm_grad<T, F::n, F::l, F::v, F::moved>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, d_dgamma, d_dbeta);
   });
   if (blocks > 1)
     hipLaunchKernelGGL(k_layernorm_weights, dim3((unsigned)emc2_div_up(2 * channels, 32)), dim3(1024), 0, s, a.partial, (int32_t)blocks,

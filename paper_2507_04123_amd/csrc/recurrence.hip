@@ -157,6 +157,7 @@ template <int N> __device__ __forceinline__ Map<N> from_above(const Map<N>& m, i
 struct Place {
   int lane, wave, group, groups, column;   // column: the first of its channels within the slice
   int32_t channel;                         // and of all
+  int twice;                               // a last piece that would pass the channels begins so many earlier: its first values are another's
   bool in;                                 // it has channels
 };
 template <int N> __device__ __forceinline__ Place place_of(const Args& a) {
@@ -168,7 +169,17 @@ template <int N> __device__ __forceinline__ Place place_of(const Args& a) {
   p.column = (p.lane & ((1 << a.lane_shift) - 1)) * N;
   p.channel = (int32_t)blockIdx.y * (N << a.lane_shift) + p.column;
   p.in = p.channel < a.channels;
+  p.twice = p.in && p.channel + N > a.channels ? p.channel + N - a.channels : 0;
+  p.channel -= p.twice;
   return p;
+}
+
+// A thread's own values of a row, to p.
+template <int N, typename T> __device__ __forceinline__ void put(T* p, emc2_fvec<N> v, const Place& t) {
+  if (N == 1 || t.twice == 0) return emc2_store<N>(p, v);
+#pragma unroll
+  for (int e = 1; e < N; ++e)
+    if (e >= t.twice) p[e] = (T)v[e];
 }
 
 // R consecutive rows of a thread as they lie in memory; rows past the last and channels that are none read valid places.
@@ -179,7 +190,7 @@ __device__ __forceinline__ Rows<T, N, R> fetch(const Args& a, const void* p, int
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int64_t k = row + i < n ? row + i : n - 1;
-    r.v[i] = *reinterpret_cast<const emc2_vec<T, N>*>((const T*)p + (a.backwards ? n - 1 - k : k) * ld + (t.in ? t.channel : 0));
+    r.v[i] = emc2_piece<N>((const T*)p + (a.backwards ? n - 1 - k : k) * ld + (t.in ? t.channel : 0));
   }
   return r;
 }
@@ -196,7 +207,7 @@ template <typename T, int N> __device__ __forceinline__ void open(emc2_vec<T, N>
 }
 
 template <int N> __device__ __forceinline__ emc2_fvec<N> state_or_zero(const float* p, const Args& a, int32_t seq, const Place& t) {
-  return p && t.in ? emc2_load_params<N>(p + (int64_t)seq * a.channels + t.channel) : emc2_fvec<N>(0.0f);
+  return p && t.in ? emc2_load<N>(p + (int64_t)seq * a.channels + t.channel) : emc2_fvec<N>(0.0f);
 }
 
 // The map of a thread's rows, first to last, from their factors and offsets.
@@ -479,9 +490,9 @@ __global__ void __launch_bounds__(64 * kWavesForward) k_recurrence(const Args a)
       if (marked && starts[t.wave][t.group * R + i] >= 0) h = state_or_zero<N>(a.h0, a, starts[t.wave][t.group * R + i], t);
       h = keep[i] * h + add[i];
       if (r < n && t.in) {
-        emc2_store<N>((T*)a.y + (int64_t)(a.backwards ? n - 1 - r : r) * a.ld_y + t.channel, h);
+        put<N>((T*)a.y + (int64_t)(a.backwards ? n - 1 - r : r) * a.ld_y + t.channel, h, t);
         if (marked && a.last && ends[t.wave][t.group * R + i] >= 0)
-          emc2_store_params<N>(a.last + (int64_t)ends[t.wave][t.group * R + i] * a.channels + t.channel, h);
+          put<N>(a.last + (int64_t)ends[t.wave][t.group * R + i] * a.channels + t.channel, h, t);
       }
     }
 #pragma unroll
@@ -608,10 +619,10 @@ __global__ void __launch_bounds__(64 * kWavesGrad) k_recurrence_grad(const Args 
         if (at < n) u = keep[i] * du;
         if (at < n && t.in) {
           const int64_t place = a.backwards ? n - 1 - at : at;
-          emc2_store<N>((T*)a.y + place * a.ld_y + t.channel, take[i] * du);
-          emc2_store<N>((T*)a.dgate + place * a.ld_dgate + t.channel, (prev[i] - x[i]) * (keep[i] * take[i]) * du);
+          put<N>((T*)a.y + place * a.ld_y + t.channel, take[i] * du, t);
+          put<N>((T*)a.dgate + place * a.ld_dgate + t.channel, (prev[i] - x[i]) * (keep[i] * take[i]) * du, t);
           if (marked && a.dh0 && starts[t.wave][t.group * R + i] >= 0)
-            emc2_store_params<N>(a.dh0 + (int64_t)starts[t.wave][t.group * R + i] * a.channels + t.channel, u);
+            put<N>(a.dh0 + (int64_t)starts[t.wave][t.group * R + i] * a.channels + t.channel, u, t);
         }
       }
     }
@@ -620,19 +631,28 @@ __global__ void __launch_bounds__(64 * kWavesGrad) k_recurrence_grad(const Args 
 
 // One row per sequence: N channels of a row a thread.
 template <typename T, int N>
-__global__ void __launch_bounds__(kStepThreads) k_recurrence_step(const T* __restrict__ x, int64_t ld_x, const T* __restrict__ gate, int64_t ld_gate,
-                                                              const float* h_in, float* h_out, T* __restrict__ y, int64_t ld_y, int64_t rows,
-                                                              int32_t channels) {
-  const int32_t pieces = channels / N;
+__global__ void __launch_bounds__(kStepThreads) k_recurrence_step(const T* x, int64_t ld_x, const T* gate, int64_t ld_gate, const float* h_in,
+                                                                  float* h_out, T* y, int64_t ld_y, int64_t rows, int32_t channels) {
+  const int32_t pieces = (channels + N - 1) / N;
   const int64_t i = (int64_t)blockIdx.x * kStepThreads + threadIdx.x;
   if (i >= rows * pieces) return;
   const int64_t row = i / pieces;
   const int32_t c = (int32_t)(i - row * pieces) * N;
-  emc2_fvec<N> keep, take;
-  open<T, N>(*reinterpret_cast<const emc2_vec<T, N>*>(gate + row * ld_gate + c), keep, take);
-  const emc2_fvec<N> h = keep * emc2_load_params<N>(h_in + row * channels + c) + take * emc2_load<N>(x + row * ld_x + c);
-  emc2_store_params<N>(h_out + row * channels + c, h);
-  emc2_store<N>(y + row * ld_y + c, h);
+  if (c + N <= channels) {
+    emc2_fvec<N> keep, take;
+    open<T, N>(emc2_piece<N>(gate + row * ld_gate + c), keep, take);
+    const emc2_fvec<N> h = keep * emc2_load<N>(h_in + row * channels + c) + take * emc2_load<N>(x + row * ld_x + c);
+    emc2_store<N>(h_out + row * channels + c, h);
+    emc2_store<N>(y + row * ld_y + c, h);
+  } else {                                                 // the row's last, incomplete piece: states may be in place, so value by value
+    for (int32_t k = c; k < channels; ++k) {
+      float keep, take;
+      emc2_logistic<sizeof(T) == 4>((float)gate[row * ld_gate + k], keep, take);
+      const float h = keep * h_in[row * channels + k] + take * (float)x[row * ld_x + k];
+      h_out[row * channels + k] = h;
+      y[row * ld_y + k] = (T)h;
+    }
+  }
 }
 
 // How a call is cut: row groups, tiles a block, blocks, and the pieces of the work buffer.
@@ -642,10 +662,10 @@ struct Plan {
   bool totals;                       // a first launch is needed
   int64_t bytes;
 };
-Plan plan_of(emc2_dtype dtype, int64_t capacity, int32_t channels, bool wide, bool grad) {
+Plan plan_of(emc2_dtype dtype, int64_t capacity, int32_t channels, bool grad) {
   Plan p = {};
-  p.n = wide ? 4 : 1;
-  const int pieces = (channels + p.n - 1) / p.n, most = wide ? (dtype == EMC2_F32 ? 3 : 4) : 6;     // row groups of 128 bytes at most
+  p.n = channels >= 4 ? 4 : 1;       // pieces of four values, wherever they lie
+  const int pieces = (channels + p.n - 1) / p.n, most = dtype == EMC2_F32 ? 3 : 4;     // row groups of 128 bytes at most
   while (p.lane_shift < most && (1 << p.lane_shift) < pieces) ++p.lane_shift;
   const int slice = p.n << p.lane_shift, groups = 64 >> p.lane_shift;
   p.slices = (channels + slice - 1) / slice;
@@ -700,8 +720,6 @@ emc2_status check(emc2_ctx* ctx, const char* what, emc2_dtype dtype, int64_t cap
   return EMC2_OK;
 }
 bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
-// True if the rows at p can be moved in pieces of four values.
-bool whole_pieces(const void* p, int64_t pitch, size_t size) { return (uintptr_t)p % (4 * size) == 0 && pitch % 4 == 0; }
 
 }  // namespace
 
@@ -719,12 +737,8 @@ extern "C" emc2_status emc2_frame_offsets(emc2_ctx* ctx, const int32_t* d_coords
 
 extern "C" int64_t emc2_recurrence_work(emc2_dtype dtype, int64_t capacity, int32_t channels) {
   if (!emc2_is_float(dtype) || channels < 1 || channels > (1 << 16) || capacity < 0 || capacity > (1ll << 30)) return -1;
-  int64_t most = 0;
-  for (int i = 0; i < 4; ++i) {
-    const int64_t b = plan_of(dtype, capacity, channels, i & 1, i & 2).bytes;
-    most = b > most ? b : most;
-  }
-  return most;
+  const int64_t forward = plan_of(dtype, capacity, channels, false).bytes, grad = plan_of(dtype, capacity, channels, true).bytes;
+  return forward > grad ? forward : grad;
 }
 
 extern "C" emc2_status emc2_recurrence(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate,
@@ -739,9 +753,7 @@ extern "C" emc2_status emc2_recurrence(emc2_ctx* ctx, emc2_dtype dtype, const vo
   if (!emc2_rows_ok(d_x, ld_x, channels, size, none) || !emc2_rows_ok(d_gate, ld_gate, channels, size, none) ||
       !emc2_rows_ok(d_y, ld_y, channels, size, none))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence: null or misaligned rows, or a pitch below the channels");
-  const bool wide = channels % 4 == 0 && whole_pieces(d_x, ld_x, size) && whole_pieces(d_gate, ld_gate, size) &&
-                    whole_pieces(d_y, ld_y, size) && aligned(d_h0) && aligned(d_last);
-  const Plan p = plan_of(dtype, capacity, channels, wide, false);
+  const Plan p = plan_of(dtype, capacity, channels, false);
   if (work_bytes < p.bytes || (p.bytes && (!d_work || !aligned(d_work))))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence: work buffer null, misaligned or smaller than emc2_recurrence_work");
   Args a = {};
@@ -773,10 +785,7 @@ extern "C" emc2_status emc2_recurrence_backward(emc2_ctx* ctx, emc2_dtype dtype,
       !emc2_rows_ok(d_dy, ld_dy, channels, size, none) || !emc2_rows_ok(d_dx, ld_dx, channels, size, none) ||
       !emc2_rows_ok(d_dgate, ld_dgate, channels, size, none))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_backward: null or misaligned rows, or a pitch below the channels");
-  const bool wide = channels % 4 == 0 && whole_pieces(d_x, ld_x, size) && whole_pieces(d_gate, ld_gate, size) &&
-                    whole_pieces(d_dy, ld_dy, size) && whole_pieces(d_dx, ld_dx, size) && whole_pieces(d_dgate, ld_dgate, size) &&
-                    aligned(d_h0) && aligned(d_dlast) && aligned(d_dh0);
-  const Plan p = plan_of(dtype, capacity, channels, wide, true);
+  const Plan p = plan_of(dtype, capacity, channels, true);
   if (work_bytes < p.bytes || (p.bytes && (!d_work || !aligned(d_work))))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_backward: work buffer null, misaligned or smaller than emc2_recurrence_work");
   Args a = {};
@@ -808,10 +817,8 @@ extern "C" emc2_status emc2_recurrence_step(emc2_ctx* ctx, emc2_dtype dtype, con
   if (!emc2_rows_ok(d_x, ld_x, channels, size, false) || !emc2_rows_ok(d_gate, ld_gate, channels, size, false) ||
       !emc2_rows_ok(d_y, ld_y, channels, size, false))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_step: null or misaligned rows, or a pitch below the channels");
-  const bool wide = channels % 4 == 0 && whole_pieces(d_x, ld_x, size) && whole_pieces(d_gate, ld_gate, size) &&
-                    whole_pieces(d_y, ld_y, size) && aligned(d_h) && aligned(d_h_out);
-  const int n = wide ? 4 : 1;
-  const int64_t blocks = emc2_div_up(rows * (channels / n), kStepThreads);
+  const int n = channels >= 4 ? 4 : 1;
+  const int64_t blocks = emc2_div_up(rows * emc2_div_up(channels, n), kStepThreads);
   if (blocks > 0x7fffffff) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "emc2_recurrence_step: too many rows for one launch");
   with_type(dtype, n, [&](auto type, auto length) {
     using T = decltype(type);

@@ -6,35 +6,18 @@
 template <typename T, int N> using emc2_vec = T __attribute__((ext_vector_type(N)));
 template <int N> using emc2_fvec = emc2_vec<float, N>;
 
-// N values at p, which lies on a multiple of their size (of 16 bytes where they take more), as floats; and back, one rounding to
-// nearest even each.
+// N values at p as they lie in memory, anywhere: the target's vector loads and stores need no more than the alignment of a value, so rows of odd
+// lengths and pitches move in 16-byte pieces too.
+template <typename T, int N> struct emc2_anywhere { typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
+template <int N, typename T> __device__ __forceinline__ emc2_vec<T, N> emc2_piece(const T* p) {
+  return *reinterpret_cast<const typename emc2_anywhere<T, N>::type*>(p);
+}
+// The same as floats; and back, one rounding to nearest even each.
 template <int N, typename T> __device__ __forceinline__ emc2_fvec<N> emc2_load(const T* p) {
-  return __builtin_convertvector(*reinterpret_cast<const emc2_vec<T, N>*>(p), emc2_fvec<N>);
+  return __builtin_convertvector(emc2_piece<N>(p), emc2_fvec<N>);
 }
 template <int N, typename T> __device__ __forceinline__ void emc2_store(T* p, emc2_fvec<N> v) {
-  *reinterpret_cast<emc2_vec<T, N>*>(p) = __builtin_convertvector(v, emc2_vec<T, N>);
-}
-// N floats of a parameter vector that lies on a multiple of 16 bytes (4 where N is 1)
-template <int N> __device__ __forceinline__ emc2_fvec<N> emc2_load_params(const float* p) {
-  if constexpr (N <= 4) {
-    return *reinterpret_cast<const emc2_fvec<N>*>(p);
-  } else {
-    emc2_fvec<N> v;
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const emc2_fvec<4> q = *reinterpret_cast<const emc2_fvec<4>*>(p + i);
-      v[i] = q[0], v[i + 1] = q[1], v[i + 2] = q[2], v[i + 3] = q[3];
-    }
-    return v;
-  }
-}
-template <int N> __device__ __forceinline__ void emc2_store_params(float* p, emc2_fvec<N> v) {
-  if constexpr (N <= 4) {
-    *reinterpret_cast<emc2_fvec<N>*>(p) = v;
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 4) *reinterpret_cast<emc2_fvec<4>*>(p + i) = emc2_fvec<4>{v[i], v[i + 1], v[i + 2], v[i + 3]};
-  }
+  *reinterpret_cast<typename emc2_anywhere<T, N>::type*>(p) = __builtin_convertvector(v, emc2_vec<T, N>);
 }
 
 // Rows that a call deals with: the device count, if it is given, kept within the capacity.
@@ -59,10 +42,6 @@ template <bool EXACT> __device__ __forceinline__ void emc2_logistic(float z, flo
   rest = t > 126.0f ? 1.0f : e * s;
 }
 
-// True if the rows at p, `pitch` elements apart, can be moved in pieces of 16 bytes (p may be null).
-static inline bool emc2_wide_rows(const void* p, int64_t pitch, size_t size) {
-  return ((uintptr_t)p & 15) == 0 && (pitch * (int64_t)size) % 16 == 0;
-}
 // Null, misaligned or overlapping-by-pitch rows are refused; p may be null if it is optional or there are no rows.
 static inline bool emc2_rows_ok(const void* p, int64_t pitch, int32_t channels, size_t size, bool optional) {
   if (!p) return optional;
