@@ -93,18 +93,15 @@ template <typename T, int CT, bool WIDE> struct emc2_row {
 };
 
 // act(g) of either activation as g s, s = logistic(z): SiLU z = g, GELU (its tanh form) z = sqrt(8 / pi) (g + 0.044715 g^3); and the slope
-// s (1 + g (1 - s) dz/dg).
+// s + g s (1 - s) dz/dg (1 - s is taken from s here: where nothing is left of it, the slope is s).
 template <bool EXACT, bool GELU> __device__ __forceinline__ float emc2_activate(float g) {
-  float s, rest;
-  emc2_logistic<EXACT>(GELU ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g, s, rest);
-  return g * s;
+  return g * emc2_logistic<EXACT>(GELU ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g);
 }
 template <bool EXACT, bool GELU> __device__ __forceinline__ float emc2_activate(float g, float& slope) {
-  float s, rest;
-  emc2_logistic<EXACT>(GELU ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g, s, rest);
-  const float dz = GELU ? 1.5957691216057308f * (1.0f + 0.134145f * g * g) : 1.0f;
-  slope = s + g * s * rest * dz;
-  return g * s;
+  const float s = emc2_logistic<EXACT>(GELU ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g), a = g * s;
+  const float rest = GELU ? (1.0f - s) * (1.5957691216057308f + 0.2140644488f * g * g) : 1.0f - s;
+  slope = __builtin_fmaf(a, rest, s);
+  return a;
 }
 // Two neighbouring values of a result tile, registers r and r + 1 (r even), into the fragments made of it.
 template <typename T> __device__ __forceinline__ void emc2_put_pair(typename emc2_tile<T>::frag* f, int r, float a, float b) {

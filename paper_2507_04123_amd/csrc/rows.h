@@ -30,16 +30,25 @@ __device__ __forceinline__ int32_t emc2_row_count(const int32_t* d_n, int64_t ca
 // The logistic function s = 1 / (1 + exp(-z)) and 1 - s = exp(-z) / (1 + exp(-z)), each to a few ulp: 1 - s is not taken from s, which
 // would leave nothing of it where s is near 1.  Where exp(-z) is beyond the range s is 0 and 1 - s is 1; NaN passes through.
 // EXACT (32-bit values): the exponent's product with log2(e) is carried to twice the precision, which matters beyond |z| of about 8.
-template <bool EXACT> __device__ __forceinline__ void emc2_logistic(float z, float& s, float& rest) {
+template <bool EXACT> __device__ __forceinline__ float emc2_exp_of_minus(float z, float& t) {
   const float log2e = 1.44269504088896341f;
-  const float t = -z * log2e;
+  t = -z * log2e;
   float e = __builtin_amdgcn_exp2f(t);
   if constexpr (EXACT) {
     const float low = __builtin_fmaf(-z, log2e, -t) - z * 1.92596299112661746e-8f;
     e = t > -126.0f && t < 126.0f ? __builtin_fmaf(e, low * 0.693147180559945309f, e) : e;
   }
+  return e;
+}
+template <bool EXACT> __device__ __forceinline__ void emc2_logistic(float z, float& s, float& rest) {
+  float t;
+  const float e = emc2_exp_of_minus<EXACT>(z, t);
   s = __builtin_amdgcn_rcpf(1.0f + e);
   rest = t > 126.0f ? 1.0f : e * s;
+}
+template <bool EXACT> __device__ __forceinline__ float emc2_logistic(float z) {
+  float t;
+  return __builtin_amdgcn_rcpf(1.0f + emc2_exp_of_minus<EXACT>(z, t));
 }
 
 // Null, misaligned or overlapping-by-pitch rows are refused; p may be null if it is optional or there are no rows.
