@@ -25,16 +25,21 @@ template <typename T, bool WIDE> __device__ __forceinline__ void put_dx(const em
 }
 
 // Many rows: every wave has 32 rows of its own and walks all slices, whose weights pass through LDS for the whole block; the next
-// slice's are on their way meanwhile.  us, the form below (whose waves split the slices) / this one: 100 k x 64 x 256 bf16 78 / 35.
-constexpr int64_t kFewRows = 16384;
-template <typename T, int CT> constexpr bool kDxMany = sizeof(T) * CT <= 8;               // two waves a SIMD have the registers
-template <typename T, int CT> constexpr int kDxManyWaves = sizeof(T) * CT <= 4 ? 4 : 8;   // (and the fragments under way are fewer a wave)
+// slice's are on their way meanwhile.  Wide rows of 16 bits take this form whatever their number; the others from that on where it is the faster one.
+// us, the form below (whose waves split the slices) / this one at 16 k, 32 k and 64 k rows: f16 64 x 256 11 / 12, 22 / 13, 39 / 21;
+// f16 128 x 512 27 / 42, 51 / 46, 99 / 54; f16 256 x 512 122 / 71, 199 / 76, 353 / 147 (2 k rows 79 / 67);
+// f32 96 x 384 67 / 106, 129 / 113, 250 / 217.
+template <typename T, int CT> constexpr bool kDxMany = sizeof(T) * CT <= 16;              // LDS has room for two slices' weights
+template <typename T, int CT> constexpr bool kDxFew = sizeof(T) == 4 || CT <= 4;
+template <typename T, int CT> constexpr int64_t kDxFewRows = !kDxFew<T, CT> ? 0 : sizeof(T) * CT < 8 ? 16384 : 32768;
+template <typename T, int CT> constexpr int kDxManyASimd = sizeof(T) * CT <= 8 ? 2 : 1;   // waves a SIMD that the registers are enough for
+template <typename T, int CT> constexpr int kDxManyWaves = sizeof(T) * CT <= 4 || sizeof(T) * CT > 8 ? 4 : 8;   // (and the fragments under way are fewer a wave)
 template <typename T, int CT, bool GELU, bool WIDE>
-__global__ void __launch_bounds__((64 * kDxManyWaves<T, CT>), 2) k_ffn_dx_many(const emc2_ffn_args a) {
+__global__ void __launch_bounds__((64 * kDxManyWaves<T, CT>), (kDxManyASimd<T, CT>)) k_ffn_dx_many(const emc2_ffn_args a) {
   typedef emc2_tile<T> M;
   typedef typename M::frag frag;
   constexpr int W = kDxManyWaves<T, CT>, KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep, kStaged = (3 * KK + W - 1) / W;
-  constexpr bool kExact = sizeof(T) == 4;
+  constexpr bool kExact = sizeof(T) == 4, kShort = sizeof(T) * CT == 16;   // registers are short: weights no further ahead
   __shared__ frag ring[2][5 * KK * 64];
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -74,6 +79,7 @@ __global__ void __launch_bounds__((64 * kDxManyWaves<T, CT>), 2) k_ffn_dx_many(c
       g = emc2_mma<T>(w[k * 64], x[k], g);
       u = emc2_mma<T>(w[(KK + k) * 64], x[k], u);
       dh = emc2_mma<T>(w[(2 * KK + k) * 64], dy[k], dh);
+      if constexpr (kShort) if (k % 8 == 7) __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_sched_barrier(0);
     keep((s + 1) & 1, 0, 3 * KK);
@@ -91,6 +97,7 @@ __global__ void __launch_bounds__((64 * kDxManyWaves<T, CT>), 2) k_ffn_dx_many(c
     for (int k = 0; k < KK; ++k) {
       dx[k / MM] = emc2_mma<T>(w[(3 * KK + k) * 64], dg[k % MM], dx[k / MM]);
       dx[k / MM] = emc2_mma<T>(w[(4 * KK + k) * 64], du[k % MM], dx[k / MM]);
+      if constexpr (kShort) if (k % 8 == 7) __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_sched_barrier(0);
     keep((s + 1) & 1, 3 * KK, 5 * KK);
@@ -105,7 +112,7 @@ __global__ void __launch_bounds__((64 * kDxManyWaves<T, CT>), 2) k_ffn_dx_many(c
 
 // A block has 32 rows; its waves (eight, or four where x, dy and dx's sums take over half of a SIMD's registers) share the slices out, each
 // reading its own weights from memory at once, and their sums meet in LDS.
-template <typename T, int CT> constexpr int kDxWaves = sizeof(T) == 2 ? (CT > 4 ? 4 : 8) : CT == 4 ? 4 : 8;
+template <typename T, int CT> constexpr int kDxWaves = sizeof(T) == 4 && CT == 4 ? 4 : 8;
 template <typename T, int CT, bool GELU, bool WIDE>
 __global__ void __launch_bounds__((64 * kDxWaves<T, CT>)) k_ffn_dx(const emc2_ffn_args a) {
   typedef emc2_tile<T> M;
@@ -179,11 +186,7 @@ __device__ __forceinline__ void turned(const emc2_row<T, CT, WIDE>& rows, int fi
 // units, columns: channels), the CB tiles of channels from C0 on.  A block has one slice, whose weights lie in LDS, and one part of the rows, which
 // its four waves share out; the next tile of rows is on its way while one is worked on.
 // Waves a SIMD: two without the next tile's rows where the sums are few.
-#ifndef DW2
-#define DW2 2
-#define DCB (CT > 4 ? CT / 2 : CT)
-#endif
-template <typename T, int CT> constexpr int kDwWaves = sizeof(T) == 2 && CT <= DW2 ? 2 : 1;
+template <typename T, int CT> constexpr int kDwWaves = sizeof(T) * CT <= 4 ? 2 : 1;   // (parts_of counts on it)
 template <typename T, int CT, bool GELU, bool WIDE, int C0, int CB>
 __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const emc2_ffn_args a) {
   typedef emc2_tile<T> M;
@@ -287,17 +290,29 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
     }
 }
 
-// Adds the parts, four values a thread, and puts them where they belong.
+// Adds the parts, four values a thread, and puts them where they belong.  Eight threads share a sum's parts out (500 parts of 32 x 128 values:
+// 9.0 us by one thread, 5.3 by eight) and meet in LDS, always in the same order.
+constexpr int kSumThreads = 8;
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_ffn_sum(const float4* __restrict__ partial, int32_t parts, int32_t slices, int32_t tiles,
                                                       int32_t channels, int32_t hidden, T* __restrict__ dwg, T* __restrict__ dwu,
                                                       T* __restrict__ dwd) {
-  const int64_t quads = (int64_t)slices * 3 * tiles * 64 * 4, at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (at >= quads) return;
-  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  constexpr int kSums = kThreads / kSumThreads;
+  __shared__ float4 meet[kSumThreads][kSums];
+  const int64_t quads = (int64_t)slices * 3 * tiles * 64 * 4, at = (int64_t)blockIdx.x * kSums + threadIdx.x % kSums;
+  const int mine = threadIdx.x / kSums;
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);              // (768 sums a tile and slice: no block has fewer than kSums)
 #pragma unroll 8
-  for (int32_t p = 0; p < parts; ++p) {
+  for (int32_t p = mine; p < parts; p += kSumThreads) {
     const float4 q = partial[p * quads + at];
+    s.x += q.x, s.y += q.y, s.z += q.z, s.w += q.w;
+  }
+  meet[mine][threadIdx.x % kSums] = s;
+  __syncthreads();
+  if (mine) return;
+#pragma unroll
+  for (int i = 1; i < kSumThreads; ++i) {
+    const float4 q = meet[i][threadIdx.x];
     s.x += q.x, s.y += q.y, s.z += q.z, s.w += q.w;
   }
   const int j = (int)(at & 3), lane = (int)(at >> 2 & 63);
@@ -316,11 +331,19 @@ __global__ void __launch_bounds__(kThreads) k_ffn_sum(const float4* __restrict__
   }
 }
 
-// Parts that the rows are cut into: about 512 blocks, two for every CU, and none of them without a tile of rows for each wave.
-int32_t parts_of(int64_t capacity, int32_t hidden) {
-  const int64_t slices = (hidden + 31) / 32, aim = emc2_div_up(512, slices), most = emc2_div_up(capacity, 32 * (kThreads / 64));
-  const int64_t parts = aim < most ? aim : most;
-  return (int32_t)(parts < 1 ? 1 : parts);
+// Parts that the rows are cut into.  The chip holds kDwWaves blocks a CU; a launch takes as many rounds of them as it needs, each as long as a
+// wave's tiles of rows and about one tile's time for the weights and the sums.  The best of one to three rounds, then the fewest parts with as many
+// tiles a wave.  us, k_ffn_dw with four blocks more than two rounds / this: 32000 x 96 x 384 f32 250 / 173, f16 58 / 38.
+int32_t parts_of(emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t hidden) {
+  const int64_t slices = (hidden + 31) / 32, tiles = emc2_div_up(capacity, 32), waves = kThreads / 64;
+  const int64_t room = 256 * (emc2_size_of(dtype) * emc2_ffn_tiles(channels) <= 4 ? 2 : 1);
+  int64_t best = 1, cost = INT64_MAX;
+  for (int64_t rounds = 1; rounds <= 3; ++rounds) {
+    const int64_t most = room * rounds / slices, turns = emc2_div_up(tiles, waves * (most ? most : 1));
+    const int64_t parts = turns ? emc2_div_up(tiles, waves * turns) : 1, c = emc2_div_up(parts * slices, room) * (turns + 1);
+    if (c < cost) best = parts, cost = c;
+  }
+  return (int32_t)best;
 }
 
 }  // namespace
@@ -329,7 +352,7 @@ extern "C" int64_t emc2_ffn_work(emc2_dtype dtype, int64_t capacity, int32_t cha
   if (!emc2_is_float(dtype) || channels < 1 || channels > kFfnMaxChannels || hidden < 1 || hidden > kFfnMaxHidden || capacity < 0 ||
       capacity > (1ll << 30))
     return -1;
-  return (int64_t)parts_of(capacity, hidden) * 3 * 32 * emc2_ffn_tiles(channels) * 32 * ((hidden + 31) / 32) * (int64_t)sizeof(float);
+  return (int64_t)parts_of(dtype, capacity, channels, hidden) * 3 * 32 * emc2_ffn_tiles(channels) * 32 * ((hidden + 31) / 32) * (int64_t)sizeof(float);
 }
 
 extern "C" emc2_status emc2_ffn_backward(emc2_ctx* ctx, emc2_dtype dtype, int32_t activation, const void* d_x, int64_t ld_x,
@@ -351,7 +374,7 @@ extern "C" emc2_status emc2_ffn_backward(emc2_ctx* ctx, emc2_dtype dtype, int32_
   emc2_ffn_args a = {};
   a.x = d_x, a.dy = d_dy, a.packed = d_packed, a.y = d_dx, a.partial = (float*)d_work, a.d_n = d_n, a.ld_x = ld_x, a.ld_dy = ld_dy, a.ld_y = ld_dx;
   a.capacity = capacity, a.channels = channels, a.hidden = hidden, a.slices = (hidden + 31) / 32;
-  a.parts = parts_of(capacity, hidden);
+  a.parts = parts_of(dtype, capacity, channels, hidden);
   const bool wide = channels % (16 / size) == 0;
   hipStream_t s = (hipStream_t)stream;
   const int tiles = emc2_ffn_tiles(channels);
@@ -359,18 +382,20 @@ extern "C" emc2_status emc2_ffn_backward(emc2_ctx* ctx, emc2_dtype dtype, int32_
   emc2_ffn_dispatch(dtype, tiles, activation == EMC2_ACT_GELU, wide, [&](auto type, auto count, auto gelu, auto pieces) {
     using T = decltype(type);
     constexpr bool G = decltype(gelu)::value, P = decltype(pieces)::value;
-    constexpr int CT = decltype(count)::value, CB = DCB;
+    constexpr int CT = decltype(count)::value, CB = CT > 4 ? CT / 2 : CT;   // (the sums of more tiles of channels leave no registers)
     // the weights' launches first: dx may lie where dy did
     hipLaunchKernelGGL((k_ffn_dw<T, CT, G, P, 0, CB>), dw_grid, dim3(kThreads), 0, s, a);
     if constexpr (CB < CT) hipLaunchKernelGGL((k_ffn_dw<T, CT, G, P, CB, CT - CB>), dw_grid, dim3(kThreads), 0, s, a);
     if constexpr (kDxMany<T, CT>) {
       constexpr int W = kDxManyWaves<T, CT>;
-      if (capacity > kFewRows)
+      if (capacity > kDxFewRows<T, CT>)
         hipLaunchKernelGGL((k_ffn_dx_many<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32 * W)), dim3(64 * W), 0, s, a);
     }
-    if (!none && !(kDxMany<T, CT> && capacity > kFewRows))
-      hipLaunchKernelGGL((k_ffn_dx<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32)), dim3(64 * kDxWaves<T, CT>), 0, s, a);
-    hipLaunchKernelGGL(k_ffn_sum<T>, dim3((unsigned)emc2_div_up((int64_t)a.slices * 3 * CT * 256, kThreads)), dim3(kThreads), 0, s,
+    if constexpr (kDxFew<T, CT>) {
+      if (!none && !(kDxMany<T, CT> && capacity > kDxFewRows<T, CT>))
+        hipLaunchKernelGGL((k_ffn_dx<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32)), dim3(64 * kDxWaves<T, CT>), 0, s, a);
+    }
+    hipLaunchKernelGGL(k_ffn_sum<T>, dim3((unsigned)((int64_t)a.slices * 3 * CT * 256 / (kThreads / kSumThreads))), dim3(kThreads), 0, s,
                        (const float4*)d_work, a.parts, a.slices, CT, channels, hidden, (T*)d_dwg, (T*)d_dwu, (T*)d_dwd);
   });
   return emc2_check_hip(ctx, hipGetLastError(), "emc2_ffn_backward launch");

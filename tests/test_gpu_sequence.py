@@ -312,6 +312,24 @@ def test_ffn_many_rows_device_count_in_place_and_no_rows(ctx, dtype):
     assert not any(t.any() for t in g)
 
 
+@pytest.mark.parametrize("dtype,c", [("f16", 24), ("f16", 40), ("f16", 96), ("f16", 128), ("f16", 192), ("f16", 250), ("bf16", 64), ("bf16", 100),
+                                     ("bf16", 256), ("f32", 32), ("f32", 48), ("f32", 96), ("f32", 126), ("f32", 200)])
+def test_ffn_of_more_rows_than_the_chip_holds_at_once(ctx, dtype, c):
+    """33 001 rows: every wave of either pass has rows of its own, and several tiles of them in the weights' gradients."""
+    n, f, act, how = 33001, 72, "gelu" if c % 3 else "silu", "slice" if c % 2 else "odd" if c % 5 == 0 else "packed"
+    code, w = B.ACT_SILU if act == "silu" else B.ACT_GELU, _weights(c, f, dtype)
+    packed = torch.full((ctx.ffn_packed_size(DT[dtype], c, f),), float("nan"), dtype=TD[dtype], device="cuda")
+    ctx.ffn_pack(DT[dtype], *(t.cuda() for t in w), packed)
+    x, dy = (_draw(60 + i, n, c, dtype=dtype) for i in range(2))
+    (xs, ds), ws = (_np(x), _np(dy)), [_np(t) for t in w]
+    y, dx, g = _like(x, how), _like(x, how), [torch.full(t.shape, 9.0, dtype=TD[dtype], device="cuda") for t in w]
+    ctx.ffn(DT[dtype], code, _rows(x, how), packed, f, y)
+    _within(y, S.ffn(act, xs, *ws), L.ffn(act, xs, *ws, np.zeros_like(xs), dtype), "y")
+    ctx.ffn_backward(DT[dtype], code, _rows(x, how), packed, f, _rows(dy, how), dx, *g, _work(ctx.ffn_work(DT[dtype], n, c, f)))
+    for got, e, b, what in zip((dx, *g), S.ffn_backward(act, xs, *ws, ds), L.ffn_backward(act, xs, *ws, ds, dtype), ("dx", "dwg", "dwu", "dwd")):
+        _within(got, e, b, what)
+
+
 # ------------------------------------------------------------------------------------------------------------ all of them
 
 def test_rows_beyond_32_bits_of_elements(ctx):
