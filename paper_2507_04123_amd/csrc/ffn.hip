@@ -7,6 +7,9 @@
 namespace {
 
 constexpr int kThreads = 256;
+// Up to here a block has 32 rows and its waves share the slices out (k_ffn_few), beyond it a wave has 32 rows of its own (k_ffn).
+// us, few / many at 8 k, 16 k, 24 k and 64 k rows: f16 64 x 256 5.3 / 9.6, 7.4 / 9.9, 10.4 / 10.2, 22 / 15; f16 128 x 512 11 / 18, 18 / 19, 26 / 19,
+// 65 / 36; f16 256 x 512 20 / 40, 38 / 42, 55 / 44, 143 / 90; f32 48 x 200 12 / 30, 20 / 31, 29 / 32, 69 / 60.
 constexpr int64_t kFewRows = 16384;
 
 // Four neighbouring values of a result's row, from channel `at` on.
@@ -38,8 +41,10 @@ template <typename T, int CT> constexpr int kFfnWaves = sizeof(T) * CT <= 8 ? 2 
 
 // Many rows: a block of four waves has 128 rows and passes the weights, slice by slice, through LDS, where all waves read them.  Turn t multiplies
 // slice t's gates, activates slice t - 1 and multiplies slice t - 2's way down: three independent strands, so that the vector ALU's
-// activation (two quarter-rate instructions an element) runs under the matrix cores' products.  The loads of turn t + 1's
-// weights are under way meanwhile.
+// activation (an exponential and a reciprocal an element) runs under the matrix cores' products.  The loads of turn t + 1's
+// weights are under way meanwhile.  300 k x 128 x 512 f16 165 us, 720 TFLOP/s: a fragment from LDS (128 bytes a clock) feeds one product of a wave,
+// which takes about as long as its reading, and 2344 blocks, two a CU at once, leave the fifth round half empty.  Measured and not better: 64 rows
+// a wave (fragments feed two products, one wave a SIMD) 211, eight waves a block with the weights two turns ahead 180, Wd's lines past LDS 244.
 constexpr int kManyWaves = 4;
 template <typename T, int CT, bool GELU, bool WIDE>
 __global__ void __launch_bounds__(64 * kManyWaves, (kFfnWaves<T, CT>)) k_ffn(const emc2_ffn_args a) {
@@ -272,7 +277,7 @@ extern "C" emc2_status emc2_ffn(emc2_ctx* ctx, emc2_dtype dtype, int32_t activat
     using T = decltype(type);
     constexpr int CT = decltype(tiles)::value;
     constexpr bool G = decltype(gelu)::value, P = decltype(pieces)::value;
-        // up to 16 384 rows there are more CUs than blocks of 128 rows need; fp32 rows of over 64 channels would leave a SIMD one wave
+    // fp32 rows of over 64 channels would leave a SIMD one wave of k_ffn: 155 / 142 us for 64 k x 96 x 384, but 79 / 72 and 42 / 67 for 32 k and 16 k
     constexpr bool kFew = sizeof(T) * CT > 8 && sizeof(T) == 4;
     if (kFew || capacity <= kFewRows)
       hipLaunchKernelGGL((k_ffn_few<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32)), dim3(64 * kFewWaves<CT, P>), 0, (hipStream_t)stream, a);

@@ -28,7 +28,8 @@ template <typename T, bool WIDE> __device__ __forceinline__ void put_dx(const em
 // slice's are on their way meanwhile.  Wide rows of 16 bits take this form whatever their number; the others from that on where it is the faster one.
 // us, the form below (whose waves split the slices) / this one at 16 k, 32 k and 64 k rows: f16 64 x 256 11 / 12, 22 / 13, 39 / 21;
 // f16 128 x 512 27 / 42, 51 / 46, 99 / 54; f16 256 x 512 122 / 71, 199 / 76, 353 / 147 (2 k rows 79 / 67);
-// f32 96 x 384 67 / 106, 129 / 113, 250 / 217.
+// f32 96 x 384 67 / 106, 129 / 113, 250 / 217.  At 300 k x 128 x 512 f16 256 us, 770 TFLOP/s: like the forward pass, bound by the weights' way out of LDS
+// (a wave's fragment feeds one product) and the products themselves.
 template <typename T, int CT> constexpr bool kDxMany = sizeof(T) * CT <= 16;              // LDS has room for two slices' weights
 template <typename T, int CT> constexpr bool kDxFew = sizeof(T) == 4 || CT <= 4;
 template <typename T, int CT> constexpr int64_t kDxFewRows = !kDxFew<T, CT> ? 0 : sizeof(T) * CT < 8 ? 16384 : 32768;
@@ -184,8 +185,11 @@ __device__ __forceinline__ void turned(const emc2_row<T, CT, WIDE>& rows, int fi
 
 // Partial sums [part][slice][3][C / 32][64 lanes][16]: of a tile of dWg, dWu (rows: channels, columns: hidden units) and of dWd (rows: hidden
 // units, columns: channels), the CB tiles of channels from C0 on.  A block has one slice, whose weights lie in LDS, and one part of the rows, which
-// its four waves share out; the next tile of rows is on its way while one is worked on.
-// Waves a SIMD: two without the next tile's rows where the sums are few.
+// its four waves share out.  16-bit values: 100 k x 64 x 256 in 40 us, 300 k x 128 x 512 in 510: 490 and 460 TFLOP/s without
+// the turning.  For every 32 products at 64 channels there are 200 plain and 32 slow vector instructions of activation, slopes and roundings.  Measured and
+// not better: the next tile's rows on their way during the activation (within 4 %, or no registers for it), the turning spread over the
+// activation (up to 9 % slower), a part's slices on one XCD (up to 10 % slower).
+// Waves a SIMD: two where the sums are few.
 template <typename T, int CT> constexpr int kDwWaves = sizeof(T) * CT <= 4 ? 2 : 1;   // (parts_of counts on it)
 template <typename T, int CT, bool GELU, bool WIDE, int C0, int CB>
 __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const emc2_ffn_args a) {
@@ -193,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
   typedef typename M::frag frag;
   constexpr int KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep, kWaves = kThreads / 64;
   constexpr int kWavesASimd = kDwWaves<T, CT>;
-  constexpr bool kExact = sizeof(T) == 4, kAhead = false;
+  constexpr bool kExact = sizeof(T) == 4;
   __shared__ frag w[3 * KK * 64];
   __shared__ emc2_fvec<4> meet[kWaves][4][64];
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
@@ -213,12 +217,11 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
 #pragma unroll
   for (int c = 0; c < CB; ++c) dwg[c] = 0.0f, dwu[c] = 0.0f, dwd[c] = 0.0f;
   const int32_t step = a.parts * kWaves;
-  const auto read = [&](int64_t tile, emc2_row<T, CT, WIDE>& x, emc2_row<T, CT, WIDE>& dy) {
+  for (int64_t tile = (int64_t)part * kWaves + wave; tile * 32 < n; tile += step) {
     const int64_t row = tile * 32 + (lane & 31);
+    emc2_row<T, CT, WIDE> x, dy;
     x.set(a.x, a.ld_x, row, n, a.channels, half);
     dy.set(a.dy, a.ld_dy, row, n, a.channels, half);
-  };
-  const auto work = [&](const emc2_row<T, CT, WIDE>& x, const emc2_row<T, CT, WIDE>& dy) {
     int at = lane;
     asm volatile("" : "+v"(at));                           // the weights are read from LDS each time: registers have no room for them
     emc2_acc g = 0.0f, u = 0.0f, dh = 0.0f;
@@ -253,26 +256,6 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
         else dwg[c] = emc2_mma<T>(t[0][m], dg[m], dwg[c]), dwu[c] = emc2_mma<T>(t[0][m], du[m], dwu[c]);
       }
       if constexpr (kWavesASimd == 1) __builtin_amdgcn_sched_barrier(0);   // no further ahead: registers
-    }
-  };
-  int64_t tile = (int64_t)part * kWaves + wave;
-  if constexpr (kAhead) {
-    emc2_row<T, CT, WIDE> x[2], dy[2];
-    if (tile * 32 < n) read(tile, x[0], dy[0]);
-    while (tile * 32 < n) {
-      read(tile + step, x[1], dy[1]);                      // (nothing is read beyond the rows)
-      work(x[0], dy[0]);
-      tile += step;
-      if (tile * 32 >= n) break;
-      read(tile + step, x[0], dy[0]);
-      work(x[1], dy[1]);
-      tile += step;
-    }
-  } else {
-    for (; tile * 32 < n; tile += step) {
-      emc2_row<T, CT, WIDE> x, dy;
-      read(tile, x, dy);
-      work(x, dy);
     }
   }
   emc2_fvec<4>* out = (emc2_fvec<4>*)a.partial + ((int64_t)part * a.slices + s) * 3 * CT * 256;
