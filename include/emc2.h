@@ -486,7 +486,8 @@ emc2_status emc2_project_gather(emc2_ctx* ctx, const float* d_points, int32_t st
  *   - d_work: caller's scratch, 16-byte aligned, of at least emc2_*_work bytes; its contents need not be kept between calls.  The calls touch
  *     no mutable context state but the status word and may run on several streams at once, each with a d_work of its own.
  *   - Results do not depend on the run: no sum is taken in an order that may change.
- * The *_work and *_size calls are host-only queries; -1 for arguments that the call itself would refuse.
+ * The *_work and *_size calls are host-only queries; -1 for arguments that the call itself would refuse.  A *_work of more rows is never
+ * less: scratch for the largest call serves the smaller ones.
  */
 
 /* First row of every frame: d_offsets[b] = number of rows of d_coords [capacity][4] (b, z, y, x), sorted by b as every voxel list here is, whose

@@ -317,16 +317,23 @@ __global__ void __launch_bounds__(kThreads) k_ffn_sum(const float4* __restrict__
 // Parts that the rows are cut into.  The chip holds kDwWaves blocks a CU; a launch takes as many rounds of them as it needs, each as long as a
 // wave's tiles of rows and about one tile's time for the weights and the sums.  The best of one to three rounds, then the fewest parts with as many
 // tiles a wave.  us, k_ffn_dw with four blocks more than two rounds / this: 32000 x 96 x 384 f32 250 / 173, f16 58 / 38.
+constexpr int64_t kMostRounds = 3;
+int64_t room_of(emc2_dtype dtype, int32_t channels) { return 256 * (emc2_size_of(dtype) * emc2_ffn_tiles(channels) <= 4 ? 2 : 1); }
 int32_t parts_of(emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t hidden) {
-  const int64_t slices = (hidden + 31) / 32, tiles = emc2_div_up(capacity, 32), waves = kThreads / 64;
-  const int64_t room = 256 * (emc2_size_of(dtype) * emc2_ffn_tiles(channels) <= 4 ? 2 : 1);
+  const int64_t slices = (hidden + 31) / 32, tiles = emc2_div_up(capacity, 32), waves = kThreads / 64, room = room_of(dtype, channels);
   int64_t best = 1, cost = INT64_MAX;
-  for (int64_t rounds = 1; rounds <= 3; ++rounds) {
+  for (int64_t rounds = 1; rounds <= kMostRounds; ++rounds) {
     const int64_t most = room * rounds / slices, turns = emc2_div_up(tiles, waves * (most ? most : 1));
     const int64_t parts = turns ? emc2_div_up(tiles, waves * turns) : 1, c = emc2_div_up(parts * slices, room) * (turns + 1);
     if (c < cost) best = parts, cost = c;
   }
   return (int32_t)best;
+}
+// As many parts as a call of up to that many rows may have: more rows may well have fewer parts, and a buffer for them has to serve both.
+int64_t most_parts(emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t hidden) {
+  const int64_t room = kMostRounds * room_of(dtype, channels) / ((hidden + 31) / 32), blocks = emc2_div_up(emc2_div_up(capacity, 32), kThreads / 64);
+  const int64_t parts = room < blocks ? room : blocks;
+  return parts < 1 ? 1 : parts;
 }
 
 }  // namespace
@@ -335,7 +342,7 @@ extern "C" int64_t emc2_ffn_work(emc2_dtype dtype, int64_t capacity, int32_t cha
   if (!emc2_is_float(dtype) || channels < 1 || channels > kFfnMaxChannels || hidden < 1 || hidden > kFfnMaxHidden || capacity < 0 ||
       capacity > (1ll << 30))
     return -1;
-  return (int64_t)parts_of(dtype, capacity, channels, hidden) * 3 * 32 * emc2_ffn_tiles(channels) * 32 * ((hidden + 31) / 32) * (int64_t)sizeof(float);
+  return most_parts(dtype, capacity, channels, hidden) * 3 * 32 * emc2_ffn_tiles(channels) * 32 * ((hidden + 31) / 32) * (int64_t)sizeof(float);
 }
 
 extern "C" emc2_status emc2_ffn_backward(emc2_ctx* ctx, emc2_dtype dtype, int32_t activation, const void* d_x, int64_t ld_x,

@@ -663,7 +663,7 @@ struct Plan {
   int n, lane_shift, slices;
   int32_t tiles, blocks, width;
   bool totals;                       // a first launch is needed
-  int64_t bytes;
+  int64_t bytes, most;               // of scratch: what the call takes, and what no call of up to that many rows takes more than
 };
 Plan plan_of(emc2_dtype dtype, int64_t capacity, int32_t channels, bool grad) {
   Plan p = {};
@@ -685,7 +685,11 @@ Plan plan_of(emc2_dtype dtype, int64_t capacity, int32_t channels, bool grad) {
   p.tiles = (int32_t)(per < kMaxTiles ? per : kMaxTiles);
   p.blocks = (int32_t)emc2_div_up(tiles, p.tiles);
   p.totals = true;
-  p.bytes = (int64_t)p.blocks * p.width * (int64_t)sizeof(float2) * (grad ? 2 + p.tiles : 1 + kWavesForward);
+  const int64_t line = p.width * (int64_t)sizeof(float2);
+  p.bytes = p.blocks * line * (grad ? 2 + p.tiles : 1 + kWavesForward);
+  // blocks may become fewer as rows become more; what bounds them does not
+  const int64_t some = tiles < aim ? tiles : aim, full = emc2_div_up(tiles, kMaxTiles), blocks = some > full ? some : full;
+  p.most = line * (grad ? 2 * blocks + tiles + p.tiles - 1 : (1 + kWavesForward) * blocks);
   return p;
 }
 
@@ -740,7 +744,7 @@ extern "C" emc2_status emc2_frame_offsets(emc2_ctx* ctx, const int32_t* d_coords
 
 extern "C" int64_t emc2_recurrence_work(emc2_dtype dtype, int64_t capacity, int32_t channels) {
   if (!emc2_is_float(dtype) || channels < 1 || channels > (1 << 16) || capacity < 0 || capacity > (1ll << 30)) return -1;
-  const int64_t forward = plan_of(dtype, capacity, channels, false).bytes, grad = plan_of(dtype, capacity, channels, true).bytes;
+  const int64_t forward = plan_of(dtype, capacity, channels, false).most, grad = plan_of(dtype, capacity, channels, true).most;
   return forward > grad ? forward : grad;
 }
 

@@ -399,6 +399,29 @@ def test_equal_inputs_give_equal_bits_on_other_streams(ctx):
         assert all(torch.equal(p, q) for p, q in zip(first, o))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scratch_of_the_largest_call_serves_the_smaller_ones(ctx, dtype):
+    c, f, cap = 40, 200, 60000
+    x, gate, dy = (_draw(i, cap, c, dtype=dtype).cuda() for i in range(3))
+    gamma, w = torch.ones(c).cuda(), [t.cuda() for t in _weights(c, f, dtype)]
+    packed = torch.empty(ctx.ffn_packed_size(DT[dtype], c, f), dtype=TD[dtype], device="cuda")
+    ctx.ffn_pack(DT[dtype], *w, packed)
+
+    def run(n, work):
+        x_, gate_, dy_, off = x[:n], gate[:n], dy[:n], torch.tensor([0, n // 3, n], dtype=torch.int32, device="cuda")
+        o = [torch.empty_like(x_) for _ in range(5)] + [torch.empty_like(t) for t in w] + [torch.empty_like(gamma) for _ in range(2)]
+        ctx.recurrence(DT[dtype], x_, gate_, off, o[0], work(ctx.recurrence_work))
+        ctx.recurrence_backward(DT[dtype], x_, gate_, off, dy_, o[1], o[2], work(ctx.recurrence_work))
+        ctx.ffn_backward(DT[dtype], B.ACT_SILU, x_, packed, f, dy_, o[3], *o[5:8], work(ctx.ffn_work, f))
+        ctx.layernorm_backward(DT[dtype], x_, gamma, 1e-5, dy_, o[4], o[8], o[9], work(ctx.layernorm_work))
+        return o
+
+    for n in (cap - 1, 33000, 16385, 8193, 700, 1):
+        large = run(n, lambda query, *hidden: _work(query(DT[dtype], cap, c, *hidden)))
+        own = run(n, lambda query, *hidden: _work(query(DT[dtype], n, c, *hidden)))
+        assert all(torch.equal(p, q) for p, q in zip(large, own)), n
+
+
 def test_frame_offsets(ctx):
     for lens in ([5, 0, 3], [0], [0, 0, 4000, 1, 0], [1] * 700):
         ids = np.repeat(np.arange(len(lens)), lens)
