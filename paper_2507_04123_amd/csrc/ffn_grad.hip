@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
 }
 
 // Adds the parts, four values a thread, and puts them where they belong.  Eight threads share a sum's parts out (500 parts of 32 x 128 values:
-// 9.0 us by one thread, 5.3 by eight) and meet in LDS, always in the same order.
+// 9.0 us by one thread, 5.3 by eight; 61 parts of 64 x 256 values with their loads in a row 5.5, together 5.0) and meet in LDS, always in the same order.
 constexpr int kSumThreads = 8;
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_ffn_sum(const float4* __restrict__ partial, int32_t parts, int32_t slices, int32_t tiles,
@@ -285,10 +285,13 @@ __global__ void __launch_bounds__(kThreads) k_ffn_sum(const float4* __restrict__
   const int64_t quads = (int64_t)slices * 3 * tiles * 64 * 4, at = (int64_t)blockIdx.x * kSums + threadIdx.x % kSums;
   const int mine = threadIdx.x / kSums;
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);              // (768 sums a tile and slice: no block has fewer than kSums)
-#pragma unroll 8
-  for (int32_t p = mine; p < parts; p += kSumThreads) {
-    const float4 q = partial[p * quads + at];
-    s.x += q.x, s.y += q.y, s.z += q.z, s.w += q.w;
+  for (int32_t p = mine; p < parts; p += kSumThreads * 8) {    // eight loads under way, beyond the last part of the last one again
+    float4 q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = partial[min(p + kSumThreads * i, parts - 1) * quads + at];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (p + kSumThreads * i < parts) s.x += q[i].x, s.y += q[i].y, s.z += q[i].z, s.w += q[i].w;
   }
   meet[mine][threadIdx.x % kSums] = s;
   __syncthreads();

@@ -190,15 +190,21 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 5 : 2) k_layernorm_grad(con
     }
 }
 
-// dgamma and dbeta from the blocks' sums: 32 columns a block, 32 threads a column.
+// dgamma and dbeta from the blocks' sums: 32 columns a block, 32 threads a column, each with eight loads under way (beyond the last sum: of the last one
+// again, not counted; 1251 sums of 180 columns 5.7 us, 6.2 with the last ones loaded in a row).
 __global__ void __launch_bounds__(1024) k_layernorm_weights(const float* __restrict__ partial, int32_t blocks, int32_t channels,
                                                             float* __restrict__ dgamma, float* __restrict__ dbeta) {
   __shared__ float part[32][33];
   const int col = blockIdx.x * 32 + (threadIdx.x & 31), seg = threadIdx.x >> 5;
   float s = 0.0f;
   if (col < 2 * channels) {
-#pragma unroll 8
-    for (int b = seg; b < blocks; b += 32) s += partial[(int64_t)b * 2 * channels + col];
+    for (int b = seg; b < blocks; b += 32 * 8) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = partial[(int64_t)min(b + 32 * i, blocks - 1) * 2 * channels + col];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += b + 32 * i < blocks ? v[i] : 0.0f;
+    }
   }
   part[seg][threadIdx.x & 31] = s;
   __syncthreads();
