@@ -519,7 +519,8 @@ emc2_status emc2_layernorm_backward(emc2_ctx* ctx, emc2_dtype dtype, const void*
  * rows beyond are then left out).  backwards != 0: every sequence is walked from its last row to its first.
  *   d_h0 [n_seq][channels] states before the first row, NULL = zeros; d_last [n_seq][channels] receives the states after the last
  *   (an empty sequence's is its d_h0), NULL to skip.  d_last must not overlap d_h0 (nor d_dh0 d_dlast below).
- * The states are fp32 throughout; what an infinity or NaN in x or gate makes of a sequence stays within it and its channel.
+ * The states are fp32 throughout; an infinity or NaN in x, gate or a state stays in the state to the end of its sequence (through gates that are
+ * shut, too: 0 times it is NaN) and reaches no other sequence or channel.  So do those of dy and d_dlast in the gradients, the other way.
  */
 int64_t emc2_recurrence_work(emc2_dtype dtype, int64_t capacity, int32_t channels);
 emc2_status emc2_recurrence(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate,

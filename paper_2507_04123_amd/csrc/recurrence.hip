@@ -5,12 +5,13 @@
 // Row t maps the state h -> A h + B, and maps compose: any run of rows is one such pair per channel, so a long sequence is cut into
 // blocks of rows that are worked on side by side.  A first launch reduces every block to its pair (k_recurrence_totals), the second
 // composes the pairs of the blocks before its own into the state that enters it and then walks its rows (k_recurrence).  A sequence's
-// first row begins a new map (A = 0, B = the given state), so sequences of any length share a block and none is padded.
+// first row begins a new map (A = -0, B = the given state), so sequences of any length share a block and none is padded.
 // The gradients' u runs the other way with the same factors: the first launch reduces both directions at once, the second walks a block's
 // tiles from the last to the first, with the state that enters every tile known from the first launch.
 // A thread holds R consecutive rows of N neighbouring channels in registers; maps are composed over a wave's
 // row groups by shuffles, over waves through LDS.  The order of composition is fixed: equal inputs give equal bits.  Maps and states are fp32.
-// A map with A = 0 drops what lies before it, whatever that holds: an infinity or NaN in one sequence never reaches another one.
+// The map that begins a sequence drops what lies before it, whatever that holds: an infinity or NaN in one sequence never reaches another one.
+// Its factor is -0, which no product of gates is: within a sequence a NaN or infinity travels on to the end, also where the gates' product is 0.
 // Bound by memory, and close behind by the logistic function's two slow instructions an element.  Rows are read by both launches: 613 k x 64 f16 in
 // eight sequences 98 us, 4.0 TB/s of both launches' bytes (the second finds much of its input in the last cache); 150 k x 96 fp32 in 9001 sequences 88 us,
 // 3.3 TB/s; forward pass and gradients of 200 k x 128 bf16 173 us, 3.8 TB/s.
@@ -123,7 +124,9 @@ __device__ __forceinline__ bool mark(const Args& a, int32_t n, int32_t row0, int
 
 // A map h -> A h + B of N channels, and what it makes of a state.
 template <int N> struct Map { emc2_fvec<N> A, B; };
-__device__ __forceinline__ float apply(float A, float B, float h) { return A == 0.0f ? B : __builtin_fmaf(A, h, B); }
+constexpr float kBegins = -0.0f;     // A of a map that drops the state before it; gates are >= +0, and so are their products
+__device__ __forceinline__ bool begins(float A) { return __float_as_uint(A) == 0x80000000u; }
+__device__ __forceinline__ float apply(float A, float B, float h) { return begins(A) ? B : __builtin_fmaf(A, h, B); }
 template <int N> __device__ __forceinline__ emc2_fvec<N> apply(const Map<N>& m, emc2_fvec<N> h) {
 #pragma unroll
   for (int e = 0; e < N; ++e) h[e] = apply(m.A[e], m.B[e], h[e]);
@@ -131,7 +134,7 @@ template <int N> __device__ __forceinline__ emc2_fvec<N> apply(const Map<N>& m, 
 }
 // `second` after `first`.  A second map that drops the state stays one, even if the first one's factor is NaN.
 __device__ __forceinline__ float2 then(float2 first, float2 second) {
-  return make_float2(second.x == 0.0f ? 0.0f : first.x * second.x, apply(second.x, second.y, first.y));
+  return make_float2(begins(second.x) ? kBegins : first.x * second.x, apply(second.x, second.y, first.y));
 }
 template <int N> __device__ __forceinline__ Map<N> then(const Map<N>& first, const Map<N>& second) {
   Map<N> m;
@@ -225,7 +228,7 @@ __device__ __forceinline__ Map<N> run_forward(const Args& a, const emc2_fvec<N> 
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int32_t s = starts[i];
-      if (s >= 0) m = {emc2_fvec<N>(0.0f), state_or_zero<N>(a.h0, a, s, t)};
+      if (s >= 0) m = {emc2_fvec<N>(kBegins), state_or_zero<N>(a.h0, a, s, t)};
       m.A *= keep[i], m.B = keep[i] * m.B + add[i];
     }
   }
@@ -240,7 +243,7 @@ __device__ __forceinline__ Map<N> run_backward(const Args& a, const emc2_fvec<N>
   for (int i = R - 1; i >= 0; --i) {
     if (marked) {
       const int32_t s = ends[i];
-      if (s >= 0) m = {emc2_fvec<N>(0.0f), state_or_zero<N>(a.dlast, a, s, t)};
+      if (s >= 0) m = {emc2_fvec<N>(kBegins), state_or_zero<N>(a.dlast, a, s, t)};
     }
     m.A *= keep[i], m.B = keep[i] * (dy[i] + m.B);
   }
