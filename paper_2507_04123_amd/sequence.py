@@ -86,9 +86,11 @@ class SequenceBlock:
         return dx
 
     def step(self, x: torch.Tensor, h: torch.Tensor) -> torch.Tensor:
-        """One new row per frame, x [frames][channels]: the frames' states h (fp32) move on in place; returns y."""
+        """One new row per frame, x [frames][channels]: the frames' states h (fp32) move on in place; returns y (where run()'s lies).  What a
+        backward() still to come reads of the last run() is left as it is: a training block's step works in that pass's own buffers."""
         ctx, p, k = self.ctx, self.params, x.shape[0]
-        u, v, gate, y = self.u[:k], self.v[:k], self.gate[:k], self.y[:k]
+        u, v, gate = (self.u, self.v, self.gate) if self.grads is None else (self.du, self.dv, self.dgate)
+        u, v, gate, y = u[:k], v[:k], gate[:k], self.y[:k]
         ctx.layernorm(self.dtype, x, p["gamma"], p["beta"], _EPS, u)
         ctx.ffn(self.dtype, self.activation, u, self.packed, self.hidden, v, residual=x)
         ctx.layernorm(self.dtype, x, p["gate_gamma"], p["gate_beta"], _EPS, gate)
