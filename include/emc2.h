@@ -482,7 +482,8 @@ emc2_status emc2_project_gather(emc2_ctx* ctx, const float* d_points, int32_t st
  *     element.  Any length and pitch moves in pieces of up to 16 bytes; rows that begin at multiples of 16 bytes are fastest.
  *   - `d_n` (device int32, or NULL): rows present, of `capacity` at most; rows beyond are neither read nor written.
  *   - Parameters and states of float* are fp32 whatever the rows' type; sums are fp32; each result is rounded once, to nearest even.
- *   - Results may lie where inputs of the same call do, if pointer and pitch are the same; otherwise they must not overlap.
+ *   - Results may lie where inputs of the same call do, if pointer and pitch are the same; otherwise they must not overlap.  (The states of
+ *     emc2_recurrence and their gradients: see there.)
  *   - d_work: caller's scratch, 16-byte aligned, of at least emc2_*_work bytes; its contents need not be kept between calls.  The calls touch
  *     no mutable context state but the status word and may run on several streams at once, each with a d_work of its own.
  *   - Results do not depend on the run: no sum is taken in an order that may change.
@@ -518,7 +519,7 @@ emc2_status emc2_layernorm_backward(emc2_ctx* ctx, emc2_dtype dtype, const void*
  * may be empty.  d_offsets[n_seq] is the number of rows, of `capacity` at most (EMC2_ERR_CAPACITY through the status word if it is more; the
  * rows beyond are then left out).  backwards != 0: every sequence is walked from its last row to its first.
  *   d_h0 [n_seq][channels] states before the first row, NULL = zeros; d_last [n_seq][channels] receives the states after the last
- *   (an empty sequence's is its d_h0), NULL to skip.  d_last must not overlap d_h0 (nor d_dh0 d_dlast below).
+ *   (an empty sequence's is its d_h0), NULL to skip.  d_last must not overlap d_h0 (nor d_dh0 d_dlast below): such calls are refused.
  * The states are fp32 throughout; an infinity or NaN in x, gate or a state stays in the state to the end of its sequence (through gates that are
  * shut, too: 0 times it is NaN) and reaches no other sequence or channel.  So do those of dy and d_dlast in the gradients, the other way.
  */

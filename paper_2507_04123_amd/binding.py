@@ -729,7 +729,8 @@ class Context:
 
     def recurrence(self, dtype: int, x: torch.Tensor, gate: torch.Tensor, offsets: torch.Tensor, y: torch.Tensor, work: torch.Tensor,
                    backwards: bool = False, h0: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None) -> None:
-        """y_t = h_t = a_t h_{t-1} + (1 - a_t) x_t along every sequence, a = sigmoid(gate); offsets [sequences + 1] device int32."""
+        """y_t = h_t = a_t h_{t-1} + (1 - a_t) x_t along every sequence, a = sigmoid(gate); offsets [sequences + 1] device int32.
+        `last` must not overlap h0."""
         like, rows, c = _rows_of(x, dtype)
         ld = _pitch(x, like, "x"), _pitch(gate, like, "gate"), _pitch(y, like, "y")
         _dev_check(offsets, torch.int32, "offsets")
@@ -743,7 +744,7 @@ class Context:
     def recurrence_backward(self, dtype: int, x: torch.Tensor, gate: torch.Tensor, offsets: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor,
                             dgate: torch.Tensor, work: torch.Tensor, backwards: bool = False, h0: Optional[torch.Tensor] = None,
                             dlast: Optional[torch.Tensor] = None, dh0: Optional[torch.Tensor] = None) -> None:
-        """dx, dgate and dh0 of a recurrence over x and gate, for dy and the gradient of the last states."""
+        """dx, dgate and dh0 of a recurrence over x and gate, for dy and the gradient of the last states; dh0 must not overlap dlast."""
         like, rows, c = _rows_of(x, dtype)
         ld = _pitch(x, like, "x"), _pitch(gate, like, "gate"), _pitch(dy, like, "dy"), _pitch(dx, like, "dx"), _pitch(dgate, like, "dgate")
         _dev_check(offsets, torch.int32, "offsets")

@@ -730,6 +730,11 @@ emc2_status check(emc2_ctx* ctx, const char* what, emc2_dtype dtype, int64_t cap
   return EMC2_OK;
 }
 bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// States [n_seq][channels] of both lie apart: one sequence's are read by some waves while others write another's.
+bool apart(const float* p, const float* q, int32_t n_seq, int32_t channels) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q, size = (uintptr_t)n_seq * channels * sizeof(float);
+  return !p || !q || a + size <= b || b + size <= a;
+}
 
 }  // namespace
 
@@ -763,6 +768,7 @@ extern "C" emc2_status emc2_recurrence(emc2_ctx* ctx, emc2_dtype dtype, const vo
   if (!emc2_rows_ok(d_x, ld_x, channels, size, none) || !emc2_rows_ok(d_gate, ld_gate, channels, size, none) ||
       !emc2_rows_ok(d_y, ld_y, channels, size, none))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence: null or misaligned rows, or a pitch below the channels");
+  if (!apart(d_h0, d_last, n_seq, channels)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence: d_last must not overlap d_h0");
   const Plan p = plan_of(dtype, capacity, channels, false);
   if (work_bytes < p.bytes || (p.bytes && (!d_work || !aligned(d_work))))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence: work buffer null, misaligned or smaller than emc2_recurrence_work");
@@ -795,6 +801,8 @@ extern "C" emc2_status emc2_recurrence_backward(emc2_ctx* ctx, emc2_dtype dtype,
       !emc2_rows_ok(d_dy, ld_dy, channels, size, none) || !emc2_rows_ok(d_dx, ld_dx, channels, size, none) ||
       !emc2_rows_ok(d_dgate, ld_dgate, channels, size, none))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_backward: null or misaligned rows, or a pitch below the channels");
+  if (!apart(d_dlast, d_dh0, n_seq, channels))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_backward: d_dh0 must not overlap d_dlast");
   const Plan p = plan_of(dtype, capacity, channels, true);
   if (work_bytes < p.bytes || (p.bytes && (!d_work || !aligned(d_work))))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_backward: work buffer null, misaligned or smaller than emc2_recurrence_work");

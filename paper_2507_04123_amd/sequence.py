@@ -61,7 +61,8 @@ class SequenceBlock:
         return self.offsets
 
     def run(self, x: torch.Tensor, offsets: torch.Tensor, h0: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """x [rows][channels] of packed frames -> y of as many rows; the states behind each frame's last voxel go to self.last."""
+        """x [rows][channels] of packed frames -> y of as many rows; the states behind each frame's last voxel go to self.last (of which h0, to go
+        on from there, has to be a copy)."""
         ctx, p, n, k = self.ctx, self.params, offsets[-1:], x.shape[0]
         u, v, gate, y = self.u[:k], self.v[:k], self.gate[:k], self.y[:k]
         ctx.layernorm(self.dtype, x, p["gamma"], p["beta"], _EPS, u, n=n)
