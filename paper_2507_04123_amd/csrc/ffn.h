@@ -93,13 +93,14 @@ template <typename T, int CT, bool WIDE> struct emc2_row {
 };
 
 // act(g) of either activation as g s, s = logistic(z): SiLU z = g, GELU (its tanh form) z = sqrt(8 / pi) (g + 0.044715 g^3); and the slope
-// s + g s (1 - s) dz/dg (1 - s is taken from s here: where nothing is left of it, the slope is s).
+// s + g s (1 - s) dz/dg (1 - s is taken from s here: where nothing is left of it, the slope is s; g^2 is held finite for that).
 template <bool EXACT, bool GELU> __device__ __forceinline__ float emc2_activate(float g) {
   return g * emc2_logistic<EXACT>(GELU ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g);
 }
 template <bool EXACT, bool GELU> __device__ __forceinline__ float emc2_activate(float g, float& slope) {
-  const float s = emc2_logistic<EXACT>(GELU ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g), a = g * s;
-  const float rest = GELU ? (1.0f - s) * (1.5957691216057308f + 0.2140644488f * g * g) : 1.0f - s;
+  const float sq = GELU ? __builtin_fminf(g * g, 1e30f) : 0.0f;
+  const float s = emc2_logistic<EXACT>(GELU ? g * __builtin_fmaf(sq, 0.0713548163f, 1.5957691216057308f) : g), a = g * s;
+  const float rest = GELU ? (1.0f - s) * __builtin_fmaf(sq, 0.2140644488f, 1.5957691216057308f) : 1.0f - s;
   slope = __builtin_fmaf(a, rest, s);
   return a;
 }
