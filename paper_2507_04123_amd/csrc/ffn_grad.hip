@@ -4,7 +4,7 @@
 // and dU would move six times n F values.
 // k_ffn_dx works like the forward pass: hidden units along the lanes' registers, rows along the lanes.
 // k_ffn_dw has them the other way round (rows along the registers), which is what a contraction over rows takes: dG, dU and H are its operands as
-// they are.  x and dy have to be turned round for it: a product with the identity does that on the matrix cores, exactly.  Each block sums
+// they are.  x and dy have to be turned round for it: a product with the identity does that on the matrix cores, exactly (of finite values).  Each block sums
 // its slice of 32 hidden units over a part of the rows; the parts are added by k_ffn_sum in a fixed order (fp32, no atomics).
 #include "ffn.h"
 
@@ -259,11 +259,10 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
     }
   }
   emc2_fvec<4>* out = (emc2_fvec<4>*)a.partial + ((int64_t)part * a.slices + s) * 3 * CT * 256;
-#pragma unroll
-  for (int which = 0; which < 3; ++which)
+  const auto put = [&](int which, const emc2_acc (&sums)[CB]) {
 #pragma unroll
     for (int c = 0; c < CB; ++c) {
-      const emc2_acc& t = which == 0 ? dwg[c] : which == 1 ? dwu[c] : dwd[c];
+      const emc2_acc& t = sums[c];
       if (which + c) __syncthreads();
 #pragma unroll
       for (int j = 0; j < 4; ++j) meet[wave][j][lane] = emc2_fvec<4>{t[4 * j], t[4 * j + 1], t[4 * j + 2], t[4 * j + 3]};
@@ -271,6 +270,56 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
       // registers 4 wave .. 4 wave + 3 of every lane
       out[((which * CT + C0 + c) * 64 + lane) * 4 + wave] = meet[0][wave][lane] + meet[1][wave][lane] + meet[2][wave][lane] + meet[3][wave][lane];
     }
+  };
+  put(0, dwg);
+  put(1, dwu);
+  // A value of dy that is not finite makes its turned row NaN, 0 times it being that, in all columns of the tile: then the wave sums dWd once more,
+  // with dy's values read one by one where they belong.  (One of x leaves no gradient of its row finite in any column.)  Here, where the
+  // other sums' registers are free, it costs the loop above none.
+  bool nan = false;
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) nan |= dwd[c][r] != dwd[c][r];
+  if (__any(nan)) {
+#pragma unroll
+    for (int c = 0; c < CB; ++c) dwd[c] = 0.0f;
+    for (int64_t tile = (int64_t)part * kWaves + wave; tile * 32 < n; tile += step) {
+      // channels and rows that are not there take the last one's values: they meet weights and hidden values of 0, or are not kept
+      const int64_t row = tile * 32 + (lane & 31), most = n - 1;
+      const T* x = (const T*)a.x + min(row, most) * a.ld_x;
+      int at = lane, channel = half * M::kPer;
+      asm volatile("" : "+v"(at), "+v"(channel));
+      emc2_acc g = 0.0f, u = 0.0f;
+#pragma unroll
+      for (int k = 0; k < KK; ++k) {
+        frag v;
+#pragma unroll
+        for (int e = 0; e < M::kPer; ++e) v[e] = x[min(channel + k * M::kDeep + e, a.channels - 1)];
+        if (row > most) v = emc2_zero_frag<T>();
+        g = emc2_mma<T>(v, w[k * 64 + at], g);
+        u = emc2_mma<T>(v, w[(KK + k) * 64 + at], u);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      frag h[MM];
+#pragma unroll
+      for (int r = 0; r < 16; r += 2)
+        emc2_put_pair<T>(h, r, emc2_activate<kExact, GELU>(g[r]) * u[r], emc2_activate<kExact, GELU>(g[r + 1]) * u[r + 1]);
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        const T* dy = (const T*)a.dy + min(32 * (C0 + c) + (at & 31), a.channels - 1);
+#pragma unroll
+        for (int m = 0; m < MM; ++m) {
+          frag t;
+#pragma unroll
+          for (int e = 0; e < M::kPer; ++e) t[e] = dy[min(tile * 32 + emc2_hidden_of<T>(m, half, e), most) * a.ld_dy];
+          dwd[c] = emc2_mma<T>(h[m], t, dwd[c]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+  }
+  put(2, dwd);
 }
 
 // Adds the parts, four values a thread, and puts them where they belong.  Eight threads share a sum's parts out (500 parts of 32 x 128 values:
