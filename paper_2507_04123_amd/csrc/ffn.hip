@@ -147,8 +147,8 @@ __global__ void __launch_bounds__((64 * kFewWaves<CT, WIDE>)) k_ffn_few(const em
   __shared__ emc2_fvec<4> part[kWaves][4][64];
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if ((int64_t)blockIdx.x * 32 >= n) return;
-  const int64_t row = (int64_t)blockIdx.x * 32 + (lane & 31);
+  if (emc2_block() * 32 >= n) return;
+  const int64_t row = emc2_block() * 32 + (lane & 31);
   emc2_row<T, CT, WIDE> x;
   x.set(a.x, a.ld_x, row, n, a.channels, half);
   emc2_acc y[CT];
@@ -280,7 +280,7 @@ extern "C" emc2_status emc2_ffn(emc2_ctx* ctx, emc2_dtype dtype, int32_t activat
     // fp32 rows of over 64 channels would leave a SIMD one wave of k_ffn: 155 / 142 us for 64 k x 96 x 384, but 79 / 72 and 42 / 67 for 32 k and 16 k
     constexpr bool kFew = sizeof(T) * CT > 8 && sizeof(T) == 4;
     if (kFew || capacity <= kFewRows)
-      hipLaunchKernelGGL((k_ffn_few<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32)), dim3(64 * kFewWaves<CT, P>), 0, (hipStream_t)stream, a);
+      hipLaunchKernelGGL((k_ffn_few<T, CT, G, P>), emc2_grid(emc2_div_up(capacity, 32)), dim3(64 * kFewWaves<CT, P>), 0, (hipStream_t)stream, a);
     else if constexpr (!kFew)
       hipLaunchKernelGGL((k_ffn<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32 * kManyWaves)), dim3(64 * kManyWaves), 0, (hipStream_t)stream, a);
   });

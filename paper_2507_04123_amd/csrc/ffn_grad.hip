@@ -124,8 +124,8 @@ __global__ void __launch_bounds__((64 * kDxWaves<T, CT>)) k_ffn_dx(const emc2_ff
   __shared__ emc2_fvec<4> part[kWaves][4][64];
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if ((int64_t)blockIdx.x * 32 >= n) return;
-  const int64_t row = (int64_t)blockIdx.x * 32 + (lane & 31);
+  if (emc2_block() * 32 >= n) return;
+  const int64_t row = emc2_block() * 32 + (lane & 31);
   emc2_row<T, CT, WIDE> x, dy;
   x.set(a.x, a.ld_x, row, n, a.channels, half);
   dy.set(a.dy, a.ld_dy, row, n, a.channels, half);
@@ -435,7 +435,7 @@ extern "C" emc2_status emc2_ffn_backward(emc2_ctx* ctx, emc2_dtype dtype, int32_
     }
     if constexpr (kDxFew<T, CT>) {
       if (!none && !(kDxMany<T, CT> && capacity > kDxFewRows<T, CT>))
-        hipLaunchKernelGGL((k_ffn_dx<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32)), dim3(64 * kDxWaves<T, CT>), 0, s, a);
+        hipLaunchKernelGGL((k_ffn_dx<T, CT, G, P>), emc2_grid(emc2_div_up(capacity, 32)), dim3(64 * kDxWaves<T, CT>), 0, s, a);
     }
     hipLaunchKernelGGL(k_ffn_sum<T>, dim3((unsigned)((int64_t)a.slices * 3 * CT * 256 / (kThreads / kSumThreads))), dim3(kThreads), 0, s,
                        (const float4*)d_work, a.parts, a.slices, CT, channels, hidden, (T*)d_dwg, (T*)d_dwu, (T*)d_dwd);

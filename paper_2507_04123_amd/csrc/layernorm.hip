@@ -60,8 +60,8 @@ template <typename T, int N, int L, int V, int U, bool MOVED>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) k_layernorm(const NormArgs a) {
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
   constexpr int kGroups = kThreads / L;
-  const int64_t first = (int64_t)blockIdx.x * (kGroups * U) + threadIdx.x / L;
-  if ((int64_t)blockIdx.x * (kGroups * U) >= n) return;
+  const int64_t first = emc2_block() * (kGroups * U) + threadIdx.x / L;
+  if (emc2_block() * (kGroups * U) >= n) return;
   const Places<N, L, V, MOVED> p(a.channels, threadIdx.x % L);
   emc2_fvec<N> x[U][V];
 #pragma unroll
@@ -302,7 +302,7 @@ extern "C" emc2_status emc2_layernorm(emc2_ctx* ctx, emc2_dtype dtype, const voi
     using F = decltype(form);
     using T = decltype(type);
     const int64_t rows = kThreads / F::l * F::u;
-    hipLaunchKernelGGL((k_layernorm<T, F::n, F::l, F::v, F::u, F::moved>), dim3((unsigned)emc2_div_up(capacity, rows)), dim3(kThreads), 0,
+    hipLaunchKernelGGL((k_layernorm<T, F::n, F::l, F::v, F::u, F::moved>), emc2_grid(emc2_div_up(capacity, rows)), dim3(kThreads), 0,
                        (hipStream_t)stream, a);
   });
   return emc2_check_hip(ctx, hipGetLastError(), "emc2_layernorm launch");

@@ -640,7 +640,7 @@ template <typename T, int N>
 __global__ void __launch_bounds__(kStepThreads) k_recurrence_step(const T* x, int64_t ld_x, const T* gate, int64_t ld_gate, const float* h_in,
                                                                   float* h_out, T* y, int64_t ld_y, int64_t rows, int32_t channels) {
   const int32_t pieces = (channels + N - 1) / N;
-  const int64_t i = (int64_t)blockIdx.x * kStepThreads + threadIdx.x;
+  const int64_t i = emc2_block() * kStepThreads + threadIdx.x;
   if (i >= rows * pieces) return;
   const int64_t row = i / pieces;
   const int32_t c = (int32_t)(i - row * pieces) * N;
@@ -837,11 +837,10 @@ extern "C" emc2_status emc2_recurrence_step(emc2_ctx* ctx, emc2_dtype dtype, con
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "emc2_recurrence_step: null or misaligned rows, or a pitch below the channels");
   const int n = channels >= 4 ? 4 : 1;
   const int64_t blocks = emc2_div_up(rows * emc2_div_up(channels, n), kStepThreads);
-  if (blocks > 0x7fffffff) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "emc2_recurrence_step: too many rows for one launch");
   with_type(dtype, n, [&](auto type, auto length) {
     using T = decltype(type);
     constexpr int N = kLength<decltype(length)>;
-    hipLaunchKernelGGL((k_recurrence_step<T, N>), dim3((unsigned)blocks), dim3(kStepThreads), 0, (hipStream_t)stream, (const T*)d_x, ld_x,
+    hipLaunchKernelGGL((k_recurrence_step<T, N>), emc2_grid(blocks), dim3(kStepThreads), 0, (hipStream_t)stream, (const T*)d_x, ld_x,
                        (const T*)d_gate, ld_gate, d_h, d_h_out, (T*)d_y, ld_y, rows, channels);
   });
   return emc2_check_hip(ctx, hipGetLastError(), "emc2_recurrence_step launch");

@@ -27,6 +27,13 @@ __device__ __forceinline__ int32_t emc2_row_count(const int32_t* d_n, int64_t ca
   return n < 0 ? 0 : n < capacity ? n : (int32_t)capacity;
 }
 
+// A launch of as many blocks as a call needs.  An axis of a grid has fewer than 2^32 threads: more than 2^21 blocks lie in lines of 2^21.
+constexpr int64_t kEmc2BlocksALine = 1 << 21;
+static inline dim3 emc2_grid(int64_t blocks) {
+  return blocks <= kEmc2BlocksALine ? dim3((unsigned)blocks) : dim3((unsigned)kEmc2BlocksALine, (unsigned)((blocks + kEmc2BlocksALine - 1) / kEmc2BlocksALine));
+}
+__device__ __forceinline__ int64_t emc2_block() { return blockIdx.y * kEmc2BlocksALine + blockIdx.x; }
+
 // The logistic function s = 1 / (1 + exp(-z)) and 1 - s = exp(-z) / (1 + exp(-z)), each to a few ulp: 1 - s is not taken from s, which
 // would leave nothing of it where s is near 1.  Where exp(-z) is beyond the range s is 0 and 1 - s is 1; NaN passes through.
 // EXACT (32-bit values): the exponent's product with log2(e) is carried to twice the precision, which matters beyond |z| of about 8.
