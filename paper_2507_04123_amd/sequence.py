@@ -52,8 +52,13 @@ class SequenceBlock:
 
     def load(self, params: Dict[str, torch.Tensor]) -> None:
         """Takes the parameters over: the tensors are kept, the weights' fragments made of them.  Call it again when they have changed."""
-        self.params = params
+        c, f = self.channels, self.hidden
+        shapes = {"wg": (c, f), "wu": (c, f), "wd": (f, c), "gamma": (c,), "beta": (c,), "gate_gamma": (c,), "gate_beta": (c,)}
+        got = {k: tuple(params[k].shape) if k in params else None for k in shapes}
+        if got != shapes:
+            raise ValueError(f"load: need parameters of {shapes}, got {got}")
         self.ctx.ffn_pack(self.dtype, params["wg"], params["wu"], params["wd"], self.packed)
+        self.params = params
 
     def find_frames(self, coords: torch.Tensor, n: torch.Tensor, capacity: int) -> torch.Tensor:
         """First row of every frame of a voxel list (its coordinates and device count), into self.offsets."""

@@ -43,3 +43,23 @@ def test_a_step_between_run_and_backward_changes_no_gradient(dtype):
     assert torch.equal(b.step(rows, one), serve.step(rows, two)) and torch.equal(one, two) and not torch.equal(one, h)
     ctx.status_sync()
     ctx.close()
+
+
+def test_parameters_of_other_shapes_are_refused():
+    """The fragments' buffer would take smaller weights, which the block would then read as its own."""
+    ctx = B.Context(1, 1, 1)
+    b = _block(ctx, B.F16, 16, 1, 32, 96)
+    x, offsets = _normal(1, (16, 32), torch.float16), torch.tensor([0, 16], dtype=torch.int32, device="cuda")
+    before = b.run(x, offsets).clone()
+    for c, f in ((32, 64), (16, 96), (32, 128)):
+        with pytest.raises(ValueError, match="load"):
+            b.load(sequence_params(gen.make_sequence_params(c, f, 6), B.F16))
+    with pytest.raises(ValueError, match="load"):
+        b.load({k: t for k, t in b.params.items() if k != "beta"})
+    with pytest.raises(ValueError, match="wg"):
+        b.load(sequence_params(gen.make_sequence_params(32, 96, 6), B.F32))
+    assert torch.equal(b.run(x, offsets), before)             # the old ones are still there
+    b.load(sequence_params(gen.make_sequence_params(32, 96, 6), B.F16))
+    assert not torch.equal(b.run(x, offsets), before)
+    ctx.status_sync()
+    ctx.close()
