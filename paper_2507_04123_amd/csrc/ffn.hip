@@ -1,7 +1,9 @@
 // Gated feed-forward network, forward pass and the order of its weights (ffn.h has the mathematics and the fragments).
 // A wave keeps its 32 rows of x and of y's sums in registers and walks the hidden units in slices of 32: two products for G and U, the
-// activation, H rounded to the operands' type (the matrix cores multiply 16-bit values; its error is that of the result's own rounding),
-// and the product with the slice's lines of Wd.
+// activation, H rounded to the operands' type, and the product with the slice's lines of Wd.
+// The matrix cores multiply 16-bit values.  H's rounding adds an error as large as the result's own: 1.4 times that of one whose H stays in fp32, and what is
+// beyond f16's range (65504) is infinite.  A second product with what the rounding leaves over takes that away at 162 -> 185 us (300 k x 128 x 512 f16),
+// 139 -> 166 (bf16), and for 300 rows 8.6 -> 10.4 (bf16): the hidden values are held as the rows and weights are.
 #include "ffn.h"
 
 namespace {
@@ -42,7 +44,7 @@ template <typename T, int CT> constexpr int kFfnWaves = sizeof(T) * CT <= 8 ? 2 
 // Many rows: a block of four waves has 128 rows and passes the weights, slice by slice, through LDS, where all waves read them.  Turn t multiplies
 // slice t's gates, activates slice t - 1 and multiplies slice t - 2's way down: three independent strands, so that the vector ALU's
 // activation (an exponential and a reciprocal an element) runs under the matrix cores' products.  The loads of turn t + 1's
-// weights are under way meanwhile.  300 k x 128 x 512 f16 165 us, 720 TFLOP/s: a fragment from LDS (128 bytes a clock) feeds one product of a wave,
+// weights are under way meanwhile.  300 k x 128 x 512 f16 160 to 166 us, 720 TFLOP/s: a fragment from LDS (128 bytes a clock) feeds one product of a wave,
 // which takes about as long as its reading, and 2344 blocks, two a CU at once, leave the fifth round half empty.  Measured and not better: 64 rows
 // a wave (fragments feed two products, one wave a SIMD) 211, eight waves a block with the weights two turns ahead 180, Wd's lines past LDS 244.
 constexpr int kManyWaves = 4;
@@ -277,7 +279,8 @@ extern "C" emc2_status emc2_ffn(emc2_ctx* ctx, emc2_dtype dtype, int32_t activat
     using T = decltype(type);
     constexpr int CT = decltype(tiles)::value;
     constexpr bool G = decltype(gelu)::value, P = decltype(pieces)::value;
-    // fp32 rows of over 64 channels would leave a SIMD one wave of k_ffn: 155 / 142 us for 64 k x 96 x 384, but 79 / 72 and 42 / 67 for 32 k and 16 k
+    // fp32 rows of over 64 channels would leave a SIMD one wave of k_ffn.  us, few / many, 96 x 384 at 16 k, 32 k and 64 k rows: 42 / 67, 79 / 72, 155 / 142: the
+    // form for few rows takes them all, and a tenth longer than it might from 32 k rows on
     constexpr bool kFew = sizeof(T) * CT > 8 && sizeof(T) == 4;
     if (kFew || capacity <= kFewRows)
       hipLaunchKernelGGL((k_ffn_few<T, CT, G, P>), emc2_grid(emc2_div_up(capacity, 32)), dim3(64 * kFewWaves<CT, P>), 0, (hipStream_t)stream, a);

@@ -1,7 +1,8 @@
 // Gradients of the gated feed-forward network (ffn.h has the mathematics of the forward pass and the fragments).
 //   dH = dy Wd^T, dU = dH act(G), dG = dH U act'(G);   dx = dG Wg^T + dU Wu^T;   dWg = x^T dG, dWu = x^T dU, dWd = H^T dy
 // G, U and dH are computed again in both kernels rather than stored: a slice of 32 hidden units costs 3 products per pass, and storing H, dG
-// and dU would move six times n F values.
+// and dU would move six times n F values.  dG, dU and H are rounded to the operands' type for their products, as H is in the forward pass (ffn.hip has what that
+// costs and saves): 16-bit gradients are 1.4 times as far from exact ones as with fp32 hidden values, and those of f16 lose places below 6e-5.
 // k_ffn_dx works like the forward pass: hidden units along the lanes' registers, rows along the lanes.
 // k_ffn_dw has them the other way round (rows along the registers), which is what a contraction over rows takes: dG, dU and H are its operands as
 // they are.  x and dy have to be turned round for it: a product with the identity does that on the matrix cores, exactly (of finite values).  Each block sums
@@ -25,10 +26,11 @@ template <typename T, bool WIDE> __device__ __forceinline__ void put_dx(const em
 }
 
 // Many rows: every wave has 32 rows of its own and walks all slices, whose weights pass through LDS for the whole block; the next
-// slice's are on their way meanwhile.  Wide rows of 16 bits take this form whatever their number; the others from that on where it is the faster one.
+// slice's are on their way meanwhile.  Wide rows of 16 bits take this form whatever their number; the others beyond the power of two that is nearest to where both
+// take as long.
 // us, the form below (whose waves split the slices) / this one at 16 k, 32 k and 64 k rows: f16 64 x 256 11 / 12, 22 / 13, 39 / 21;
 // f16 128 x 512 27 / 42, 51 / 46, 99 / 54; f16 256 x 512 122 / 71, 199 / 76, 353 / 147 (2 k rows 79 / 67);
-// f32 96 x 384 67 / 106, 129 / 113, 250 / 217.  At 300 k x 128 x 512 f16 256 us, 770 TFLOP/s: like the forward pass, bound by the weights' way out of LDS
+// f32 96 x 384 67 / 106, 129 / 113, 250 / 217 (at 32 k rows, the limit of these two, 5 and 16 us are lost).  At 300 k x 128 x 512 f16 256 us, 770 TFLOP/s: like the forward pass, bound by the weights' way out of LDS
 // (a wave's fragment feeds one product) and the products themselves.
 template <typename T, int CT> constexpr bool kDxMany = sizeof(T) * CT <= 16;              // LDS has room for two slices' weights
 template <typename T, int CT> constexpr bool kDxFew = sizeof(T) == 4 || CT <= 4;

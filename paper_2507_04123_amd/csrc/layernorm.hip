@@ -7,7 +7,7 @@
 // pass.  The weights' sums stay in each lane's registers while its block walks the rows; the blocks' sums are added by a second
 // launch in a fixed order (fp32 throughout, no atomics: equal inputs give equal bits).
 // Both are bound by memory: 613 k x 64 f16 with residual and sum 63 us, 5.0 TB/s of what it has to move (a copy of that size reaches 5.0); forward and
-// backward pass of 240 k x 128 bf16 67 us, 4.6 TB/s.
+// backward pass of 240 k x 128 bf16 68 us, 4.5 TB/s.
 #include "rows.h"
 
 namespace {
@@ -200,7 +200,7 @@ template <int N> __device__ __forceinline__ float sum_by_halves(float (&v)[N]) {
 }
 
 // dgamma and dbeta from the blocks' sums: 32 columns a block, 32 threads a column, each with eight loads under way (beyond the last sum: of the last one
-// again, not counted; 1251 sums of 180 columns 5.7 us, 6.2 with the last ones loaded in a row).  Added by halves: of 1280 sums none has more than
+// again, not counted; 1251 sums of 180 columns 4.9 us, 0.5 more with the last ones loaded in a row).  Added by halves: of 1280 sums none has more than
 // 13 additions behind it.
 __global__ void __launch_bounds__(1024) k_layernorm_weights(const float* __restrict__ partial, int32_t blocks, int32_t channels,
                                                             float* __restrict__ dgamma, float* __restrict__ dbeta) {
@@ -271,8 +271,9 @@ template <typename F> void with_type(emc2_dtype dtype, const Shape& s, F&& f) {
 }
 
 // Blocks of the backward pass, each walking the rows in steps of all blocks: about as many as the chip holds at once (a lane's sums and one row of 16
-// bytes leave room for five or six a CU, several vectors a lane for three), one row a lane at a time.  us with the forward pass, 240 k x 128 bf16 / 600 k x 64 f16 /
-// 30 k x 1024 bf16: 1280 or 1536 blocks 69 / 81 / 74, 1024 of two rows at a time 76 / 85 / 65, 1024 of four 94 / 106 / 67.
+// bytes leave room for five or six a CU, several vectors a lane for three), one row a lane at a time.  us with the forward pass, 240 k x 128 bf16 / 600 k x 64 f16:
+// 1280 or 1536 blocks 69 / 81, 1024 of two rows at a time 76 / 85, 1024 of four 94 / 106; several vectors a lane, 30 k x 1024 bf16 / 20 k x 768 f32 /
+// 60 k x 600 f16: 512 blocks 71 / 55 / 130, 768 65 / 56 / 107, 1024 74 / 59 / 133, 1280 71 / 60 / 122.
 constexpr int64_t kGradBlocks = 1280;
 constexpr int64_t grad_blocks(int vectors) { return vectors == 1 ? kGradBlocks : 768; }
 

@@ -13,19 +13,18 @@
 // The map that begins a sequence drops what lies before it, whatever that holds: an infinity or NaN in one sequence never reaches another one.
 // Its factor is -0, which no product of gates is: within a sequence a NaN or infinity travels on to the end, also where the gates' product is 0.
 // Bound by memory, and close behind by the logistic function's two slow instructions an element.  Rows are read by both launches: 613 k x 64 f16 in
-// eight sequences 98 us, 4.0 TB/s of both launches' bytes (the second finds much of its input in the last cache); 150 k x 96 fp32 in 9001 sequences 88 us,
-// 3.3 TB/s; forward pass and gradients of 200 k x 128 bf16 173 us, 3.8 TB/s.
+// eight sequences 99 us, 4.0 TB/s of both launches' bytes (the second finds much of its input in the last cache); 150 k x 96 fp32 in 9001 sequences 87 us,
+// 3.3 TB/s; forward pass and gradients of 200 k x 128 bf16 176 us, 3.8 TB/s (over the same inputs again and again 88, 72 and 166).
 #include "rows.h"
 
 namespace {
 
 constexpr int kMaxTiles = 32;        // tiles of a wave's run (forward) or of a block (gradients)
 constexpr int kSlice = 64;           // channels of a block at most
-// Waves of a block, rows of a thread and blocks aimed at, as measured (us, 613 k x 64 f16 forward; 200 k x 128 bf16 gradients): the second launch's
-// blocks compose the maps of all others, which costs 1024 of them 20 us; blocks of eight waves need half as many.
-//   forward, 8 waves, 4 rows: 512 blocks 102, 256 blocks 108; 8 rows, 256 blocks 102 (fp32 over 96 channels 82, 93, 91); 4 waves, 8 rows: 1024, 512,
-//   256 blocks 125, 111, 124.  gradients with the forward pass, 4 waves, 4 rows: 1024, 512, 256 blocks 220, 187, 241; 8 rows 274; 8 waves: 512,
-//   256 blocks 211, 195 (before the pieces of four values: 173 now)
+// Waves of a block, rows of a thread and blocks aimed at: the second launch's blocks compose the maps of all others, which costs 1024 of them 20 us;
+// blocks of eight waves need half as many.  us, 613 k x 64 f16 forward / 150 k x 96 fp32 in 9001 sequences forward / 200 k x 128 bf16 with gradients, over
+// the same inputs each time: as below 88 / 72 / 166; 256 blocks 92 / 83 / 219, 1024 105 / 87 / 203; forward of 4 waves 98 / 80, of 2 rows 96 / 75, of
+// 8 rows 98 / 96; gradients of 8 waves 194, of 2 rows 198, of 8 rows 202.
 constexpr int kStepThreads = 256;    // of the kernels of one value or piece a thread
 constexpr int kWavesForward = 8, kWavesGrad = 4, kRowsForward = 4, kRowsGrad = 4, kBlocks = 512;
 
