@@ -1,9 +1,12 @@
 """Capacities up to the 2^30 rows that the sequence operators accept: one launch holds the blocks of them all.  Rows beyond the device's count
 are neither read nor written, so the buffers here are those of the rows present."""
+import numpy as np
 import pytest
 import torch
 
 from paper_2507_04123_amd import binding as B
+
+import sequence_bounds as L
 
 pytestmark = pytest.mark.gpu
 
@@ -52,6 +55,8 @@ def test_fp32_networks_of_a_large_capacity(ctx, c):
         assert ctx.lib.emc2_ffn_backward(ctx.h, B.F32, B.ACT_SILU, x.data_ptr(), c, packed.data_ptr(), dy.data_ptr(), c, count.data_ptr(), cap, c,
                                          f, dx.data_ptr(), c, *(t.data_ptr() for t in g), work.data_ptr(), work.numel(), st) == B.OK
         out.append([y, dx, *g])
-    for p, q in zip(*out):                                    # (the weights' sums, and for 96 channels dx's, are cut otherwise)
-        assert torch.allclose(p, q, rtol=1e-4, atol=1e-4)
     assert torch.equal(out[0][0], out[1][0])
+    # the weights' sums, and for 96 channels dx's, are cut otherwise: either is within its bound of the exact one
+    bounds = L.ffn_backward("silu", *(t.double().cpu().numpy() for t in (x, *w, dy)), "f32")
+    for p, q, b in zip(out[0][1:], out[1][1:], bounds):
+        assert np.all(np.abs(p.double().cpu().numpy() - q.double().cpu().numpy()) <= 2 * b)

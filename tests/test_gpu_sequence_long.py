@@ -76,8 +76,9 @@ def _recurrence(ctx, dtype, c, n, off, backwards, spare, compare):
 
 
 # f16 and bf16: 24 tiles of 128 rows (gradients: 47 of 64) in blocks of 2 (3); 64 in 8 blocks of 8 (128 in 8 of 16); 71 in 3 blocks of 32 at most (141 in 5).
-# fp32: 20 tiles of 256 (40 of 128) in blocks of 3 (5); 36 in 2 blocks of 32 at most (71 in 3)
-@pytest.mark.parametrize("dtype,c,n", [("f16", 2048, 3000), ("bf16", 4096, 8190), ("f16", 16384, 9000), ("f32", 2047, 5001), ("f32", 16384, 9001)])
+# fp32: 20 tiles of 256 (40 of 128) in blocks of 3 (5); 36 in 2 blocks of 32 at most (71 in 3); as many channels as there may be in one block
+@pytest.mark.parametrize("dtype,c,n", [("f16", 2048, 3000), ("bf16", 4096, 8190), ("f16", 16384, 9000), ("f32", 2047, 5001), ("f32", 16384, 9001),
+                                       ("f16", 65536, 300), ("f32", 65533, 700)])
 @pytest.mark.parametrize("kind", ["one", "edges"])
 @pytest.mark.parametrize("backwards", [False, True])
 def test_recurrence_over_several_tiles(ctx, dtype, c, n, kind, backwards):
