@@ -544,11 +544,12 @@ emc2_status emc2_recurrence_step(emc2_ctx* ctx, emc2_dtype dtype, const void* d_
  *   y = (act(x Wg) * (x Wu)) Wd (+ res);   x, y [n][channels], Wg and Wu [channels][hidden], Wd [hidden][channels], all of `dtype`
  *   act: EMC2_ACT_SILU g / (1 + exp(-g)); EMC2_ACT_GELU its tanh form 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
  * The products run on the matrix cores with fp32 sums; the hidden values act * up are rounded to `dtype` between them (as are their gradients in
- * the backward pass) and never leave the chip.  So F16 holds hidden values up to 65504, infinite beyond it whatever Wd makes of them, and gradients of hidden
- * values in full from 6e-5 on: scale a loss, or take BF16, which has fp32's range.  A value of dy that is not finite makes its row of dx, its
+ * the backward pass) and never leave the chip.  Calls of up to 2048 rows hold what that leaves over as well, so that results are as near as with fp32 hidden
+ * values; those of more rows are 1.4 times as far.  F16 holds hidden values up to 65504, not finite beyond it whatever Wd makes of them, and gradients of
+ * hidden values in full from 6e-5 on: scale a loss, or take BF16, which has fp32's range.  A value of dy that is not finite makes its row of dx, its
  * column of dWd and all of dWg and dWu not finite, and nothing else.  channels in [1, 256], hidden in [1, 65536].
- * Up to 32 rows are one block's work, which reads all of the weights: 24 rows of F16 take 8 us for 128 x 512 (backward 23), 26 for 256 x 1024 (149), 172 for
- * 256 x 4096 (511); F32 30 and 124 for the first two (73, 333).
+ * Up to 32 rows are one block's work, which reads all of the weights: 24 rows of F16 take 8 us for 128 x 512 (backward 25), 30 for 256 x 1024 (169), 209 for
+ * 256 x 4096 (563); F32 30 and 125 for the first two (73, 333).
  * emc2_ffn_pack: the three weights, contiguous, re-ordered into matrix-core fragments: d_packed [emc2_ffn_packed_size] values of `dtype`,
  * 16-byte aligned; once per model for serving, after every change of the weights in training.
  */

@@ -104,10 +104,10 @@ template <bool EXACT, bool GELU> __device__ __forceinline__ float emc2_activate(
   slope = __builtin_fmaf(a, rest, s);
   return a;
 }
-// Two neighbouring values of a result tile, registers r and r + 1 (r even), into the fragments made of it.
-template <typename T> __device__ __forceinline__ void emc2_put_pair(typename emc2_tile<T>::frag* f, int r, float a, float b) {
+// Two neighbouring values of a result tile, registers r and r + 1 (r even), into the fragments made of it: P = 1 rounded, P = 2 also what the rounding
+// leaves over, in fragments of its own, whose products with the same operand make up for it.
+template <typename T> __device__ __forceinline__ void emc2_put_pair(typename emc2_tile<T>::frag* f, int r, emc2_vec<T, 2> v) {
   constexpr int kPer = emc2_tile<T>::kPer;
-  const emc2_vec<T, 2> v = __builtin_convertvector((emc2_fvec<2>{a, b}), emc2_vec<T, 2>);
   if constexpr (sizeof(T) == 2) {
     emc2_vec<uint32_t, 4> w = __builtin_bit_cast(emc2_vec<uint32_t, 4>, f[r / kPer]);
     w[r % kPer / 2] = __builtin_bit_cast(uint32_t, v);
@@ -116,6 +116,25 @@ template <typename T> __device__ __forceinline__ void emc2_put_pair(typename emc
     f[r / kPer][r % kPer] = v[0], f[r / kPer][r % kPer + 1] = v[1];
   }
 }
+template <typename T> __device__ __forceinline__ void emc2_put_pair(typename emc2_tile<T>::frag* f, int r, float a, float b) {
+  emc2_put_pair<T>(f, r, __builtin_convertvector((emc2_fvec<2>{a, b}), emc2_vec<T, 2>));
+}
+template <typename T, int P, int MM>
+__device__ __forceinline__ void emc2_put_pair(typename emc2_tile<T>::frag (&f)[P][MM], int r, float a, float b) {
+  const emc2_vec<T, 2> v = __builtin_convertvector((emc2_fvec<2>{a, b}), emc2_vec<T, 2>);
+  emc2_put_pair<T>(f[0], r, v);
+  if constexpr (P == 2) {
+    const emc2_fvec<2> q = __builtin_convertvector(v, emc2_fvec<2>);
+    emc2_put_pair<T>(f[1], r, __builtin_convertvector((emc2_fvec<2>{a - q[0], b - q[1]}), emc2_vec<T, 2>));
+  }
+}
+
+// Rows up to which 16-bit hidden values and their gradients are held in two parts (P = 2), the rounded value and what that leaves over: results are as near as
+// with fp32 hidden values.  One part adds an error as large as the result's own rounding (1.4 times the plain one's over many values, up to twice over those of
+// a few rows).  A second product each is hidden by the latency of small calls and not by the products of large ones.  us, one part / two: forward, 24 rows x 128 x 512 f16
+// 8.5 / 8.9, 300 x 256 x 1024 27 / 31, 16 k x 128 x 512 18 / 20 (bf16), 300 k 162 / 185 (f16) and 139 / 166 (bf16); with gradients, 24 rows x 128 x 512 f16 40 / 42,
+// 2 k x 64 x 256 29 / 29, 2 k x 128 x 512 bf16 49 / 51, 2 k x 256 x 512 f16 141 / 158, 100 k x 64 x 256 bf16 106 / 122 (forward in one part).
+constexpr int64_t kFfnRestRows = 2048;
 
 // Arguments of a launch.
 struct emc2_ffn_args {

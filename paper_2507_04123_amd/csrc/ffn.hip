@@ -1,9 +1,7 @@
 // Gated feed-forward network, forward pass and the order of its weights (ffn.h has the mathematics and the fragments).
 // A wave keeps its 32 rows of x and of y's sums in registers and walks the hidden units in slices of 32: two products for G and U, the
-// activation, H rounded to the operands' type, and the product with the slice's lines of Wd.
-// The matrix cores multiply 16-bit values.  H's rounding adds an error as large as the result's own: 1.4 times that of one whose H stays in fp32, and what is
-// beyond f16's range (65504) is infinite.  A second product with what the rounding leaves over takes that away at 162 -> 185 us (300 k x 128 x 512 f16),
-// 139 -> 166 (bf16), and for 300 rows 8.6 -> 10.4 (bf16): the hidden values are held as the rows and weights are.
+// activation, H rounded to the operands' type (the matrix cores multiply 16-bit values; up to kFfnRestRows rows in two parts), and the product with the
+// slice's lines of Wd.  What is beyond f16's range (65504) is not finite.
 #include "ffn.h"
 
 namespace {
@@ -13,6 +11,7 @@ constexpr int kThreads = 256;
 // us, few / many at 8 k, 16 k, 24 k and 64 k rows: f16 64 x 256 5.3 / 9.6, 7.4 / 9.9, 10.4 / 10.2, 22 / 15; f16 128 x 512 11 / 18, 18 / 19, 26 / 19,
 // 65 / 36; f16 256 x 512 20 / 40, 38 / 42, 55 / 44, 143 / 90; f32 48 x 200 12 / 30, 20 / 31, 29 / 32, 69 / 60.
 constexpr int64_t kFewRows = 16384;
+static_assert(kFfnRestRows <= kFewRows, "two parts: in the form for few rows only");
 
 // Four neighbouring values of a result's row, from channel `at` on.
 template <typename T, bool WIDE> __device__ __forceinline__ void put(const emc2_ffn_args& a, int64_t row, int at, emc2_fvec<4> v) {
@@ -29,10 +28,10 @@ template <typename T, bool WIDE> __device__ __forceinline__ void put(const emc2_
 }
 
 // H's registers r and r + 1, as operands
-template <typename T, bool GELU>
-__device__ __forceinline__ void hidden(const emc2_acc& g, const emc2_acc& u, int r, typename emc2_tile<T>::frag* h) {
+template <typename T, bool GELU, int P, int MM>
+__device__ __forceinline__ void hidden(const emc2_acc& g, const emc2_acc& u, int r, typename emc2_tile<T>::frag (&h)[P][MM]) {
   constexpr bool kExact = sizeof(T) == 4;
-  emc2_put_pair<T>(h, r, emc2_activate<kExact, GELU>(g[r]) * u[r], emc2_activate<kExact, GELU>(g[r + 1]) * u[r + 1]);
+  emc2_put_pair<T, P, MM>(h, r, emc2_activate<kExact, GELU>(g[r]) * u[r], emc2_activate<kExact, GELU>(g[r + 1]) * u[r + 1]);
 }
 
 template <bool GATES, bool ACT, bool DOWN> struct Stages { static constexpr bool gates = GATES, act = ACT, down = DOWN; };
@@ -64,7 +63,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, (kFfnWaves<T, CT>)) k_ffn(con
 #pragma unroll
   for (int c = 0; c < CT; ++c) y[c] = 0.0f;
   emc2_acc g[2], u[2];                   // of the slice whose gates were multiplied last, and of this turn's
-  frag h[2][MM];                         // likewise
+  frag h[2][1][MM];                      // likewise
   const frag* packed = (const frag*)a.packed + lane;
   // A turn's weights, fragment by fragment over the waves: gates of slice t + 1 and lines down of slice t - 1, by way of registers (loads
   // straight into LDS are waited for, all of them, before the next read of LDS).
@@ -99,10 +98,10 @@ __global__ void __launch_bounds__(64 * kManyWaves, (kFfnWaves<T, CT>)) k_ffn(con
         g[now] = emc2_mma<T>(w[(KK + k) * 64], x[k], g[now]);
         u[now] = emc2_mma<T>(w[(2 * KK + k) * 64], x[k], u[now]);
       }
-      if constexpr (kDown) y[k / MM] = emc2_mma<T>(w[k * 64], h[now][k % MM], y[k / MM]);
+      if constexpr (kDown) y[k / MM] = emc2_mma<T>(w[k * 64], h[now][0][k % MM], y[k / MM]);
       if constexpr (kAct) {
 #pragma unroll
-        for (int r = 8 * k / KK; r < 8 * (k + 1) / KK; ++r) hidden<T, GELU>(g[now ^ 1], u[now ^ 1], 2 * r, h[now ^ 1]);
+        for (int r = 8 * k / KK; r < 8 * (k + 1) / KK; ++r) hidden<T, GELU, 1, MM>(g[now ^ 1], u[now ^ 1], 2 * r, h[now ^ 1]);
       }
     }
     if constexpr (kGates && kAct && kDown && sizeof(T) == 2) {
@@ -140,12 +139,13 @@ __global__ void __launch_bounds__(64 * kManyWaves, (kFfnWaves<T, CT>)) k_ffn(con
 
 // Few rows: a block has 32 of them, its waves share the slices out, each reading its own from memory at once, and their sums meet in LDS.
 template <int CT, bool WIDE> constexpr int kFewWaves = CT == 8 && !WIDE ? 4 : 8;   // (four: rows value by value take more registers)
-template <typename T, int CT, bool GELU, bool WIDE>
+template <typename T, int CT, bool GELU, bool WIDE, int P>
 __global__ void __launch_bounds__((64 * kFewWaves<CT, WIDE>)) k_ffn_few(const emc2_ffn_args a) {
   typedef emc2_tile<T> M;
   typedef typename M::frag frag;
   constexpr int KK = 32 * CT / M::kDeep, MM = 32 / M::kDeep;
   constexpr int kWaves = kFewWaves<CT, WIDE>;
+  constexpr bool kAhead = P == 2 && CT <= 4;               // the lines down are requested before the activation, where registers allow it
   __shared__ emc2_fvec<4> part[kWaves][4][64];
   const int32_t n = emc2_row_count(a.d_n, a.capacity);
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -165,12 +165,21 @@ __global__ void __launch_bounds__((64 * kFewWaves<CT, WIDE>)) k_ffn_few(const em
       g = emc2_mma<T>(w[(EMC2_FFN_GATE * KK + k) * 64], x[k], g);
       u = emc2_mma<T>(w[(EMC2_FFN_UP * KK + k) * 64], x[k], u);
     }
-    frag h[MM];
+    frag h[P][MM], down[kAhead ? KK : 1];
+    if constexpr (kAhead) {
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) hidden<T, GELU>(g, u, r, h);
+      for (int k = 0; k < KK; ++k) down[k] = w[(EMC2_FFN_DOWN * KK + k) * 64];
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) hidden<T, GELU, P, MM>(g, u, r, h);
     if constexpr (CT == 8) __builtin_amdgcn_sched_barrier(0);   // no loads further ahead: registers
 #pragma unroll
-    for (int k = 0; k < KK; ++k) y[k / MM] = emc2_mma<T>(w[(EMC2_FFN_DOWN * KK + k) * 64], h[k % MM], y[k / MM]);
+    for (int k = 0; k < KK; ++k) {
+      if constexpr (!kAhead) down[0] = w[(EMC2_FFN_DOWN * KK + k) * 64];
+#pragma unroll
+      for (int p = 0; p < P; ++p) y[k / MM] = emc2_mma<T>(down[kAhead ? k : 0], h[p][k % MM], y[k / MM]);
+    }
   }
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
@@ -278,14 +287,19 @@ extern "C" emc2_status emc2_ffn(emc2_ctx* ctx, emc2_dtype dtype, int32_t activat
   emc2_ffn_dispatch(dtype, emc2_ffn_tiles(channels), activation == EMC2_ACT_GELU, wide, [&](auto type, auto tiles, auto gelu, auto pieces) {
     using T = decltype(type);
     constexpr int CT = decltype(tiles)::value;
-    constexpr bool G = decltype(gelu)::value, P = decltype(pieces)::value;
+    constexpr bool G = decltype(gelu)::value, W = decltype(pieces)::value;
+    const auto few = [&](auto parts) {
+      hipLaunchKernelGGL((k_ffn_few<T, CT, G, W, decltype(parts)::value>), emc2_grid(emc2_div_up(capacity, 32)), dim3(64 * kFewWaves<CT, W>), 0,
+                         (hipStream_t)stream, a);
+    };
+    if constexpr (sizeof(T) == 2)
+      if (capacity <= kFfnRestRows) return few(emc2_const<2>());
     // fp32 rows of over 64 channels would leave a SIMD one wave of k_ffn.  us, few / many, 96 x 384 at 16 k, 32 k and 64 k rows: 42 / 67, 79 / 72, 155 / 142: the
     // form for few rows takes them all, and a tenth longer than it might from 32 k rows on
     constexpr bool kFew = sizeof(T) * CT > 8 && sizeof(T) == 4;
-    if (kFew || capacity <= kFewRows)
-      hipLaunchKernelGGL((k_ffn_few<T, CT, G, P>), emc2_grid(emc2_div_up(capacity, 32)), dim3(64 * kFewWaves<CT, P>), 0, (hipStream_t)stream, a);
+    if (kFew || capacity <= kFewRows) few(emc2_const<1>());
     else if constexpr (!kFew)
-      hipLaunchKernelGGL((k_ffn<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32 * kManyWaves)), dim3(64 * kManyWaves), 0, (hipStream_t)stream, a);
+      hipLaunchKernelGGL((k_ffn<T, CT, G, W>), dim3((unsigned)emc2_div_up(capacity, 32 * kManyWaves)), dim3(64 * kManyWaves), 0, (hipStream_t)stream, a);
   });
   return emc2_check_hip(ctx, hipGetLastError(), "emc2_ffn launch");
 }

@@ -1,8 +1,8 @@
 // Gradients of the gated feed-forward network (ffn.h has the mathematics of the forward pass and the fragments).
 //   dH = dy Wd^T, dU = dH act(G), dG = dH U act'(G);   dx = dG Wg^T + dU Wu^T;   dWg = x^T dG, dWu = x^T dU, dWd = H^T dy
 // G, U and dH are computed again in both kernels rather than stored: a slice of 32 hidden units costs 3 products per pass, and storing H, dG
-// and dU would move six times n F values.  dG, dU and H are rounded to the operands' type for their products, as H is in the forward pass (ffn.hip has what that
-// costs and saves): 16-bit gradients are 1.4 times as far from exact ones as with fp32 hidden values, and those of f16 lose places below 6e-5.
+// and dU would move six times n F values.  dG, dU and H are rounded to the operands' type for their products, up to kFfnRestRows rows in two parts; f16 ones lose
+// places below 6e-5 all the same.
 // k_ffn_dx works like the forward pass: hidden units along the lanes' registers, rows along the lanes.
 // k_ffn_dw has them the other way round (rows along the registers), which is what a contraction over rows takes: dG, dU and H are its operands as
 // they are.  x and dy have to be turned round for it: a product with the identity does that on the matrix cores, exactly (of finite values).  Each block sums
@@ -35,9 +35,10 @@ template <typename T, bool WIDE> __device__ __forceinline__ void put_dx(const em
 template <typename T, int CT> constexpr bool kDxMany = sizeof(T) * CT <= 16;              // LDS has room for two slices' weights
 template <typename T, int CT> constexpr bool kDxFew = sizeof(T) == 4 || CT <= 4;
 template <typename T, int CT> constexpr int64_t kDxFewRows = !kDxFew<T, CT> ? 0 : sizeof(T) * CT < 8 ? 16384 : 32768;
+static_assert(kFfnRestRows <= 16384, "two parts: this form has the types that have no other one");
 template <typename T, int CT> constexpr int kDxManyASimd = sizeof(T) * CT <= 8 ? 2 : 1;   // waves a SIMD that the registers are enough for
 template <typename T, int CT> constexpr int kDxManyWaves = sizeof(T) * CT <= 4 || sizeof(T) * CT > 8 ? 4 : 8;   // (and the fragments under way are fewer a wave)
-template <typename T, int CT, bool GELU, bool WIDE>
+template <typename T, int CT, bool GELU, bool WIDE, int P>
 __global__ void __launch_bounds__((64 * kDxManyWaves<T, CT>), (kDxManyASimd<T, CT>)) k_ffn_dx_many(const emc2_ffn_args a) {
   typedef emc2_tile<T> M;
   typedef typename M::frag frag;
@@ -87,19 +88,22 @@ __global__ void __launch_bounds__((64 * kDxManyWaves<T, CT>), (kDxManyASimd<T, C
     __builtin_amdgcn_sched_barrier(0);
     keep((s + 1) & 1, 0, 3 * KK);
     fetch(s + 1, 3 * KK, 5 * KK);
-    frag dg[MM], du[MM];
+    frag dg[P][MM], du[P][MM];
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
       float slope[2];
       const float act[2] = {emc2_activate<kExact, GELU>(g[r], slope[0]), emc2_activate<kExact, GELU>(g[r + 1], slope[1])};
-      emc2_put_pair<T>(dg, r, dh[r] * u[r] * slope[0], dh[r + 1] * u[r + 1] * slope[1]);
-      emc2_put_pair<T>(du, r, dh[r] * act[0], dh[r + 1] * act[1]);
+      emc2_put_pair<T, P, MM>(dg, r, dh[r] * u[r] * slope[0], dh[r + 1] * u[r + 1] * slope[1]);
+      emc2_put_pair<T, P, MM>(du, r, dh[r] * act[0], dh[r + 1] * act[1]);
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
-      dx[k / MM] = emc2_mma<T>(w[(3 * KK + k) * 64], dg[k % MM], dx[k / MM]);
-      dx[k / MM] = emc2_mma<T>(w[(4 * KK + k) * 64], du[k % MM], dx[k / MM]);
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        dx[k / MM] = emc2_mma<T>(w[(3 * KK + k) * 64], dg[p][k % MM], dx[k / MM]);
+        dx[k / MM] = emc2_mma<T>(w[(4 * KK + k) * 64], du[p][k % MM], dx[k / MM]);
+      }
       if constexpr (kShort) if (k % 8 == 7) __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -116,7 +120,7 @@ __global__ void __launch_bounds__((64 * kDxManyWaves<T, CT>), (kDxManyASimd<T, C
 // A block has 32 rows; its waves (eight, or four where x, dy and dx's sums take over half of a SIMD's registers) share the slices out, each
 // reading its own weights from memory at once, and their sums meet in LDS.
 template <typename T, int CT> constexpr int kDxWaves = sizeof(T) == 4 && CT == 4 ? 4 : 8;
-template <typename T, int CT, bool GELU, bool WIDE>
+template <typename T, int CT, bool GELU, bool WIDE, int P>
 __global__ void __launch_bounds__((64 * kDxWaves<T, CT>)) k_ffn_dx(const emc2_ffn_args a) {
   typedef emc2_tile<T> M;
   typedef typename M::frag frag;
@@ -144,18 +148,22 @@ __global__ void __launch_bounds__((64 * kDxWaves<T, CT>)) k_ffn_dx(const emc2_ff
       u = emc2_mma<T>(w[(EMC2_FFN_UP * KK + k) * 64], x[k], u);
       dh = emc2_mma<T>(w[(EMC2_FFN_DOWN_T * KK + k) * 64], dy[k], dh);
     }
-    frag dg[MM], du[MM];
+    frag dg[P][MM], du[P][MM];
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
       float slope[2];
       const float act[2] = {emc2_activate<kExact, GELU>(g[r], slope[0]), emc2_activate<kExact, GELU>(g[r + 1], slope[1])};
-      emc2_put_pair<T>(dg, r, dh[r] * u[r] * slope[0], dh[r + 1] * u[r + 1] * slope[1]);
-      emc2_put_pair<T>(du, r, dh[r] * act[0], dh[r + 1] * act[1]);
+      emc2_put_pair<T, P, MM>(dg, r, dh[r] * u[r] * slope[0], dh[r + 1] * u[r + 1] * slope[1]);
+      emc2_put_pair<T, P, MM>(du, r, dh[r] * act[0], dh[r + 1] * act[1]);
     }
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
-      dx[k / MM] = emc2_mma<T>(w[(EMC2_FFN_GATE_T * KK + k) * 64], dg[k % MM], dx[k / MM]);
-      dx[k / MM] = emc2_mma<T>(w[(EMC2_FFN_UP_T * KK + k) * 64], du[k % MM], dx[k / MM]);
+      const frag gate = w[(EMC2_FFN_GATE_T * KK + k) * 64], up = w[(EMC2_FFN_UP_T * KK + k) * 64];
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        dx[k / MM] = emc2_mma<T>(gate, dg[p][k % MM], dx[k / MM]);
+        dx[k / MM] = emc2_mma<T>(up, du[p][k % MM], dx[k / MM]);
+      }
     }
   }
 #pragma unroll
@@ -193,7 +201,7 @@ __device__ __forceinline__ void turned(const emc2_row<T, CT, WIDE>& rows, int fi
 // activation (up to 9 % slower), a part's slices on one XCD (up to 10 % slower).
 // Waves a SIMD: two where the sums are few.
 template <typename T, int CT> constexpr int kDwWaves = sizeof(T) * CT <= 4 ? 2 : 1;   // (parts_of counts on it)
-template <typename T, int CT, bool GELU, bool WIDE, int C0, int CB>
+template <typename T, int CT, bool GELU, bool WIDE, int C0, int CB, int P>
 __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const emc2_ffn_args a) {
   typedef emc2_tile<T> M;
   typedef typename M::frag frag;
@@ -233,14 +241,14 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
       u = emc2_mma<T>(x[k], w[(KK + k) * 64 + at], u);
       dh = emc2_mma<T>(dy[k], w[(2 * KK + k) * 64 + at], dh);
     }
-    frag h[MM], dg[MM], du[MM];
+    frag h[P][MM], dg[P][MM], du[P][MM];
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
       float slope[2];
       const float act[2] = {emc2_activate<kExact, GELU>(g[r], slope[0]), emc2_activate<kExact, GELU>(g[r + 1], slope[1])};
-      emc2_put_pair<T>(h, r, act[0] * u[r], act[1] * u[r + 1]);
-      emc2_put_pair<T>(dg, r, dh[r] * u[r] * slope[0], dh[r + 1] * u[r + 1] * slope[1]);
-      emc2_put_pair<T>(du, r, dh[r] * act[0], dh[r + 1] * act[1]);
+      emc2_put_pair<T, P, MM>(h, r, act[0] * u[r], act[1] * u[r + 1]);
+      emc2_put_pair<T, P, MM>(dg, r, dh[r] * u[r] * slope[0], dh[r + 1] * u[r + 1] * slope[1]);
+      emc2_put_pair<T, P, MM>(du, r, dh[r] * act[0], dh[r + 1] * act[1]);
     }
     // tile 2 c of x and 2 c + 1 of dy, each turned one step ahead of its products
     frag t[2][MM];
@@ -254,8 +262,11 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
       }
 #pragma unroll
       for (int m = 0; m < MM; ++m) {
-        if (i % 2) dwd[c] = emc2_mma<T>(h[m], t[1][m], dwd[c]);
-        else dwg[c] = emc2_mma<T>(t[0][m], dg[m], dwg[c]), dwu[c] = emc2_mma<T>(t[0][m], du[m], dwu[c]);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          if (i % 2) dwd[c] = emc2_mma<T>(h[p][m], t[1][m], dwd[c]);
+          else dwg[c] = emc2_mma<T>(t[0][m], dg[p][m], dwg[c]), dwu[c] = emc2_mma<T>(t[0][m], du[p][m], dwu[c]);
+        }
       }
       if constexpr (kWavesASimd == 1) __builtin_amdgcn_sched_barrier(0);   // no further ahead: registers
     }
@@ -303,10 +314,10 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
         u = emc2_mma<T>(v, w[(KK + k) * 64 + at], u);
         __builtin_amdgcn_sched_barrier(0);
       }
-      frag h[MM];
+      frag h[P][MM];
 #pragma unroll
       for (int r = 0; r < 16; r += 2)
-        emc2_put_pair<T>(h, r, emc2_activate<kExact, GELU>(g[r]) * u[r], emc2_activate<kExact, GELU>(g[r + 1]) * u[r + 1]);
+        emc2_put_pair<T, P, MM>(h, r, emc2_activate<kExact, GELU>(g[r]) * u[r], emc2_activate<kExact, GELU>(g[r + 1]) * u[r + 1]);
 #pragma unroll
       for (int c = 0; c < CB; ++c) {
         const T* dy = (const T*)a.dy + min(32 * (C0 + c) + (at & 31), a.channels - 1);
@@ -315,7 +326,8 @@ __global__ void __launch_bounds__(kThreads, (kDwWaves<T, CT>)) k_ffn_dw(const em
           frag t;
 #pragma unroll
           for (int e = 0; e < M::kPer; ++e) t[e] = dy[min(tile * 32 + emc2_hidden_of<T>(m, half, e), most) * a.ld_dy];
-          dwd[c] = emc2_mma<T>(h[m], t, dwd[c]);
+#pragma unroll
+          for (int p = 0; p < P; ++p) dwd[c] = emc2_mma<T>(h[p][m], t, dwd[c]);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -425,19 +437,31 @@ extern "C" emc2_status emc2_ffn_backward(emc2_ctx* ctx, emc2_dtype dtype, int32_
   const dim3 dw_grid((unsigned)((int64_t)a.parts * a.slices));
   emc2_ffn_dispatch(dtype, tiles, activation == EMC2_ACT_GELU, wide, [&](auto type, auto count, auto gelu, auto pieces) {
     using T = decltype(type);
-    constexpr bool G = decltype(gelu)::value, P = decltype(pieces)::value;
+    constexpr bool G = decltype(gelu)::value;
     constexpr int CT = decltype(count)::value, CB = CT > 4 ? CT / 2 : CT;   // (the sums of more tiles of channels leave no registers)
-    // the weights' launches first: dx may lie where dy did
-    hipLaunchKernelGGL((k_ffn_dw<T, CT, G, P, 0, CB>), dw_grid, dim3(kThreads), 0, s, a);
-    if constexpr (CB < CT) hipLaunchKernelGGL((k_ffn_dw<T, CT, G, P, CB, CT - CB>), dw_grid, dim3(kThreads), 0, s, a);
-    if constexpr (kDxMany<T, CT>) {
-      constexpr int W = kDxManyWaves<T, CT>;
-      if (capacity > kDxFewRows<T, CT>)
-        hipLaunchKernelGGL((k_ffn_dx_many<T, CT, G, P>), dim3((unsigned)emc2_div_up(capacity, 32 * W)), dim3(64 * W), 0, s, a);
-    }
-    if constexpr (kDxFew<T, CT>) {
-      if (!none && !(kDxMany<T, CT> && capacity > kDxFewRows<T, CT>))
-        hipLaunchKernelGGL((k_ffn_dx<T, CT, G, P>), emc2_grid(emc2_div_up(capacity, 32)), dim3(64 * kDxWaves<T, CT>), 0, s, a);
+    const auto launch = [&](auto whole, auto parts) {
+      constexpr bool W = decltype(whole)::value;
+      constexpr int P = decltype(parts)::value;
+      // the weights' launches first: dx may lie where dy did
+      hipLaunchKernelGGL((k_ffn_dw<T, CT, G, W, 0, CB, P>), dw_grid, dim3(kThreads), 0, s, a);
+      if constexpr (CB < CT) hipLaunchKernelGGL((k_ffn_dw<T, CT, G, W, CB, CT - CB, P>), dw_grid, dim3(kThreads), 0, s, a);
+      // (two parts are for fewer rows than need a choice of forms)
+      constexpr bool kMany = kDxMany<T, CT> && (P == 1 || !kDxFew<T, CT>);
+      if constexpr (kMany) {
+        constexpr int kWaves = kDxManyWaves<T, CT>;
+        if (capacity > kDxFewRows<T, CT>)
+          hipLaunchKernelGGL((k_ffn_dx_many<T, CT, G, W, P>), dim3((unsigned)emc2_div_up(capacity, 32 * kWaves)), dim3(64 * kWaves), 0, s, a);
+      }
+      if constexpr (kDxFew<T, CT>) {
+        if (!none && !(kMany && capacity > kDxFewRows<T, CT>))
+          hipLaunchKernelGGL((k_ffn_dx<T, CT, G, W, P>), emc2_grid(emc2_div_up(capacity, 32)), dim3(64 * kDxWaves<T, CT>), 0, s, a);
+      }
+    };
+    if constexpr (sizeof(T) == 2) {
+      if (capacity <= kFfnRestRows) launch(emc2_const<0>(), emc2_const<2>());   // (one form for whole pieces and others)
+      else launch(pieces, emc2_const<1>());
+    } else {
+      launch(pieces, emc2_const<1>());
     }
     hipLaunchKernelGGL(k_ffn_sum<T>, dim3((unsigned)((int64_t)a.slices * 3 * CT * 256 / (kThreads / kSumThreads))), dim3(kThreads), 0, s,
                        (const float4*)d_work, a.parts, a.slices, CT, channels, hidden, (T*)d_dwg, (T*)d_dwu, (T*)d_dwd);
