@@ -567,6 +567,52 @@ emc2_status emc2_ffn_backward(emc2_ctx* ctx, emc2_dtype dtype, int32_t activatio
                               void* d_dx, int64_t ld_dx, void* d_dwg, void* d_dwu, void* d_dwd, void* d_work, int64_t work_bytes,
                               void* stream);
 
+/*
+ * Short causal convolution along the rows of every sequence, channel by channel:
+ *   z_t = bias + sum over k in [0, taps) of w[k] x_{t-k};   y_t = z_t / (1 + exp(-z_t)) with silu != 0, else z_t
+ * Sequences, d_offsets and `backwards` as for emc2_recurrence.  d_w [taps][channels]: w[0] is the row's own; d_bias [channels], NULL = 0.
+ * d_before [n_seq][taps - 1][channels]: the rows before a sequence's first, oldest first, NULL = zeros; d_last, of the same shape, receives the last rows
+ * of every sequence in the same way (those of d_before that are still among them included), NULL to skip: the d_before with which the sequence goes on.
+ * taps in [2, 8], channels in [1, 65536].  d_y must not overlap d_x, nor d_last d_before (nor, below, d_dx d_x or d_dy, nor d_dbefore d_before or
+ * d_dlast): blocks read the rows of their neighbours.  Such calls are refused.
+ */
+emc2_status emc2_causal_conv(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const float* d_w, const float* d_bias, int32_t silu,
+                             const int32_t* d_offsets, int32_t n_seq, int64_t capacity, int32_t channels, int32_t taps, int32_t backwards,
+                             const float* d_before, void* d_y, int64_t ld_y, float* d_last, void* stream);
+/* Its gradients for dy and d_dlast (of the rows kept, NULL = zeros): dx, dw, dbias and d_dbefore (both NULL to skip). */
+int64_t emc2_causal_conv_work(emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t taps);
+emc2_status emc2_causal_conv_backward(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const float* d_w, const float* d_bias,
+                                      int32_t silu, const int32_t* d_offsets, int32_t n_seq, int64_t capacity, int32_t channels, int32_t taps,
+                                      int32_t backwards, const float* d_before, const void* d_dy, int64_t ld_dy, const float* d_dlast, void* d_dx,
+                                      int64_t ld_dx, float* d_dw, float* d_dbias, float* d_dbefore, void* d_work, int64_t work_bytes,
+                                      void* stream);
+/* The convolution for one row per sequence (serving a stream): d_state [rows][taps - 1][channels] the rows before, d_state_out (may be d_state) the
+ * same moved on by the row. */
+emc2_status emc2_causal_conv_step(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const float* d_w, const float* d_bias,
+                                  int32_t silu, const float* d_state, int64_t rows, int32_t channels, int32_t taps, float* d_state_out, void* d_y,
+                                  int64_t ld_y, void* stream);
+
+/*
+ * From a block's result to the next block's input, per row: the norm behind the block, its gate, the scale of the residual branch, the residual sum, and the
+ * norm before the next block:
+ *   sum = x + scale * act * rms(branch) * post;   y = rms(sum) * next;   rms(v) = v / sqrt(mean of v^2 + eps), act = gate / (1 + exp(-gate))
+ * d_gate NULL: act = 1.  d_post, d_next [channels]; d_scale one value.  d_next and d_y NULL: the sum only (behind the last block).  y is taken from the sum
+ * before that is rounded.  channels in [1, 1024].
+ */
+emc2_status emc2_gated_residual(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_branch, int64_t ld_branch,
+                                const void* d_gate, int64_t ld_gate, const float* d_post, const float* d_scale, const float* d_next, float eps,
+                                const int32_t* d_n, int64_t capacity, int32_t channels, void* d_sum, int64_t ld_sum, void* d_y, int64_t ld_y,
+                                void* stream);
+/* Its gradients for dsum and dy (one of them may be NULL = zeros; dy, d_next and d_dnext go together, so do d_gate and d_dgate): dx, dbranch, dgate, and
+ * dpost, dscale, dnext summed over the rows.  All is computed again from x, branch and gate. */
+int64_t emc2_gated_residual_work(emc2_dtype dtype, int64_t capacity, int32_t channels);
+emc2_status emc2_gated_residual_backward(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_branch, int64_t ld_branch,
+                                         const void* d_gate, int64_t ld_gate, const float* d_post, const float* d_scale, const float* d_next,
+                                         float eps, const void* d_dsum, int64_t ld_dsum, const void* d_dy, int64_t ld_dy, const int32_t* d_n,
+                                         int64_t capacity, int32_t channels, void* d_dx, int64_t ld_dx, void* d_dbranch, int64_t ld_dbranch,
+                                         void* d_dgate, int64_t ld_dgate, float* d_dpost, float* d_dscale, float* d_dnext, void* d_work,
+                                         int64_t work_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -36,7 +36,8 @@ EXPORTS = ["emc2_create", "emc2_destroy", "emc2_status_sync", "emc2_last_error",
            "emc2_build_stacks", "emc2_spconv_list", "emc2_group_slots",
            "emc2_frame_offsets", "emc2_layernorm", "emc2_layernorm_work", "emc2_layernorm_backward", "emc2_recurrence", "emc2_recurrence_work",
            "emc2_recurrence_backward", "emc2_recurrence_step", "emc2_ffn_packed_size", "emc2_ffn_pack", "emc2_ffn", "emc2_ffn_work",
-           "emc2_ffn_backward"]
+           "emc2_ffn_backward", "emc2_causal_conv", "emc2_causal_conv_work", "emc2_causal_conv_backward", "emc2_causal_conv_step",
+           "emc2_gated_residual", "emc2_gated_residual_work", "emc2_gated_residual_backward"]
 
 
 class Emc2Error(RuntimeError):
@@ -180,6 +181,22 @@ def load_library() -> ctypes.CDLL:
     lib.emc2_ffn_work.argtypes = [ctypes.c_int, i64, i32, i32]
     lib.emc2_ffn_backward.restype = ctypes.c_int
     lib.emc2_ffn_backward.argtypes = [vp, ctypes.c_int, i32, vp, i64, vp, vp, i64, vp, i64, i32, i32, vp, i64, vp, vp, vp, vp, i64, vp]
+    lib.emc2_causal_conv.restype = ctypes.c_int
+    lib.emc2_causal_conv.argtypes = [vp, ctypes.c_int, vp, i64, vp, vp, i32, vp, i32, i64, i32, i32, i32, vp, vp, i64, vp, vp]
+    lib.emc2_causal_conv_work.restype = i64
+    lib.emc2_causal_conv_work.argtypes = [ctypes.c_int, i64, i32, i32]
+    lib.emc2_causal_conv_backward.restype = ctypes.c_int
+    lib.emc2_causal_conv_backward.argtypes = [vp, ctypes.c_int, vp, i64, vp, vp, i32, vp, i32, i64, i32, i32, i32, vp, vp, i64, vp, vp, i64, vp, vp,
+                                              vp, vp, i64, vp]
+    lib.emc2_causal_conv_step.restype = ctypes.c_int
+    lib.emc2_causal_conv_step.argtypes = [vp, ctypes.c_int, vp, i64, vp, vp, i32, vp, i64, i32, i32, vp, vp, i64, vp]
+    lib.emc2_gated_residual.restype = ctypes.c_int
+    lib.emc2_gated_residual.argtypes = [vp, ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, vp, vp, f32, vp, i64, i32, vp, i64, vp, i64, vp]
+    lib.emc2_gated_residual_work.restype = i64
+    lib.emc2_gated_residual_work.argtypes = [ctypes.c_int, i64, i32]
+    lib.emc2_gated_residual_backward.restype = ctypes.c_int
+    lib.emc2_gated_residual_backward.argtypes = [vp, ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, vp, vp, f32, vp, i64, vp, i64, vp, i64, i32, vp,
+                                                 i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp]
     _lib = lib
     return lib
 
@@ -808,3 +825,88 @@ class Context:
         size = _work_check(work, self.lib.emc2_ffn_work(dtype, rows, c, hidden))
         self._chk(self.lib.emc2_ffn_backward(self.h, dtype, activation, _at(x), ld[0], _at(packed), _at(dy), ld[1], _at(n), rows, c, hidden,
                                              _at(dx), ld[2], _at(dwg), _at(dwu), _at(dwd), _at(work), size, _raw_stream()))
+
+    def causal_conv(self, dtype: int, x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, y: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                    silu: bool = True, backwards: bool = False, before: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None) -> None:
+        """y_t = silu(bias + sum of w[k] x_{t-k}) along every sequence; w [taps][channels]; before and last [sequences][taps - 1][channels]: the rows
+        before each sequence's first and the last ones behind it, oldest first.  y must not overlap x, nor last before."""
+        like, rows, c = _rows_of(x, dtype)
+        ld = _pitch(x, like, "x"), _pitch(y, like, "y")
+        taps, n_seq = self._conv_check(w, bias, c, offsets, ((before, "before"), (last, "last")))
+        self._chk(self.lib.emc2_causal_conv(self.h, dtype, _at(x), ld[0], _at(w), _at(bias), int(bool(silu)), _at(offsets), n_seq, rows, c, taps,
+                                            int(bool(backwards)), _at(before), _at(y), ld[1], _at(last), _raw_stream()))
+
+    def _conv_check(self, w: torch.Tensor, bias: Optional[torch.Tensor], c: int, offsets: Optional[torch.Tensor], states: Sequence,
+                    n_seq: int = 0) -> Tuple[int, int]:
+        """Taps and number of sequences."""
+        taps = w.shape[0] if w.dim() == 2 else 0
+        _params_check(w, torch.float32, (taps, c), "w")
+        _params_check(bias, torch.float32, (c,), "bias")
+        if offsets is not None:
+            _dev_check(offsets, torch.int32, "offsets")
+            n_seq = offsets.numel() - 1
+        for t, nm in states:
+            _params_check(t, torch.float32, (n_seq, taps - 1, c), nm)
+        return taps, n_seq
+
+    def causal_conv_work(self, dtype: int, capacity: int, channels: int, taps: int) -> int:
+        return self.lib.emc2_causal_conv_work(dtype, capacity, channels, taps)
+
+    def causal_conv_backward(self, dtype: int, x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor,
+                             dw: torch.Tensor, work: torch.Tensor, bias: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                             silu: bool = True, backwards: bool = False, before: Optional[torch.Tensor] = None,
+                             dlast: Optional[torch.Tensor] = None, dbefore: Optional[torch.Tensor] = None) -> None:
+        """dx, dw, dbias and dbefore of a causal_conv of x for dy and the gradient of the rows kept; dx must not overlap x or dy."""
+        like, rows, c = _rows_of(x, dtype)
+        ld = _pitch(x, like, "x"), _pitch(dy, like, "dy"), _pitch(dx, like, "dx")
+        taps, n_seq = self._conv_check(w, bias, c, offsets, ((before, "before"), (dlast, "dlast"), (dbefore, "dbefore")))
+        _params_check(dw, torch.float32, (taps, c), "dw")
+        _params_check(dbias, torch.float32, (c,), "dbias")
+        size = _work_check(work, self.lib.emc2_causal_conv_work(dtype, rows, c, taps))
+        self._chk(self.lib.emc2_causal_conv_backward(self.h, dtype, _at(x), ld[0], _at(w), _at(bias), int(bool(silu)), _at(offsets), n_seq, rows, c,
+                                                     taps, int(bool(backwards)), _at(before), _at(dy), ld[1], _at(dlast), _at(dx), ld[2], _at(dw),
+                                                     _at(dbias), _at(dbefore), _at(work), size, _raw_stream()))
+
+    def causal_conv_step(self, dtype: int, x: torch.Tensor, w: torch.Tensor, state: torch.Tensor, state_out: torch.Tensor, y: torch.Tensor,
+                         bias: Optional[torch.Tensor] = None, silu: bool = True) -> None:
+        """One row per sequence; state [rows][taps - 1][channels]: the rows before, oldest first; state_out (may be state): moved on by the row."""
+        like, rows, c = _rows_of(x, dtype)
+        ld = _pitch(x, like, "x"), _pitch(y, like, "y")
+        taps, _ = self._conv_check(w, bias, c, None, ((state, "state"), (state_out, "state_out")), rows)
+        self._chk(self.lib.emc2_causal_conv_step(self.h, dtype, _at(x), ld[0], _at(w), _at(bias), int(bool(silu)), _at(state), rows, c, taps,
+                                                 _at(state_out), _at(y), ld[1], _raw_stream()))
+
+    def gated_residual(self, dtype: int, x: torch.Tensor, branch: torch.Tensor, post: torch.Tensor, scale: torch.Tensor, total: torch.Tensor,
+                       eps: float, gate: Optional[torch.Tensor] = None, next_gain: Optional[torch.Tensor] = None,
+                       y: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None) -> None:
+        """total = x + scale silu(gate) rms(branch) post and, if y is given, y = rms(total) next_gain; scale: one value; n: device count of the rows present."""
+        like, rows, c = _rows_of(x, dtype)
+        ld = (_pitch(x, like, "x"), _pitch(branch, like, "branch"), _pitch(gate, like, "gate"), _pitch(total, like, "total"), _pitch(y, like, "y"))
+        for t, shape, nm in ((post, (c,), "post"), (scale, (1,), "scale"), (next_gain, (c,), "next_gain")):
+            _params_check(t, torch.float32, shape, nm)
+        _count_check(n)
+        self._chk(self.lib.emc2_gated_residual(self.h, dtype, _at(x), ld[0], _at(branch), ld[1], _at(gate), ld[2], _at(post), _at(scale),
+                                               _at(next_gain), eps, _at(n), rows, c, _at(total), ld[3], _at(y), ld[4], _raw_stream()))
+
+    def gated_residual_work(self, dtype: int, capacity: int, channels: int) -> int:
+        return self.lib.emc2_gated_residual_work(dtype, capacity, channels)
+
+    def gated_residual_backward(self, dtype: int, x: torch.Tensor, branch: torch.Tensor, post: torch.Tensor, scale: torch.Tensor, eps: float,
+                                dtotal: Optional[torch.Tensor], dx: torch.Tensor, dbranch: torch.Tensor, dpost: torch.Tensor,
+                                dscale: torch.Tensor, work: torch.Tensor, gate: Optional[torch.Tensor] = None,
+                                dgate: Optional[torch.Tensor] = None, next_gain: Optional[torch.Tensor] = None,
+                                dy: Optional[torch.Tensor] = None, dnext: Optional[torch.Tensor] = None,
+                                n: Optional[torch.Tensor] = None) -> None:
+        """dx, dbranch, dgate, dpost, dscale and dnext of a gated_residual for dtotal and dy (either may be None)."""
+        like, rows, c = _rows_of(x, dtype)
+        ld = [_pitch(t, like, nm) for t, nm in ((x, "x"), (branch, "branch"), (gate, "gate"), (dtotal, "dtotal"), (dy, "dy"), (dx, "dx"),
+                                                (dbranch, "dbranch"), (dgate, "dgate"))]
+        for t, shape, nm in ((post, (c,), "post"), (scale, (1,), "scale"), (next_gain, (c,), "next_gain"), (dpost, (c,), "dpost"),
+                             (dscale, (1,), "dscale"), (dnext, (c,), "dnext")):
+            _params_check(t, torch.float32, shape, nm)
+        _count_check(n)
+        size = _work_check(work, self.lib.emc2_gated_residual_work(dtype, rows, c))
+        self._chk(self.lib.emc2_gated_residual_backward(self.h, dtype, _at(x), ld[0], _at(branch), ld[1], _at(gate), ld[2], _at(post), _at(scale),
+                                                        _at(next_gain), eps, _at(dtotal), ld[3], _at(dy), ld[4], _at(n), rows, c, _at(dx), ld[5],
+                                                        _at(dbranch), ld[6], _at(dgate), ld[7], _at(dpost), _at(dscale), _at(dnext), _at(work),
+                                                        size, _raw_stream()))

@@ -8,41 +8,9 @@
 // launch in a fixed order (fp32 throughout, no atomics: equal inputs give equal bits).
 // Both are bound by memory: 613 k x 64 f16 with residual and sum 63 us, 5.0 TB/s of what it has to move (a copy of that size reaches 5.0); forward and
 // backward pass of 240 k x 128 bf16 68 us, 4.5 TB/s.
-#include "rows.h"
+#include "row_lanes.h"
 
 namespace {
-
-constexpr int kThreads = 256;
-constexpr int kMaxChannels = 1024;
-
-template <int L> __device__ __forceinline__ float lane_sum(float v) {
-#pragma unroll
-  for (int d = 1; d < L; d <<= 1) v += __shfl_xor(v, d, 64);
-  return v;
-}
-
-// A lane's vectors: vector v begins at channel at[v] (-1: there is none).  A row whose length is no multiple of N (MOVED) ends with a vector moved
-// back over its neighbour: the first twice[v] of its values are that one's too, computed alike by both and counted by one.
-template <int N, int L, int V, bool MOVED> struct Places {
-  int32_t at[V], twice[V];
-  __device__ __forceinline__ Places(int32_t channels, int sub) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int32_t c = (v * L + sub) * N;
-      at[v] = c >= channels ? -1 : !MOVED || c + N <= channels ? c : channels - N;
-      twice[v] = at[v] >= 0 ? c - at[v] : 0;
-    }
-  }
-  // The sum of the values that the lane counts.
-  __device__ __forceinline__ float sum(const emc2_fvec<N> (&x)[V]) const {
-    float s = 0.0f;
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-      for (int e = 0; e < N; ++e) s += MOVED && e < twice[v] ? 0.0f : x[v][e];
-    return s;
-  }
-};
 
 struct NormArgs {
   const void *x, *res, *dy;      // res: forward: the residual; backward: added to dx.  May be null
@@ -190,15 +158,6 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 5 : 2) k_layernorm_grad(con
     }
 }
 
-// The sum of N values by halves: log2(N) additions behind each, where one after the other would be up to N.
-template <int N> __device__ __forceinline__ float sum_by_halves(float (&v)[N]) {
-#pragma unroll
-  for (int d = N / 2; d > 0; d /= 2)
-#pragma unroll
-    for (int i = 0; i < d; ++i) v[i] += v[i + d];
-  return v[0];
-}
-
 // dgamma and dbeta from the blocks' sums: 32 columns a block, 32 threads a column, each with eight loads under way (beyond the last sum: of the last one
 // again, not counted; 1251 sums of 180 columns 4.9 us, 0.5 more with the last ones loaded in a row).  Added by halves: of 1280 sums none has more than
 // 13 additions behind it.
@@ -225,49 +184,6 @@ __global__ void __launch_bounds__(1024) k_layernorm_weights(const float* __restr
     for (int i = 0; i < 32; ++i) v[i] = part[i][threadIdx.x];
     (col < channels ? dgamma[col] : dbeta[col - channels]) = sum_by_halves(v);
   }
-}
-
-// How the rows of a call lie over the lanes: vectors of 16 bytes, single values where a row has not even one.
-struct Shape { bool wide, moved; int lanes, vectors; };
-Shape shape_of(emc2_dtype dtype, int32_t channels) {
-  const int whole = dtype == EMC2_F32 ? 4 : 8, per = channels >= whole ? whole : 1;
-  const int pieces = (channels + per - 1) / per;
-  int lanes = 8;
-  while (lanes < 64 && lanes < pieces) lanes *= 2;
-  int vectors = 1;
-  while (vectors * lanes < pieces) vectors *= 2;
-  return {per > 1, channels % per != 0, lanes, vectors};
-}
-
-// Calls f with the compile-time form (values a vector, lanes, vectors, rows at a time) of a shape.  Against one value a lane where rows are not whole
-// vectors: 200 k x 47 f16 forward and backward 94 us, 32 with a last vector moved back.
-template <int N, int L, int V, int U, bool MOVED = false> struct Form {
-  static constexpr int n = N, l = L, v = V, u = U;
-  static constexpr bool moved = MOVED;
-};
-template <int N, bool MOVED, typename F> void with_form(const Shape& s, F&& f) {
-  switch (s.lanes) {
-    case 8: return f(Form<N, 8, 1, 4, MOVED>());
-    case 16: return f(Form<N, 16, 1, 4, MOVED>());
-    case 32: return f(Form<N, 32, 1, 4, MOVED>());
-  }
-  switch (s.vectors) {
-    case 1: return f(Form<N, 64, 1, 2, MOVED>());
-    case 2: return f(Form<N, 64, 2, 1, MOVED>());
-  }
-  if constexpr (N == 4) return f(Form<N, 64, 4, 1, MOVED>());
-}
-template <typename T, typename F> void with_type(const Shape& s, F&& f) {
-  constexpr int N = 16 / sizeof(T);
-  const auto with_T = [&](auto form) { f(form, T()); };
-  if (!s.wide) with_T(Form<1, 8, 1, 4>());
-  else if (s.moved) with_form<N, true>(s, with_T);
-  else with_form<N, false>(s, with_T);
-}
-template <typename F> void with_type(emc2_dtype dtype, const Shape& s, F&& f) {
-  if (dtype == EMC2_F32) with_type<float>(s, f);
-  else if (dtype == EMC2_F16) with_type<_Float16>(s, f);
-  else with_type<__bf16>(s, f);
 }
 
 // Blocks of the backward pass, each walking the rows in steps of all blocks: about as many as the chip holds at once (a lane's sums and one row of 16

@@ -65,3 +65,36 @@ static inline bool emc2_rows_ok(const void* p, int64_t pitch, int32_t channels, 
 }
 static inline size_t emc2_size_of(emc2_dtype dtype) { return dtype == EMC2_F32 ? 4 : 2; }
 static inline bool emc2_is_float(emc2_dtype dtype) { return dtype == EMC2_F32 || dtype == EMC2_F16 || dtype == EMC2_BF16; }
+
+// A call's rows as its checks see them.
+struct emc2_rows {
+  const void* p;
+  int64_t ld;
+  int32_t width;
+};
+// No value of one is a value of the other: `n` rows each, apart in memory, or side by side in rows of the same pitch.
+static inline bool emc2_apart(const emc2_rows& a, const emc2_rows& b, int64_t n, size_t size) {
+  if (!a.p || !b.p || n <= 0) return true;
+  const uintptr_t p = (uintptr_t)a.p, q = (uintptr_t)b.p;
+  const uintptr_t p_end = p + ((n - 1) * a.ld + a.width) * size, q_end = q + ((n - 1) * b.ld + b.width) * size;
+  if (p_end <= q || q_end <= p) return true;
+  if (a.ld != b.ld) return false;
+  const uintptr_t pitch = a.ld * size, off = p <= q ? (q - p) % pitch : (p - q) % pitch;
+  const uintptr_t first = (p <= q ? a.width : b.width) * size, second = (p <= q ? b.width : a.width) * size;
+  return off >= first && off + second <= pitch;
+}
+static inline bool emc2_same(const emc2_rows& a, const emc2_rows& b) { return a.p == b.p && a.ld == b.ld; }
+// Results (`outs`) lie apart from each other, and from each input either apart or, where `in_place` allows it, in its very place.
+static inline bool emc2_results_ok(const emc2_rows* outs, int n_outs, const emc2_rows* ins, int n_ins, int64_t n, size_t size, bool in_place) {
+  for (int i = 0; i < n_outs; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (!emc2_apart(outs[i], outs[j], n, size)) return false;
+    for (int j = 0; j < n_ins; ++j)
+      if (!emc2_apart(outs[i], ins[j], n, size) && !(in_place && emc2_same(outs[i], ins[j]))) return false;
+  }
+  return true;
+}
+// Contiguous values of floats lie apart.
+static inline bool emc2_apart(const float* a, int64_t n_a, const float* b, int64_t n_b) {
+  return !a || !b || a + n_a <= b || b + n_b <= a;
+}
