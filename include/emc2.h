@@ -593,6 +593,37 @@ emc2_status emc2_causal_conv_step(emc2_ctx* ctx, emc2_dtype dtype, const void* d
                                   int64_t ld_y, void* stream);
 
 /*
+ * Selective state space scan along the rows of every sequence: per channel c a state of `states` values that the rows' own steps, B and C steer,
+ *   D_t[c] = log(1 + exp(dt_t[c] + dt_bias[c]));  h_t[c][n] = exp(D_t[c] a[c][n]) h_{t-1}[c][n] + D_t[c] x_t[c] B_t[n]
+ *   y_t[c] = sum over n of C_t[n] h_t[c][n] + skip[c] x_t[c]
+ * Sequences, d_offsets and `backwards` as for emc2_recurrence.  d_x, d_dt, d_y rows of `channels` values, d_b and d_c of `states`, which all channels share (several
+ * groups of channels with their own B and C: one call each).  d_a [channels][states], usually negative; d_skip and d_dt_bias [channels], NULL = 0.
+ * d_h0 [n_seq][channels][states] states before the first row, NULL = zeros; d_last receives the states after the last (an empty sequence's is its d_h0), NULL to
+ * skip.  States are fp32 throughout, and a sequence's reach no other sequence.  channels in [1, 65536], states in [1, 64].
+ * d_y may lie where d_x or d_dt does (as d_dx and d_ddt below may where d_x, d_dt or d_dy do); d_last must not overlap d_h0, nor d_dh0 d_h0 or d_dlast.
+ * Other overlaps are refused.
+ */
+int64_t emc2_selective_scan_work(emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t states);
+emc2_status emc2_selective_scan(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_dt, int64_t ld_dt, const float* d_a,
+                                const void* d_b, int64_t ld_b, const void* d_c, int64_t ld_c, const float* d_skip, const float* d_dt_bias,
+                                const int32_t* d_offsets, int32_t n_seq, int64_t capacity, int32_t channels, int32_t states, int32_t backwards,
+                                const float* d_h0, void* d_y, int64_t ld_y, float* d_last, void* d_work, int64_t work_bytes, void* stream);
+/* Its gradients for dy and d_dlast (of the last states, NULL = zeros): rows dx, ddt, db, dc; da, and dskip, ddt_bias (NULL to skip; dskip needs d_skip) summed
+ * over the rows; d_dh0 (NULL to skip).  The states are computed again; nothing but the call's own inputs is needed. */
+emc2_status emc2_selective_scan_backward(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_dt, int64_t ld_dt,
+                                         const float* d_a, const void* d_b, int64_t ld_b, const void* d_c, int64_t ld_c, const float* d_skip,
+                                         const float* d_dt_bias, const int32_t* d_offsets, int32_t n_seq, int64_t capacity, int32_t channels,
+                                         int32_t states, int32_t backwards, const float* d_h0, const void* d_dy, int64_t ld_dy,
+                                         const float* d_dlast, void* d_dx, int64_t ld_dx, void* d_ddt, int64_t ld_ddt, float* d_da, void* d_db,
+                                         int64_t ld_db, void* d_dc, int64_t ld_dc, float* d_dskip, float* d_ddt_bias, float* d_dh0, void* d_work,
+                                         int64_t work_bytes, void* stream);
+/* The scan for one row per sequence (serving a stream): d_h_out [rows][channels][states] (may be d_h) receives the states moved on by the row. */
+emc2_status emc2_selective_scan_step(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_dt, int64_t ld_dt,
+                                     const float* d_a, const void* d_b, int64_t ld_b, const void* d_c, int64_t ld_c, const float* d_skip,
+                                     const float* d_dt_bias, const float* d_h, int64_t rows, int32_t channels, int32_t states, float* d_h_out,
+                                     void* d_y, int64_t ld_y, void* stream);
+
+/*
  * From a block's result to the next block's input, per row: the norm behind the block, its gate, the scale of the residual branch, the residual sum, and the
  * norm before the next block:
  *   sum = x + scale * act * rms(branch) * post;   y = rms(sum) * next;   rms(v) = v / sqrt(mean of v^2 + eps), act = gate / (1 + exp(-gate))

@@ -37,7 +37,8 @@ EXPORTS = ["emc2_create", "emc2_destroy", "emc2_status_sync", "emc2_last_error",
            "emc2_frame_offsets", "emc2_layernorm", "emc2_layernorm_work", "emc2_layernorm_backward", "emc2_recurrence", "emc2_recurrence_work",
            "emc2_recurrence_backward", "emc2_recurrence_step", "emc2_ffn_packed_size", "emc2_ffn_pack", "emc2_ffn", "emc2_ffn_work",
            "emc2_ffn_backward", "emc2_causal_conv", "emc2_causal_conv_work", "emc2_causal_conv_backward", "emc2_causal_conv_step",
-           "emc2_gated_residual", "emc2_gated_residual_work", "emc2_gated_residual_backward"]
+           "emc2_gated_residual", "emc2_gated_residual_work", "emc2_gated_residual_backward",
+           "emc2_selective_scan", "emc2_selective_scan_work", "emc2_selective_scan_backward", "emc2_selective_scan_step"]
 
 
 class Emc2Error(RuntimeError):
@@ -197,6 +198,16 @@ def load_library() -> ctypes.CDLL:
     lib.emc2_gated_residual_backward.restype = ctypes.c_int
     lib.emc2_gated_residual_backward.argtypes = [vp, ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, vp, vp, f32, vp, i64, vp, i64, vp, i64, i32, vp,
                                                  i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp]
+    scan = [vp, ctypes.c_int, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp]
+    lib.emc2_selective_scan.restype = ctypes.c_int
+    lib.emc2_selective_scan.argtypes = scan + [vp, i32, i64, i32, i32, i32, vp, vp, i64, vp, vp, i64, vp]
+    lib.emc2_selective_scan_work.restype = i64
+    lib.emc2_selective_scan_work.argtypes = [ctypes.c_int, i64, i32, i32]
+    lib.emc2_selective_scan_backward.restype = ctypes.c_int
+    lib.emc2_selective_scan_backward.argtypes = scan + [vp, i32, i64, i32, i32, i32, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp,
+                                                        vp, i64, vp]
+    lib.emc2_selective_scan_step.restype = ctypes.c_int
+    lib.emc2_selective_scan_step.argtypes = scan + [vp, i64, i32, i32, vp, vp, i64, vp]
     _lib = lib
     return lib
 
@@ -910,3 +921,62 @@ class Context:
                                                         _at(next_gain), eps, _at(dtotal), ld[3], _at(dy), ld[4], _at(n), rows, c, _at(dx), ld[5],
                                                         _at(dbranch), ld[6], _at(dgate), ld[7], _at(dpost), _at(dscale), _at(dnext), _at(work),
                                                         size, _raw_stream()))
+
+    def _scan_check(self, dtype: int, x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor,
+                    skip: Optional[torch.Tensor], dt_bias: Optional[torch.Tensor]) -> Tuple[tuple, tuple, list]:
+        """What rows of channels and rows of states look like, and the arguments that all calls of the scan begin with."""
+        like, rows, ch = _rows_of(x, dtype)
+        m = a.shape[1] if a.dim() == 2 else 0
+        _params_check(a, torch.float32, (ch, m), "a")
+        shared = (True, like[1], torch.Size((rows, m)))
+        for t, nm in ((skip, "skip"), (dt_bias, "dt_bias")):
+            _params_check(t, torch.float32, (ch,), nm)
+        return like, shared, [self.h, dtype, _at(x), _pitch(x, like, "x"), _at(dt), _pitch(dt, like, "dt"), _at(a), _at(b), _pitch(b, shared, "b"), _at(c),
+                              _pitch(c, shared, "c"), _at(skip), _at(dt_bias)]
+
+    def selective_scan_work(self, dtype: int, capacity: int, channels: int, states: int) -> int:
+        return self.lib.emc2_selective_scan_work(dtype, capacity, channels, states)
+
+    def selective_scan(self, dtype: int, x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor, offsets: torch.Tensor,
+                       y: torch.Tensor, work: torch.Tensor, skip: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None,
+                       backwards: bool = False, h0: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None) -> None:
+        """h_t = exp(D_t a) h_{t-1} + D_t x_t b_t and y_t = c_t . h_t + skip x_t along every sequence, D = softplus(dt + dt_bias); x, dt, y rows of channels,
+        b, c rows of states, a [channels][states], h0 and last [sequences][channels][states].  `last` must not overlap h0."""
+        like, shared, args = self._scan_check(dtype, x, dt, a, b, c, skip, dt_bias)
+        ld = _pitch(y, like, "y")
+        _dev_check(offsets, torch.int32, "offsets")
+        n_seq, rows, (ch, m) = offsets.numel() - 1, like[2][0], a.shape
+        _params_check(h0, torch.float32, (n_seq, ch, m), "h0")
+        _params_check(last, torch.float32, (n_seq, ch, m), "last")
+        size = _work_check(work, self.lib.emc2_selective_scan_work(dtype, rows, ch, m))
+        self._chk(self.lib.emc2_selective_scan(*args, _at(offsets), n_seq, rows, ch, m, int(bool(backwards)), _at(h0), _at(y), ld, _at(last), _at(work), size,
+                                               _raw_stream()))
+
+    def selective_scan_backward(self, dtype: int, x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor,
+                                offsets: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor, ddt: torch.Tensor, da: torch.Tensor, db: torch.Tensor,
+                                dc: torch.Tensor, work: torch.Tensor, skip: Optional[torch.Tensor] = None, dskip: Optional[torch.Tensor] = None,
+                                dt_bias: Optional[torch.Tensor] = None, ddt_bias: Optional[torch.Tensor] = None, backwards: bool = False,
+                                h0: Optional[torch.Tensor] = None, dlast: Optional[torch.Tensor] = None,
+                                dh0: Optional[torch.Tensor] = None) -> None:
+        """The gradients of a selective_scan for dy and the gradient of the last states; dh0 must not overlap dlast or h0."""
+        like, shared, args = self._scan_check(dtype, x, dt, a, b, c, skip, dt_bias)
+        ld = [_pitch(t, s, nm) for t, s, nm in ((dy, like, "dy"), (dx, like, "dx"), (ddt, like, "ddt"), (db, shared, "db"), (dc, shared, "dc"))]
+        _dev_check(offsets, torch.int32, "offsets")
+        n_seq, rows, (ch, m) = offsets.numel() - 1, like[2][0], a.shape
+        for t, shape, nm in ((da, (ch, m), "da"), (dskip, (ch,), "dskip"), (ddt_bias, (ch,), "ddt_bias"), (h0, (n_seq, ch, m), "h0"),
+                             (dlast, (n_seq, ch, m), "dlast"), (dh0, (n_seq, ch, m), "dh0")):
+            _params_check(t, torch.float32, shape, nm)
+        size = _work_check(work, self.lib.emc2_selective_scan_work(dtype, rows, ch, m))
+        self._chk(self.lib.emc2_selective_scan_backward(*args, _at(offsets), n_seq, rows, ch, m, int(bool(backwards)), _at(h0), _at(dy), ld[0], _at(dlast),
+                                                        _at(dx), ld[1], _at(ddt), ld[2], _at(da), _at(db), ld[3], _at(dc), ld[4], _at(dskip),
+                                                        _at(ddt_bias), _at(dh0), _at(work), size, _raw_stream()))
+
+    def selective_scan_step(self, dtype: int, x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor, h: torch.Tensor,
+                            h_out: torch.Tensor, y: torch.Tensor, skip: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None) -> None:
+        """One row per sequence: the states h [rows][channels][states] moved on by the row, to h_out (may be h), and y."""
+        like, _, args = self._scan_check(dtype, x, dt, a, b, c, skip, dt_bias)
+        ld = _pitch(y, like, "y")
+        rows, (ch, m) = like[2][0], a.shape
+        _params_check(h, torch.float32, (rows, ch, m), "h")
+        _params_check(h_out, torch.float32, (rows, ch, m), "h_out")
+        self._chk(self.lib.emc2_selective_scan_step(*args, _at(h), rows, ch, m, _at(h_out), _at(y), ld, _raw_stream()))

@@ -1,0 +1,278 @@
+// What the kernels of the selective scan (selective_scan.hip, selective_scan_grad.hip) share: how states lie over lanes, the rows' way into registers and
+// LDS, steps and decays, and the totals of runs of rows.
+#pragma once
+#include "rows.h"
+#include "sequences.h"
+
+struct emc2_scan_args {
+  const void *x, *dt, *b, *c, *dy;
+  const float *a, *skip, *dt_bias, *h0, *dlast;   // skip, dt_bias, h0, dlast may be null
+  const int32_t* offsets;
+  void *y, *ddt, *db, *dc;                     // y: forward: y; backward: dx
+  float *last, *dh0;                           // may be null
+  // totals of chunks and spans (forward; in gradients also of the flow towards earlier rows), what enters each span, the state before every batch
+  float *chunk_s[2], *chunk_h[2], *span_s[2], *span_h[2], *enter[2], *batch_s, *batch_h;
+  float *partial, *partial_bc;                 // weights' sums per chunk; sums of dB and dC per part of the channels
+  int32_t* flags;
+  int64_t ld_x, ld_dt, ld_b, ld_c, ld_dy, ld_y, ld_ddt, ld_db, ld_dc;
+  int32_t capacity, channels, states, n_seq, backwards;
+  int32_t chunk, row_blocks, totals;           // rows of a chunk; blocks that walk rows; whether a first launch was needed
+};
+
+namespace {
+
+constexpr int kBatch = 8;                // rows under way together
+constexpr int kChunkWaves = 8;           // chunks side by side in a block of the launch that reduces them: a block's total stands for them ("span")
+constexpr int kMaxChunks = 4096;         // chunks of a call times slices of its channels, and
+constexpr int kMinChunk = 16;            // rows of a chunk at least
+constexpr int kMaxSpans = kMaxChunks / kChunkWaves;
+constexpr int kMaxStates = 64;
+
+typedef emc2_scan_args ScanArgs;
+
+// A lane has S neighbouring states of one channel; P lanes side by side have a channel's states, 64 / P channels lie in a wave.
+template <int S, int P> struct States {
+  static constexpr int kWidth = S * P, kChannels = 64 / P;
+  int32_t lane, wave, part, channel, first, there;   // first: of its states; there: how many of them there are (0 without a channel)
+  bool in;
+  __device__ __forceinline__ States(const ScanArgs& a, int32_t slice) {
+    lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    part = lane & (P - 1);
+    channel = slice * kChannels + lane / P;
+    in = channel < a.channels;
+    if (!in) channel = 0;
+    first = part * S;
+    const int32_t left = a.states - first;
+    there = !in || left < 0 ? 0 : left < S ? left : S;
+  }
+  // The lane's values of a line [channels][states].
+  __device__ __forceinline__ void load(const ScanArgs& a, const float* line, float (&v)[S]) const {
+    const float* const p = line + (int64_t)channel * a.states + first;
+    if (there == S) {
+#pragma unroll
+      for (int i = 0; i < S; i += 4) {
+        const emc2_fvec<4> q = emc2_load<4>(p + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i + e] = q[e];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < S; ++i) v[i] = i < there ? p[i] : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void load_or_zero(const ScanArgs& a, const float* lines, int64_t line, float (&v)[S]) const {
+    if (lines) return load(a, lines + line * a.channels * a.states, v);
+#pragma unroll
+    for (int i = 0; i < S; ++i) v[i] = 0.0f;
+  }
+  __device__ __forceinline__ void store(const ScanArgs& a, float* lines, int64_t line, const float (&v)[S]) const {
+    float* const p = lines + (line * a.channels + channel) * a.states + first;
+    if (there == S) {
+#pragma unroll
+      for (int i = 0; i < S; i += 4) emc2_store<4>(p + i, emc2_fvec<4>{v[i], v[i + 1], v[i + 2], v[i + 3]});
+    } else {
+#pragma unroll
+      for (int i = 0; i < S; ++i)
+        if (i < there) p[i] = v[i];
+    }
+  }
+};
+
+// Sums over the P lanes of a channel, in all of them.
+template <int CTRL> __device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int P> __device__ __forceinline__ float part_sum(float v) {
+  if constexpr (P > 1) v += moved<0xB1>(v);                // quad_perm: lane ^ 1
+  if constexpr (P > 2) v += moved<0x4E>(v);                // lane ^ 2
+  if constexpr (P > 4) v += moved<0x141>(v);               // mirrored within eight lanes, whose halves are uniform by now
+  if constexpr (P > 8) v += moved<0x140>(v);               // mirrored within sixteen
+  return v;
+}
+
+// Steps: softplus(v) = log(1 + e), e = exp(v), and its slope e / (1 + e).  u = 1 + e is rounded; log(1 + e) = log(u) + (e - (u - 1)) / u to second order, so
+// that steps far below 1 keep their places.  Beyond 20 the logarithm is v itself, to 2e-9.
+template <bool EXACT> __device__ __forceinline__ void step_of(float v, float& d, float& slope) {
+  float t;
+  const float e = emc2_exp_of_minus<EXACT>(-v, t), u = 1.0f + e, r = __builtin_amdgcn_rcpf(u);
+  const float l = __builtin_fmaf(__builtin_amdgcn_logf(u), 0.693147180559945309f, (e - (u - 1.0f)) * r);
+  d = v > 20.0f ? v : l;
+  slope = v > 20.0f ? 1.0f : e * r;
+}
+constexpr float kLog2e = 1.44269504088896341f;
+
+// Sequences from a row on, by a window of 64 starts in the wave's lanes.
+struct Cursor {
+  int32_t j, next;                       // the sequence at hand and the row at which the one behind it starts
+  int32_t base, mine;                    // of the window: its first sequence, the lane's start
+  __device__ __forceinline__ void fill(const Walk& w, int32_t from, int lane) {
+    base = from > 0 ? from : 0;
+    mine = base + lane <= w.n_seq ? w.start(base + lane) : 0x7fffffff;
+  }
+  __device__ __forceinline__ int count(const Walk& w, int32_t r, int lane) const { return __popcll(__ballot(base + lane < w.n_seq && mine <= r)); }
+  // The sequence of row r in [0, n).
+  __device__ __forceinline__ void locate(const Walk& w, int32_t r, int lane) {
+    int c = count(w, r, lane);
+    if ((c == 0 && base > 0) || c == 64) {
+      fill(w, w.find(r, lane) - 31, lane);
+      c = count(w, r, lane);
+    }
+    c = c < 1 ? 1 : c < 63 ? c : 63;
+    j = __builtin_amdgcn_readfirstlane(base + c - 1);
+    next = __builtin_amdgcn_readlane(mine, c);
+  }
+  // Before row r: a sequence that starts with it is still to come.
+  __device__ __forceinline__ void open(const Walk& w, int32_t r, int lane) {
+    fill(w, w.find(r, lane) - 31, lane);
+    before(w, r, lane);
+  }
+  __device__ __forceinline__ void before(const Walk& w, int32_t r, int lane) {
+    locate(w, r, lane);
+    if (__builtin_amdgcn_readlane(mine, j - base) >= r) next = r;
+  }
+};
+
+// B and C of a batch, ARRAYS of them: pieces of PV values in registers on their way from memory, floats in LDS.  `threads` threads, at least 64, share them out.
+template <typename T, int WIDTH, int ARRAYS> struct Staged {
+  static constexpr int kWhole = 16 / sizeof(T), PV = kWhole < WIDTH ? kWhole : WIDTH, kARow = WIDTH / PV, kAll = ARRAYS * kBatch * kARow,
+                       kMine = (kAll + 63) / 64;
+  emc2_vec<T, PV> v[kMine];
+  // Rows of the batch at r0 that are none (at `end` or beyond) and states that are none become 0.
+  __device__ __forceinline__ void fetch(const ScanArgs& a, const Walk& w, int32_t r0, int32_t end, int thread, int threads = 64) {
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      const int id = q * threads + thread, array = id / (kBatch * kARow), in = id % (kBatch * kARow), n = in % kARow * PV;
+      const int32_t r = r0 + in / kARow;
+      v[q] = (T)0.0f;
+      if (id < kAll && r < end) {
+        const T* const p = (array == 0 ? (const T*)a.b + w.row(r) * a.ld_b : (const T*)a.c + w.row(r) * a.ld_c) + n;
+        if (n + PV <= a.states) {
+          v[q] = emc2_piece<PV>(p);
+        } else {
+#pragma unroll
+          for (int e = 0; e < PV; ++e)
+            if (n + e < a.states) v[q][e] = p[e];
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void put(float* to, int thread, int threads = 64) const {   // to [ARRAYS][kBatch][WIDTH]
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      const int id = q * threads + thread;
+      if (id < kAll) {
+        const emc2_fvec<PV> f = __builtin_convertvector(v[q], emc2_fvec<PV>);
+#pragma unroll
+        for (int e = 0; e < PV; e += 4) *reinterpret_cast<emc2_fvec<4>*>(to + id * PV + e) = emc2_fvec<4>{f[e], f[e + 1], f[e + 2], f[e + 3]};
+      }
+    }
+  }
+};
+template <int S> __device__ __forceinline__ void from_lds(const float* p, float (&v)[S]) {
+#pragma unroll
+  for (int i = 0; i < S; i += 4) {
+    const emc2_fvec<4> q = *reinterpret_cast<const emc2_fvec<4>*>(p + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[i + e] = q[e];
+  }
+}
+
+// Values of one channel in the rows of a batch; rows that are none read valid places.
+template <typename T> struct Column {
+  T v[kBatch];
+  __device__ __forceinline__ void fetch(const Walk& w, const void* p, int64_t ld, int32_t channel, int32_t r0) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) v[i] = ((const T*)p + w.row(r0 + i < w.n ? r0 + i : w.n - 1) * ld)[channel];
+  }
+};
+
+// A times log2(e): the rows' decays are powers of two.
+template <int S, int P> __device__ __forceinline__ void decays(const ScanArgs& a, const States<S, P>& t, float (&a2)[S]) {
+  t.load(a, a.a, a2);
+#pragma unroll
+  for (int s = 0; s < S; ++s) a2[s] *= kLog2e;
+}
+
+// `h` behind a run of rows that multiply a state by exp(A s) and add `t`; s < 0: a sequence begins in the run, and nothing from before it is left.
+template <int S> __device__ __forceinline__ void through(const float (&a2)[S], float s, const float (&t)[S], float (&h)[S]) {
+#pragma unroll
+  for (int i = 0; i < S; ++i) h[i] = s < 0.0f ? t[i] : __builtin_fmaf(__builtin_amdgcn_exp2f(a2[i] * s), h[i], t[i]);
+}
+
+// One direction of what a block's chunks make of a state together: chunk after chunk, in the order of the direction.
+struct Spans { int32_t spans, chunks; };
+__device__ __forceinline__ Spans spans_of(const ScanArgs& a, int32_t n) {
+  const int32_t chunks = (int32_t)(((int64_t)n + a.chunk - 1) / a.chunk);
+  return {(chunks + kChunkWaves - 1) / kChunkWaves, chunks};
+}
+
+// The state that enters chunk `k` (direction 0), or the flow that enters it from later rows (1): what enters its span, then the chunks of the span before it.
+template <int DIR, int S, int P>
+__device__ __forceinline__ void entering(const ScanArgs& a, const States<S, P>& t, const float (&a2)[S], int32_t k, const Spans& q, float (&h)[S]) {
+  const int32_t span = k / kChunkWaves, lo = span * kChunkWaves, hi = lo + kChunkWaves < q.chunks ? lo + kChunkWaves : q.chunks;
+  if (q.spans > 1) t.load(a, a.enter[DIR] + (int64_t)span * a.channels * a.states, h);
+  else {
+#pragma unroll
+    for (int i = 0; i < S; ++i) h[i] = 0.0f;
+  }
+  for (int32_t m = DIR == 0 ? lo : hi - 1; m != k; m += DIR == 0 ? 1 : -1) {
+    float v[S];
+    t.load(a, a.chunk_h[DIR] + (int64_t)m * a.channels * a.states, v);
+    through<S>(a2, a.chunk_s[DIR][(int64_t)m * a.channels + t.channel], v, h);
+  }
+}
+
+// Sequences without rows hand their states on; blocks of their own, a sequence at a time.
+__device__ __forceinline__ void hand_on(const ScanArgs& a, const Walk& w, const float* from, float* to) {
+  const int64_t size = (int64_t)a.channels * a.states, step = (int64_t)(gridDim.x - a.row_blocks) * gridDim.y;
+  for (int64_t j = (int64_t)(blockIdx.x - a.row_blocks) * gridDim.y + blockIdx.y; j < a.n_seq; j += step) {
+    if (w.start((int32_t)j + 1) > w.start((int32_t)j)) continue;
+    const int64_t at = w.number((int32_t)j) * size;
+    for (int64_t i = threadIdx.x; i < size; i += blockDim.x) to[at + i] = from ? from[at + i] : 0.0f;
+  }
+}
+
+template <typename F> void with_type(emc2_dtype dtype, F&& f) {
+  if (dtype == EMC2_F32) f(float());
+  else if (dtype == EMC2_F16) f(_Float16());
+  else f(__bf16());
+}
+template <int S, int P> struct Form { static constexpr int s = S, p = P; };
+
+}  // namespace
+
+// How a call is cut (host).
+struct emc2_scan_plan {
+  int32_t chunk, chunks, spans;          // rows of a chunk; chunks and spans of the capacity
+  int64_t most;                          // chunks that no call of up to that many rows exceeds
+};
+static inline emc2_scan_plan emc2_plan_scan(int64_t capacity, int32_t channels) {
+  const int64_t slices = emc2_div_up(channels, 64), room = slices < kMaxChunks ? kMaxChunks / slices : 1;
+  emc2_scan_plan p;
+  const int64_t per = emc2_div_up(capacity, room);
+  p.chunk = (int32_t)(per < kMinChunk ? kMinChunk : emc2_div_up(per, kBatch) * kBatch);
+  p.chunks = (int32_t)emc2_div_up(capacity, p.chunk);
+  p.spans = (int32_t)emc2_div_up(p.chunks, kChunkWaves);
+  const int64_t some = emc2_div_up(capacity, kMinChunk);
+  p.most = some < room ? some : room;
+  return p;
+}
+// Totals of chunks and spans in one direction, and what enters the spans: floats.
+static inline int64_t emc2_scan_totals_size(int64_t chunks, int32_t channels, int32_t states) {
+  const int64_t spans = emc2_div_up(chunks, kChunkWaves);
+  return ((chunks + spans) * (states + 1) + spans * states) * channels;
+}
+static inline float* emc2_place_totals(ScanArgs& a, int dir, float* at, const emc2_scan_plan& p) {
+  const int64_t c = a.channels, cn = c * a.states;
+  a.chunk_h[dir] = at, at += p.chunks * cn;
+  a.span_h[dir] = at, at += p.spans * cn;
+  a.enter[dir] = at, at += p.spans * cn;
+  a.chunk_s[dir] = at, at += p.chunks * c;
+  a.span_s[dir] = at, at += p.spans * c;
+  return at;
+}
+// Launches the reduction of chunks and what enters the spans (selective_scan.hip); `grad`: of both directions, with the states before every batch.
+void emc2_scan_totals(const ScanArgs& a, emc2_dtype dtype, const emc2_scan_plan& p, bool grad, hipStream_t stream);
+// Refuses what both directions refuse.
+emc2_status emc2_scan_check(emc2_ctx* ctx, const char* what, emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t states);

@@ -1,0 +1,462 @@
+// Selective state space scan along the rows of packed sequences, and its form for one row per sequence.
+//   D_t = softplus(dt_t + dt_bias);  h_t[c][n] = exp(D_t[c] A[c][n]) h_{t-1}[c][n] + D_t[c] x_t[c] B_t[n];  y_t[c] = sum over n of C_t[n] h_t[c][n] + skip[c] x_t[c]
+// Rows map a state h to exp(A D) h + add, and runs of rows to exp(A (sum of D)) h + total: of a run, one sum a channel and one total a state are kept.
+// A long list of rows is cut into chunks that are worked on side by side: a first launch walks every chunk from a state of zeros (k_scan_totals), a second
+// composes the totals of spans of eight chunks (k_scan_enter), the third walks every chunk from the state that enters it (k_scan).  Short calls do all of it in
+// one block a slice of the channels (k_scan_short).  A sequence's first row takes the given state whatever lies before it, so sequences of any length share
+// a chunk, and nothing from one reaches another.
+// A lane holds S states of a channel and walks rows one after the other; x and dt of the next rows are on their way in registers, B and C, which all channels
+// share, pass through LDS as floats.  The order of composition is fixed: equal inputs give equal bits.  States are fp32.
+#include "selective_scan.h"
+
+namespace {
+
+enum { kTotals = 0, kGradTotals = 1, kRun = 2 };
+
+// Walks rows [row0, end) of a chunk, a wave alone, with LDS of its own (lds [2][kBatch][WIDTH]).  kTotals: h becomes what the chunk makes of it, sum the sum of its steps and `begun`
+// whether a sequence begins in it.  kGradTotals: also what flows out of the chunk towards earlier rows, from none behind it (flow), and whether a sequence ends
+// in it (ended); the states before every batch are written.  kRun: writes y and the last states.
+template <int MODE, typename T, int S, int P>
+__device__ __forceinline__ void walk(const ScanArgs& a, const Walk& w, const States<S, P>& t, const float (&a2)[S], int32_t row0, int32_t end, float* lds,
+                                     float (&h)[S], float& sum, bool& begun, float (&flow)[S], bool& ended) {
+  constexpr int kWidth = S * P, kArrays = MODE == kTotals ? 1 : 2;
+  constexpr bool kExact = sizeof(T) == 4;
+  Staged<T, kWidth, kArrays> bc;
+  Column<T> x, v, dy;
+  bc.fetch(a, w, row0, end, t.lane);
+  x.fetch(w, a.x, a.ld_x, t.channel, row0);
+  v.fetch(w, a.dt, a.ld_dt, t.channel, row0);
+  if constexpr (MODE == kGradTotals) dy.fetch(w, a.dy, a.ld_dy, t.channel, row0);
+  const float bias = a.dt_bias ? a.dt_bias[t.channel] : 0.0f;
+  const float skip = MODE == kRun && a.skip ? a.skip[t.channel] : 0.0f;
+  const bool ragged = a.states != kWidth;
+  Cursor at;
+  at.open(w, row0, t.lane);
+  float decay[S];                                          // kGradTotals: of all rows so far
+  if constexpr (MODE == kGradTotals) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) decay[s] = 1.0f, flow[s] = 0.0f;
+    ended = false;
+  }
+  for (int32_t r0 = row0; r0 < end; r0 += kBatch) {
+    bc.put(lds, t.lane);
+    float d[kBatch], gain[kBatch], through_skip[kBatch], dyv[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      float slope;
+      const float xv = (float)x.v[i];
+      step_of<kExact>((float)v.v[i] + bias, d[i], slope);
+      gain[i] = d[i] * xv;
+      if (r0 + i >= end) d[i] = 0.0f, gain[i] = 0.0f;      // changes nothing
+      through_skip[i] = a.skip ? skip * xv : 0.0f;
+      if constexpr (MODE == kGradTotals) dyv[i] = r0 + i < end ? (float)dy.v[i] : 0.0f;
+    }
+    if (r0 + kBatch < end) {
+      bc.fetch(a, w, r0 + kBatch, end, t.lane);
+      x.fetch(w, a.x, a.ld_x, t.channel, r0 + kBatch);
+      v.fetch(w, a.dt, a.ld_dt, t.channel, r0 + kBatch);
+      if constexpr (MODE == kGradTotals) dy.fetch(w, a.dy, a.ld_dy, t.channel, r0 + kBatch);
+    }
+    if constexpr (MODE == kGradTotals) {
+      if (t.in) {
+        t.store(a, a.batch_h, r0 / kBatch, h);
+        if (t.part == 0) a.batch_s[(int64_t)(r0 / kBatch) * a.channels + t.channel] = begun ? -1.0f : sum;
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int32_t r = r0 + i;
+      if (r >= at.next && r < end) {                       // a sequence begins
+        at.locate(w, r, t.lane);
+        t.load_or_zero(a, a.h0, w.number(at.j), h);
+        begun = true;
+      }
+      float b[S];
+      from_lds<S>(lds + i * kWidth + t.first, b);
+#pragma unroll
+      for (int s = 0; s < S; ++s) b[s] *= gain[i];
+      if (ragged) {                                        // an infinite gain stays out of states that are none
+#pragma unroll
+        for (int s = 0; s < S; ++s) b[s] = s < t.there ? b[s] : 0.0f;
+      }
+      float keep[S];
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        keep[s] = __builtin_amdgcn_exp2f(d[i] * a2[s]);
+        h[s] = __builtin_fmaf(keep[s], h[s], b[s]);
+      }
+      if constexpr (MODE != kRun) sum += d[i];
+      if constexpr (MODE == kGradTotals) {
+        if (!ended) {
+          float c[S];
+          from_lds<S>(lds + (kBatch + i) * kWidth + t.first, c);
+#pragma unroll
+          for (int s = 0; s < S; ++s) {
+            decay[s] *= keep[s];
+            flow[s] = __builtin_fmaf(decay[s], c[s] * dyv[i], flow[s]);
+          }
+          if (r + 1 >= at.next && r < end) {               // a sequence ends
+            float l[S];
+            t.load_or_zero(a, a.dlast, w.number(at.j), l);
+#pragma unroll
+            for (int s = 0; s < S; ++s) flow[s] = __builtin_fmaf(decay[s], l[s], flow[s]);
+            ended = true;
+          }
+        }
+      }
+      if constexpr (MODE == kRun) {
+        float c[S], y[4] = {through_skip[i], 0.0f, 0.0f, 0.0f};
+        if constexpr (P > 1) y[0] = 0.0f;
+        from_lds<S>(lds + (kBatch + i) * kWidth + t.first, c);
+#pragma unroll
+        for (int s = 0; s < S; ++s) y[s & 3] = __builtin_fmaf(c[s], h[s], y[s & 3]);
+        float all = part_sum<P>((y[0] + y[1]) + (y[2] + y[3]));
+        if constexpr (P > 1) all += through_skip[i];
+        if (r < end) {
+          if (t.in && t.part == 0) ((T*)a.y + w.row(r) * a.ld_y)[t.channel] = (T)all;
+          if (r + 1 >= at.next && a.last && t.in) t.store(a, a.last, w.number(at.j), h);
+        }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
+// First launch: what every chunk, and every span of eight, makes of a state of zeros.  Block (span, slice of the channels), a wave a chunk.
+template <bool GRAD, typename T, int S, int P> __global__ void __launch_bounds__(64 * kChunkWaves) k_scan_totals(const ScanArgs a) {
+  constexpr int kWidth = S * P, kOwn = (GRAD ? 2 : 1) * kBatch * kWidth, kLine = 64 * S;   // a wave's LDS; its total
+  __shared__ float lds[kChunkWaves * (kOwn > kLine ? kOwn : kLine)];
+  __shared__ float sums[kChunkWaves][64];
+  const Walk w(a.offsets, a.n_seq, a.capacity, a.backwards);
+  report_rows(a.offsets, a.n_seq, a.capacity, a.flags);
+  const States<S, P> t(a, blockIdx.y);
+  const int64_t k = (int64_t)blockIdx.x * kChunkWaves + t.wave, row0 = k * a.chunk;
+  if ((int64_t)blockIdx.x * kChunkWaves * a.chunk >= w.n) return;
+  float a2[S], h[S], flow[S], sum = 0.0f;
+  bool begun = false, ended = false;
+  decays(a, t, a2);
+#pragma unroll
+  for (int s = 0; s < S; ++s) h[s] = 0.0f, flow[s] = 0.0f;
+  if (row0 < w.n)
+    walk<GRAD ? kGradTotals : kTotals, T, S, P>(a, w, t, a2, (int32_t)row0, row0 + a.chunk < w.n ? (int32_t)row0 + a.chunk : w.n, lds + t.wave * kOwn, h, sum,
+                                                begun, flow, ended);
+#pragma unroll
+  for (int dir = 0; dir < (GRAD ? 2 : 1); ++dir) {
+    const float s0 = (dir == 0 ? begun : ended) ? -1.0f : sum;
+    const float(&mine)[S] = dir == 0 ? h : flow;
+    if (t.in && row0 < w.n) {
+      t.store(a, a.chunk_h[dir], k, mine);
+      if (t.part == 0) a.chunk_s[dir][k * a.channels + t.channel] = s0;
+    }
+    __syncthreads();                                       // all waves are through with their rows, or the direction before
+#pragma unroll
+    for (int s = 0; s < S; ++s) lds[(t.wave * S + s) * 64 + t.lane] = mine[s];
+    sums[t.wave][t.lane] = s0;
+    __syncthreads();
+    if (t.wave == 0) {
+      float all[S], total = 0.0f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) all[s] = 0.0f;
+      for (int m = 0; m < kChunkWaves; ++m) {
+        const int from = dir == 0 ? m : kChunkWaves - 1 - m;
+        float v[S];
+#pragma unroll
+        for (int s = 0; s < S; ++s) v[s] = lds[(from * S + s) * 64 + t.lane];
+        const float one = sums[from][t.lane];
+        through<S>(a2, one, v, all);
+        total = one < 0.0f ? -1.0f : total < 0.0f ? total : total + one;
+      }
+      if (t.in) {
+        t.store(a, a.span_h[dir], blockIdx.x, all);
+        if (t.part == 0) a.span_s[dir][(int64_t)blockIdx.x * a.channels + t.channel] = total;
+      }
+    }
+  }
+}
+
+// Second launch: what enters every span.  A block has 32 states of the line [channels][states] and 32 runs of spans; a thread composes its run and, from what
+// enters it, walks it again, out of registers.  blockIdx.y: the direction.
+constexpr int kRuns = 32, kRunSpans = kMaxSpans / kRuns;
+__global__ void __launch_bounds__(32 * kRuns) k_scan_enter(const ScanArgs a) {
+  __shared__ float part_p[kRuns][33], part_h[kRuns][33];
+  const int32_t rows = a.offsets[a.n_seq], n = rows < 0 ? 0 : rows < a.capacity ? rows : a.capacity;
+  const int32_t spans = spans_of(a, n).spans, per = (spans + kRuns - 1) / kRuns;
+  const int col = threadIdx.x & 31, run = threadIdx.x >> 5, dir = blockIdx.y;
+  const int64_t line = (int64_t)a.channels * a.states, at = (int64_t)blockIdx.x * 32 + col, mine = at < line ? at : line - 1;
+  const float* const span_s = dir == 0 ? a.span_s[0] : a.span_s[1];
+  const float* const span_h = dir == 0 ? a.span_h[0] : a.span_h[1];
+  float* const enter = dir == 0 ? a.enter[0] : a.enter[1];
+  const float a2 = a.a[mine] * kLog2e;
+  const int32_t c = (int32_t)(mine / a.states), from = run * per;
+  float p[kRunSpans], h[kRunSpans];
+#pragma unroll
+  for (int i = 0; i < kRunSpans; ++i) {
+    const int32_t m = from + i;
+    const bool there = i < per && m < spans;
+    const int64_t span = there ? (dir == 0 ? m : spans - 1 - m) : 0;
+    p[i] = there ? span_s[span * a.channels + c] : 0.0f;
+    h[i] = there ? span_h[span * line + mine] : 0.0f;
+  }
+  // products of decays; a run in which a sequence begins has -1
+  float all_p = 1.0f, all_h = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kRunSpans; ++i) {
+    p[i] = p[i] < 0.0f ? -1.0f : __builtin_amdgcn_exp2f(a2 * p[i]);
+    all_h = p[i] < 0.0f ? h[i] : __builtin_fmaf(p[i], all_h, h[i]);
+    all_p = p[i] < 0.0f || all_p < 0.0f ? -1.0f : all_p * p[i];
+  }
+  part_p[run][col] = all_p, part_h[run][col] = all_h;
+  __syncthreads();
+  float state = 0.0f;
+  for (int m = 0; m < run; ++m) state = part_p[m][col] < 0.0f ? part_h[m][col] : __builtin_fmaf(part_p[m][col], state, part_h[m][col]);
+#pragma unroll
+  for (int i = 0; i < kRunSpans; ++i) {
+    const int32_t m = from + i;
+    if (i < per && m < spans && at < line) enter[(int64_t)(dir == 0 ? m : spans - 1 - m) * line + at] = state;
+    state = p[i] < 0.0f ? h[i] : __builtin_fmaf(p[i], state, h[i]);
+  }
+}
+
+// Third launch: the rows.  Blocks as in the first; those behind them deal with sequences without rows.
+template <typename T, int S, int P> __global__ void __launch_bounds__(64 * kChunkWaves) k_scan(const ScanArgs a) {
+  __shared__ float lds[kChunkWaves * 2 * kBatch * S * P];
+  const Walk w(a.offsets, a.n_seq, a.capacity, a.backwards);
+  if ((int32_t)blockIdx.x >= a.row_blocks) return hand_on(a, w, a.h0, a.last);
+  const States<S, P> t(a, blockIdx.y);
+  const int64_t k = (int64_t)blockIdx.x * kChunkWaves + t.wave, row0 = k * a.chunk;
+  if (row0 >= w.n) return;
+  float a2[S], h[S], flow[S], sum;
+  bool begun, ended;
+  decays(a, t, a2);
+  entering<0, S, P>(a, t, a2, (int32_t)k, spans_of(a, w.n), h);
+  walk<kRun, T, S, P>(a, w, t, a2, (int32_t)row0, row0 + a.chunk < w.n ? (int32_t)row0 + a.chunk : w.n, lds + t.wave * 2 * kBatch * S * P, h, sum, begun, flow,
+                      ended);
+}
+
+// Short calls: one block a slice of the channels does all three, with four states a lane.
+constexpr int kShortWaves = 16;
+constexpr int short_waves(int p) { return p < 16 ? kShortWaves : kShortWaves / 2; }   // 64 KiB of LDS at most
+template <typename T, int P> __global__ void __launch_bounds__(64 * kShortWaves) k_scan_short(const ScanArgs a) {
+  constexpr int S = 4, kOwn = 2 * kBatch * S * P;
+  extern __shared__ float lds[];                           // [waves][kOwn], then totals [waves][S][64], then sums [waves][64]
+  const Walk w(a.offsets, a.n_seq, a.capacity, a.backwards);
+  report_rows(a.offsets, a.n_seq, a.capacity, a.flags);
+  if ((int32_t)blockIdx.x >= a.row_blocks) return hand_on(a, w, a.h0, a.last);
+  const States<S, P> t(a, blockIdx.y);
+  const int waves = blockDim.x >> 6;
+  float* const totals = lds + waves * kOwn;
+  float* const sums = totals + waves * S * 64;
+  const int64_t row0 = (int64_t)t.wave * a.chunk;
+  const int32_t end = row0 + a.chunk < w.n ? (int32_t)row0 + a.chunk : w.n;
+  float a2[S], h[S], flow[S], sum = 0.0f;
+  bool begun = false, ended = false;
+  decays(a, t, a2);
+#pragma unroll
+  for (int s = 0; s < S; ++s) h[s] = 0.0f;
+  if (waves > 1) {
+    if (row0 < w.n && t.wave < waves - 1) walk<kTotals, T, S, P>(a, w, t, a2, (int32_t)row0, end, lds + t.wave * kOwn, h, sum, begun, flow, ended);
+#pragma unroll
+    for (int s = 0; s < S; ++s) totals[(t.wave * S + s) * 64 + t.lane] = h[s];
+    sums[t.wave * 64 + t.lane] = begun ? -1.0f : sum;
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < S; ++s) h[s] = 0.0f;
+    for (int m = 0; m < t.wave; ++m) {
+      float v[S];
+#pragma unroll
+      for (int s = 0; s < S; ++s) v[s] = totals[(m * S + s) * 64 + t.lane];
+      through<S>(a2, sums[m * 64 + t.lane], v, h);
+    }
+  }
+  if (row0 < w.n) walk<kRun, T, S, P>(a, w, t, a2, (int32_t)row0, end, lds + t.wave * kOwn, h, sum, begun, flow, ended);
+}
+
+// One row per sequence: a lane has four states.
+constexpr int kStepThreads = 256;
+template <typename T, int P>
+__global__ void __launch_bounds__(kStepThreads) k_scan_step(const ScanArgs a, const float* h_in, float* h_out, int64_t rows) {
+  constexpr int S = 4;
+  const int64_t i = emc2_block() * kStepThreads + threadIdx.x, at = i / P, all = rows * a.channels;
+  const bool in = at < all;
+  const int64_t line = in ? at : all - 1, row = line / a.channels;   // lanes beyond the last take part in sums and write nothing
+  const int32_t c = (int32_t)(line - row * a.channels), first = (int32_t)(i % P) * S, left = a.states - first, there = left < 0 ? 0 : left < S ? left : S;
+  float d, slope;
+  const float x = (float)((const T*)a.x + row * a.ld_x)[c];
+  step_of<sizeof(T) == 4>((float)((const T*)a.dt + row * a.ld_dt)[c] + (a.dt_bias ? a.dt_bias[c] : 0.0f), d, slope);
+  const float* const p = h_in + line * a.states + first;
+  const float* const decay = a.a + (int64_t)c * a.states + first;
+  const T* const b = (const T*)a.b + row * a.ld_b + first;
+  const T* const cc = (const T*)a.c + row * a.ld_c + first;
+  float h[S], y = 0.0f;
+  if (there == S) {
+    const emc2_fvec<4> before = emc2_load<4>(p), rate = emc2_load<4>(decay), bv = emc2_load<4>(b), cv = emc2_load<4>(cc);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      h[s] = __builtin_fmaf(__builtin_amdgcn_exp2f(d * (rate[s] * kLog2e)), before[s], d * x * bv[s]);
+      y = __builtin_fmaf(cv[s], h[s], y);
+    }
+  } else {
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (s < there) {
+        h[s] = __builtin_fmaf(__builtin_amdgcn_exp2f(d * (decay[s] * kLog2e)), p[s], d * x * (float)b[s]);
+        y = __builtin_fmaf((float)cc[s], h[s], y);
+      }
+  }
+  y = part_sum<P>(y);
+  if (!in) return;
+  float* const to = h_out + line * a.states + first;
+  if (there == S) {
+    emc2_store<4>(to, emc2_fvec<4>{h[0], h[1], h[2], h[3]});
+  } else {
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (s < there) to[s] = h[s];
+  }
+  if (first == 0) ((T*)a.y + row * a.ld_y)[c] = (T)(a.skip ? y + a.skip[c] * x : y);
+}
+
+// States a lane and lanes a channel: many rows 16 states a lane (few lanes repeat what belongs to the channel), short calls four (short chains).
+template <typename F> void with_form(int32_t states, F&& f) {
+  if (states <= 4) return f(Form<4, 1>());
+  if (states <= 8) return f(Form<8, 1>());
+  if (states <= 16) return f(Form<16, 1>());
+  if (states <= 32) return f(Form<16, 2>());
+  f(Form<16, 4>());
+}
+template <typename F> void with_short_form(int32_t states, F&& f) {
+  if (states <= 4) return f(Form<4, 1>());
+  if (states <= 8) return f(Form<4, 2>());
+  if (states <= 16) return f(Form<4, 4>());
+  if (states <= 32) return f(Form<4, 8>());
+  f(Form<4, 16>());
+}
+
+// Rows that one block can deal with.
+constexpr int64_t kShortRows = 1024;
+int64_t hand_on_blocks(int32_t n_seq, int32_t slices, bool any) {
+  const int64_t b = any ? emc2_div_up(n_seq, 16ll * slices) : 0;
+  return b < 1024 ? b : 1024;
+}
+
+}  // namespace
+
+emc2_status emc2_scan_check(emc2_ctx* ctx, const char* what, emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t states) {
+  if (!emc2_is_float(dtype)) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "%s: dtype must be F32, F16 or BF16", what);
+  if (channels < 1 || channels > (1 << 16)) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "%s: channels outside [1, 2^16]", what);
+  if (states < 1 || states > kMaxStates) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "%s: states outside [1, %d]", what, kMaxStates);
+  if (capacity < 0 || capacity > (1ll << 30)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: rows outside [0, 2^30]", what);
+  return EMC2_OK;
+}
+
+void emc2_scan_totals(const ScanArgs& a, emc2_dtype dtype, const emc2_scan_plan& p, bool grad, hipStream_t stream) {
+  with_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    with_form(a.states, [&](auto form) {
+      using F = decltype(form);
+      const dim3 grid((unsigned)p.spans, (unsigned)emc2_div_up(a.channels, 64 / F::p));
+      if (grad) hipLaunchKernelGGL((k_scan_totals<true, T, F::s, F::p>), grid, dim3(64 * kChunkWaves), 0, stream, a);
+      else hipLaunchKernelGGL((k_scan_totals<false, T, F::s, F::p>), grid, dim3(64 * kChunkWaves), 0, stream, a);
+    });
+  });
+  if (p.spans > 1)
+    hipLaunchKernelGGL(k_scan_enter, dim3((unsigned)emc2_div_up((int64_t)a.channels * a.states, 32), grad ? 2u : 1u), dim3(32 * kRuns), 0, stream, a);
+}
+
+extern "C" emc2_status emc2_selective_scan(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_dt, int64_t ld_dt,
+                                           const float* d_a, const void* d_b, int64_t ld_b, const void* d_c, int64_t ld_c, const float* d_skip,
+                                           const float* d_dt_bias, const int32_t* d_offsets, int32_t n_seq, int64_t capacity, int32_t channels,
+                                           int32_t states, int32_t backwards, const float* d_h0, void* d_y, int64_t ld_y, float* d_last,
+                                           void* d_work, int64_t work_bytes, void* stream) {
+  if (!ctx) return EMC2_ERR_INVALID_ARG;
+  const char* const what = "emc2_selective_scan";
+  const emc2_status st = emc2_scan_check(ctx, what, dtype, capacity, channels, states);
+  if (st != EMC2_OK) return st;
+  if (n_seq < 1 || n_seq > (1 << 30) || !d_offsets) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: offsets null or n_seq outside [1, 2^30]", what);
+  const size_t size = emc2_size_of(dtype);
+  const bool none = capacity == 0;
+  const int64_t kept = (int64_t)n_seq * channels * states;
+  if (!d_a) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null argument", what);
+  if (!emc2_rows_ok(d_x, ld_x, channels, size, none) || !emc2_rows_ok(d_dt, ld_dt, channels, size, none) ||
+      !emc2_rows_ok(d_b, ld_b, states, size, none) || !emc2_rows_ok(d_c, ld_c, states, size, none) || !emc2_rows_ok(d_y, ld_y, channels, size, none))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null or misaligned rows, or a pitch below the values of a row", what);
+  const emc2_rows y = {d_y, ld_y, channels}, own[] = {{d_x, ld_x, channels}, {d_dt, ld_dt, channels}}, shared[] = {{d_b, ld_b, states}, {d_c, ld_c, states}};
+  if (!emc2_results_ok(&y, 1, own, 2, capacity, size, true) || !emc2_results_ok(&y, 1, shared, 2, capacity, size, false))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_y overlaps d_b or d_c, or d_x or d_dt at another place or pitch", what);
+  if (!emc2_apart(d_last, kept, d_h0, kept)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_last must not overlap d_h0", what);
+  const emc2_scan_plan p = emc2_plan_scan(capacity, channels);
+  const bool small = capacity <= kShortRows;
+  const int64_t need = small ? 0 : emc2_scan_totals_size(p.chunks, channels, states) * (int64_t)sizeof(float);
+  if (work_bytes < need || (need && (!d_work || ((uintptr_t)d_work & 15))))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: work buffer null, misaligned or smaller than emc2_selective_scan_work", what);
+  ScanArgs a = {};
+  a.x = d_x, a.dt = d_dt, a.b = d_b, a.c = d_c, a.a = d_a, a.skip = d_skip, a.dt_bias = d_dt_bias, a.h0 = d_h0, a.offsets = d_offsets, a.y = d_y;
+  a.last = d_last, a.flags = ctx->dev_words, a.ld_x = ld_x, a.ld_dt = ld_dt, a.ld_b = ld_b, a.ld_c = ld_c, a.ld_y = ld_y;
+  a.capacity = (int32_t)capacity, a.channels = channels, a.states = states, a.n_seq = n_seq, a.backwards = backwards != 0;
+  hipStream_t s = (hipStream_t)stream;
+  if (small) {
+    with_type(dtype, [&](auto type) {
+      using T = decltype(type);
+      with_short_form(states, [&](auto form) {
+        using F = decltype(form);
+        // chunks of whole batches, as many waves as they make
+        const int64_t per = emc2_div_up(emc2_div_up(capacity, short_waves(F::p)), kBatch) * kBatch;
+        a.chunk = (int32_t)(per < kBatch ? kBatch : per);
+        const int64_t waves = emc2_div_up(capacity, a.chunk) < 1 ? 1 : emc2_div_up(capacity, a.chunk);
+        const int32_t slices = (int32_t)emc2_div_up(channels, 64 / F::p);
+        a.row_blocks = 1;
+        const dim3 grid((unsigned)(1 + hand_on_blocks(n_seq, slices, d_last)), (unsigned)slices);
+        hipLaunchKernelGGL((k_scan_short<T, F::p>), grid, dim3((unsigned)(64 * waves)),
+                           (size_t)(waves * (2 * kBatch * 4 * F::p + 5 * 64) * sizeof(float)), s, a);
+      });
+    });
+    return emc2_check_hip(ctx, hipGetLastError(), "emc2_selective_scan launch");
+  }
+  emc2_place_totals(a, 0, (float*)d_work, p);
+  a.chunk = p.chunk, a.row_blocks = p.spans;
+  emc2_scan_totals(a, dtype, p, false, s);
+  with_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    with_form(states, [&](auto form) {
+      using F = decltype(form);
+      const int32_t slices = (int32_t)emc2_div_up(channels, 64 / F::p);
+      const dim3 grid((unsigned)(p.spans + hand_on_blocks(n_seq, slices, d_last)), (unsigned)slices);
+      hipLaunchKernelGGL((k_scan<T, F::s, F::p>), grid, dim3(64 * kChunkWaves), 0, s, a);
+    });
+  });
+  return emc2_check_hip(ctx, hipGetLastError(), "emc2_selective_scan launch");
+}
+
+extern "C" emc2_status emc2_selective_scan_step(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_dt, int64_t ld_dt,
+                                                const float* d_a, const void* d_b, int64_t ld_b, const void* d_c, int64_t ld_c,
+                                                const float* d_skip, const float* d_dt_bias, const float* d_h, int64_t rows, int32_t channels,
+                                                int32_t states, float* d_h_out, void* d_y, int64_t ld_y, void* stream) {
+  if (!ctx) return EMC2_ERR_INVALID_ARG;
+  const char* const what = "emc2_selective_scan_step";
+  const emc2_status st = emc2_scan_check(ctx, what, dtype, rows, channels, states);
+  if (st != EMC2_OK) return st;
+  if (rows == 0) return EMC2_OK;
+  const size_t size = emc2_size_of(dtype);
+  const int64_t kept = rows * channels * states;
+  if (!d_a || !d_h || !d_h_out) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null argument", what);
+  if (!emc2_rows_ok(d_x, ld_x, channels, size, false) || !emc2_rows_ok(d_dt, ld_dt, channels, size, false) ||
+      !emc2_rows_ok(d_b, ld_b, states, size, false) || !emc2_rows_ok(d_c, ld_c, states, size, false) || !emc2_rows_ok(d_y, ld_y, channels, size, false))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null or misaligned rows, or a pitch below the values of a row", what);
+  const emc2_rows y = {d_y, ld_y, channels}, own[] = {{d_x, ld_x, channels}, {d_dt, ld_dt, channels}}, shared[] = {{d_b, ld_b, states}, {d_c, ld_c, states}};
+  if (!emc2_results_ok(&y, 1, own, 2, rows, size, true) || !emc2_results_ok(&y, 1, shared, 2, rows, size, false) ||
+      (d_h != d_h_out && !emc2_apart(d_h, kept, d_h_out, kept)))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_y overlaps an input, or d_h_out d_h, at another place or pitch", what);
+  ScanArgs a = {};
+  a.x = d_x, a.dt = d_dt, a.b = d_b, a.c = d_c, a.a = d_a, a.skip = d_skip, a.dt_bias = d_dt_bias, a.y = d_y;
+  a.ld_x = ld_x, a.ld_dt = ld_dt, a.ld_b = ld_b, a.ld_c = ld_c, a.ld_y = ld_y, a.channels = channels, a.states = states;
+  with_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    with_short_form(states, [&](auto form) {
+      constexpr int P = decltype(form)::p;
+      hipLaunchKernelGGL((k_scan_step<T, P>), emc2_grid(emc2_div_up(rows * channels * P, kStepThreads)), dim3(kStepThreads), 0, (hipStream_t)stream, a, d_h,
+                         d_h_out, rows);
+    });
+  });
+  return emc2_check_hip(ctx, hipGetLastError(), "emc2_selective_scan_step launch");
+}
