@@ -599,7 +599,8 @@ emc2_status emc2_causal_conv_step(emc2_ctx* ctx, emc2_dtype dtype, const void* d
  * Sequences, d_offsets and `backwards` as for emc2_recurrence.  d_x, d_dt, d_y rows of `channels` values, d_b and d_c of `states`, which all channels share (several
  * groups of channels with their own B and C: one call each).  d_a [channels][states], usually negative; d_skip and d_dt_bias [channels], NULL = 0.
  * d_h0 [n_seq][channels][states] states before the first row, NULL = zeros; d_last receives the states after the last (an empty sequence's is its d_h0), NULL to
- * skip.  States are fp32 throughout, and a sequence's reach no other sequence.  channels in [1, 65536], states in [1, 64].
+ * skip.  States are fp32 throughout, and a sequence's reach no other sequence.  channels in [1, 65536], states in [1, 64]; rows at most 2^26 values apart (the
+ * one-row form: any distance).
  * d_y may lie where d_x or d_dt does (as d_dx and d_ddt below may where d_x, d_dt or d_dy do); d_last must not overlap d_h0, nor d_dh0 d_h0 or d_dlast.
  * Other overlaps are refused.
  */

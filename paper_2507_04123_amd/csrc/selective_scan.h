@@ -133,31 +133,108 @@ struct Cursor {
   }
 };
 
+// Rows of an operand in the order of a walk: row r lies r steps behind the first.
+template <typename T> struct Line {
+  T* first;
+  int64_t step;                          // values; negative when the walk runs backwards
+  __device__ __forceinline__ Line(const Walk& w, T* p, int64_t ld) : first(p + w.row(0) * ld), step(w.backwards ? -ld : ld) {}
+};
+// How a batch's rows lie over the lanes of a channel: of its first Q lanes (four at most) lane q has rows q, q + Q, ...; what belongs to a row and a channel is
+// loaded, computed and stored by that lane alone and handed to the others where they need it.
+template <int P> struct Slots {
+  static constexpr int Q = P < 4 ? P : 4, R = kBatch / Q;
+};
+// Row i's value, from the lane that has it.
+template <int P> __device__ __forceinline__ float of_row(const float (&v)[Slots<P>::R], int i) {
+  constexpr int Q = Slots<P>::Q;
+  if constexpr (Q == 1) return v[i];
+  if constexpr (Q == 2) return i % 2 ? moved<0xF5>(v[i / 2]) : moved<0xA0>(v[i / 2]);
+  const float own = v[i / Q];
+  return i % 4 == 0 ? moved<0x00>(own) : i % 4 == 1 ? moved<0x55>(own) : i % 4 == 2 ? moved<0xAA>(own) : moved<0xFF>(own);
+}
+// The rows of the batch at r0 as a buffer, for accesses whose address is a scalar offset a row and a 32-bit one a lane (sums of 64 bits a lane cost several
+// instructions each).  Rows beyond the last of n have its place.
+template <int P> struct Rows {
+  static constexpr int Q = Slots<P>::Q;
+  __amdgpu_buffer_rsrc_t buffer;
+  int32_t last, at0, step, lane;         // the last row; bytes to the first row, and from one to the next; the lane's own offset
+  template <typename T> __device__ __forceinline__ Rows(const Line<T>& l, int32_t bytes, int q, int32_t r0, int32_t n) {
+    last = n - 1 - r0 < kBatch - 1 ? n - 1 - r0 : kBatch - 1;
+    const int32_t low = l.step < 0 ? last : 0;             // the row of the lowest address
+    step = (int32_t)l.step * (int32_t)sizeof(T);
+    at0 = low * -step;
+    buffer = __builtin_amdgcn_make_buffer_rsrc((void*)(l.first + (r0 + low) * l.step), 0, -1, 0x00027000);
+    if constexpr (Q > 1) {
+      if (last == kBatch - 1) {
+        lane = bytes + (l.step < 0 ? q - (Q - 1) : q) * step;
+        if (l.step < 0) at0 += (Q - 1) * step;
+        return;
+      }
+    }
+    lane = bytes;
+  }
+  // Offsets of a slot's row: of the lane and of all.
+  __device__ __forceinline__ int32_t of_lane(int slot, int q) const {
+    if constexpr (Q > 1) {
+      if (last < kBatch - 1) return lane + at0 + (slot * Q + q < last ? slot * Q + q : last) * step;
+    }
+    return lane;
+  }
+  __device__ __forceinline__ int32_t of_all(int slot) const {
+    if constexpr (Q > 1) return last < kBatch - 1 ? 0 : at0 + slot * Q * step;
+    return at0 + (slot < last ? slot : last) * step;
+  }
+  template <typename T> __device__ __forceinline__ T load(int slot, int q) const {
+    if constexpr (sizeof(T) == 2) {
+      const unsigned short v = __builtin_amdgcn_raw_buffer_load_b16(buffer, of_lane(slot, q), of_all(slot), 0);
+      return __builtin_bit_cast(T, v);
+    } else {
+      const unsigned v = __builtin_amdgcn_raw_buffer_load_b32(buffer, of_lane(slot, q), of_all(slot), 0);
+      return __builtin_bit_cast(T, v);
+    }
+  }
+  template <typename T> __device__ __forceinline__ void store(int slot, int q, T v) const {
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, v), buffer, of_lane(slot, q), of_all(slot), 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), buffer, of_lane(slot, q), of_all(slot), 0);
+  }
+};
+constexpr int64_t kMaxPitch = 1 << 26;   // a batch's offsets stay below 2^31 bytes
+
 // B and C of a batch, ARRAYS of them: pieces of PV values in registers on their way from memory, floats in LDS.  `threads` threads, at least 64, share them out.
 template <typename T, int WIDTH, int ARRAYS> struct Staged {
   static constexpr int kWhole = 16 / sizeof(T), PV = kWhole < WIDTH ? kWhole : WIDTH, kARow = WIDTH / PV, kAll = ARRAYS * kBatch * kARow,
                        kMine = (kAll + 63) / 64;
   emc2_vec<T, PV> v[kMine];
+  int32_t off[kMine];                    // a piece's place behind its array's first row of a batch, in values
+  int32_t thread, threads;
+  __device__ __forceinline__ int array(int q) const { return (q * threads + thread) / (kBatch * kARow); }
+  __device__ __forceinline__ int row(int q) const { return (q * threads + thread) / kARow % kBatch; }
+  __device__ __forceinline__ int state(int q) const { return (q * threads + thread) % kARow * PV; }
+  __device__ __forceinline__ void open(const Line<const T>& b, const Line<const T>& c, int thread_, int threads_) {
+    thread = thread_, threads = threads_;
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) off[q] = row(q) * (int32_t)(array(q) ? c.step : b.step) + state(q);
+  }
   // Rows of the batch at r0 that are none (at `end` or beyond) and states that are none become 0.
-  __device__ __forceinline__ void fetch(const ScanArgs& a, const Walk& w, int32_t r0, int32_t end, int thread, int threads = 64) {
+  __device__ __forceinline__ void fetch(const Line<const T>& b, const Line<const T>& c, int32_t r0, int32_t end, int32_t states) {
+    const T *const b0 = b.first + r0 * b.step, *const c0 = c.first + r0 * c.step;
 #pragma unroll
     for (int q = 0; q < kMine; ++q) {
-      const int id = q * threads + thread, array = id / (kBatch * kARow), in = id % (kBatch * kARow), n = in % kARow * PV;
-      const int32_t r = r0 + in / kARow;
       v[q] = (T)0.0f;
-      if (id < kAll && r < end) {
-        const T* const p = (array == 0 ? (const T*)a.b + w.row(r) * a.ld_b : (const T*)a.c + w.row(r) * a.ld_c) + n;
-        if (n + PV <= a.states) {
+      if (q * threads + thread < kAll && row(q) < end - r0) {
+        const T* const p = (ARRAYS > 1 && array(q) ? c0 : b0) + off[q];
+        const int there = states - state(q);
+        if (there >= PV) {
           v[q] = emc2_piece<PV>(p);
         } else {
 #pragma unroll
           for (int e = 0; e < PV; ++e)
-            if (n + e < a.states) v[q][e] = p[e];
+            if (e < there) v[q][e] = p[e];
         }
       }
     }
   }
-  __device__ __forceinline__ void put(float* to, int thread, int threads = 64) const {   // to [ARRAYS][kBatch][WIDTH]
+  __device__ __forceinline__ void put(float* to) const {   // to [ARRAYS][kBatch][WIDTH]
 #pragma unroll
     for (int q = 0; q < kMine; ++q) {
       const int id = q * threads + thread;
@@ -169,6 +246,14 @@ template <typename T, int WIDTH, int ARRAYS> struct Staged {
     }
   }
 };
+// A row's step, at the row's begin in one of the forms of a loop over rows: what is made of it, and the reads of LDS behind it, do not move in front of this
+// (all rows' decays and reads at once, or those that several forms have in common in front of all of them, would take all registers).
+template <int FORM> __device__ __forceinline__ float a_row(float d) {
+  asm volatile("; row %1" : "+v"(d) : "i"(FORM) : "memory");
+  return d;
+}
+// A value that a row ends with: it is made before the next row begins, and does not wait, with all that it needs, until it is used.
+__device__ __forceinline__ void row_ends_with(float& v) { asm volatile("" : "+v"(v)); }
 template <int S> __device__ __forceinline__ void from_lds(const float* p, float (&v)[S]) {
 #pragma unroll
   for (int i = 0; i < S; i += 4) {
@@ -178,17 +263,26 @@ template <int S> __device__ __forceinline__ void from_lds(const float* p, float 
   }
 }
 
-// Values of one channel in the rows of a batch; rows that are none read valid places.
-template <typename T> struct Column {
-  T v[kBatch];
-  __device__ __forceinline__ void fetch(const Walk& w, const void* p, int64_t ld, int32_t channel, int32_t r0) {
+// Whether any of the values is infinite.  (A NaN may be overlooked.)
+template <int R> __device__ __forceinline__ bool any_infinite(const float (&v)[R]) {
+  float m = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) v[i] = ((const T*)p + w.row(r0 + i < w.n ? r0 + i : w.n - 1) * ld)[channel];
+  for (int i = 0; i < R; ++i) m = fmaxf(m, fabsf(v[i]));
+  return __any(m > 3.402823466e38f);
+}
+
+// Values of one channel in a lane's rows of a batch; rows that are none have the last one's.
+template <typename T, int P> struct Column {
+  T v[Slots<P>::R];
+  __device__ __forceinline__ void fetch(const Line<const T>& l, int32_t bytes, int q, int32_t r0, int32_t n) {
+    const Rows<P> rows(l, bytes, q, r0, n);
+#pragma unroll
+    for (int j = 0; j < Slots<P>::R; ++j) v[j] = rows.template load<T>(j, q);
   }
 };
 
 // A times log2(e): the rows' decays are powers of two.
-template <int S, int P> __device__ __forceinline__ void decays(const ScanArgs& a, const States<S, P>& t, float (&a2)[S]) {
+template <int S, typename Lanes> __device__ __forceinline__ void decays(const ScanArgs& a, const Lanes& t, float (&a2)[S]) {
   t.load(a, a.a, a2);
 #pragma unroll
   for (int s = 0; s < S; ++s) a2[s] *= kLog2e;
@@ -208,8 +302,8 @@ __device__ __forceinline__ Spans spans_of(const ScanArgs& a, int32_t n) {
 }
 
 // The state that enters chunk `k` (direction 0), or the flow that enters it from later rows (1): what enters its span, then the chunks of the span before it.
-template <int DIR, int S, int P>
-__device__ __forceinline__ void entering(const ScanArgs& a, const States<S, P>& t, const float (&a2)[S], int32_t k, const Spans& q, float (&h)[S]) {
+template <int DIR, int S, typename Lanes>
+__device__ __forceinline__ void entering(const ScanArgs& a, const Lanes& t, const float (&a2)[S], int32_t k, const Spans& q, float (&h)[S]) {
   const int32_t span = k / kChunkWaves, lo = span * kChunkWaves, hi = lo + kChunkWaves < q.chunks ? lo + kChunkWaves : q.chunks;
   if (q.spans > 1) t.load(a, a.enter[DIR] + (int64_t)span * a.channels * a.states, h);
   else {
@@ -233,11 +327,17 @@ __device__ __forceinline__ void hand_on(const ScanArgs& a, const Walk& w, const 
   }
 }
 
+inline bool rows_ok(const void* p, int64_t pitch, int32_t width, size_t size, bool optional) {
+  return emc2_rows_ok(p, pitch, width, size, optional) && (!p || pitch <= kMaxPitch);
+}
 template <typename F> void with_type(emc2_dtype dtype, F&& f) {
   if (dtype == EMC2_F32) f(float());
   else if (dtype == EMC2_F16) f(_Float16());
   else f(__bf16());
 }
+template <bool V> struct Flag { static constexpr bool value = V; };
+typedef Flag<true> Yes;
+typedef Flag<false> No;
 template <int S, int P> struct Form { static constexpr int s = S, p = P; };
 
 }  // namespace

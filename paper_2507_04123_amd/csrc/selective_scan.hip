@@ -13,23 +13,33 @@ namespace {
 
 enum { kTotals = 0, kGradTotals = 1, kRun = 2 };
 
-// Walks rows [row0, end) of a chunk, a wave alone, with LDS of its own (lds [2][kBatch][WIDTH]).  kTotals: h becomes what the chunk makes of it, sum the sum of its steps and `begun`
-// whether a sequence begins in it.  kGradTotals: also what flows out of the chunk towards earlier rows, from none behind it (flow), and whether a sequence ends
-// in it (ended); the states before every batch are written.  kRun: writes y and the last states.
+// Walks rows [row0, end) of a chunk, a wave alone, with LDS of its own (lds [2][kBatch][WIDTH]).  kTotals: h becomes what the chunk makes of it, sum the sum of its
+// steps and `begun` whether a sequence begins in it.  kGradTotals: also what flows out of the chunk towards earlier rows, from none behind it (flow), and whether
+// a sequence ends in it (ended); the states before every batch are written.  kRun: writes y and the last states.
 template <int MODE, typename T, int S, int P>
 __device__ __forceinline__ void walk(const ScanArgs& a, const Walk& w, const States<S, P>& t, const float (&a2)[S], int32_t row0, int32_t end, float* lds,
                                      float (&h)[S], float& sum, bool& begun, float (&flow)[S], bool& ended) {
-  constexpr int kWidth = S * P, kArrays = MODE == kTotals ? 1 : 2;
+  constexpr int kWidth = S * P, kArrays = MODE == kTotals ? 1 : 2, Q = Slots<P>::Q, R = Slots<P>::R;
   constexpr bool kExact = sizeof(T) == 4;
+  const int q = t.part % Q;
   Staged<T, kWidth, kArrays> bc;
-  Column<T> x, v, dy;
-  bc.fetch(a, w, row0, end, t.lane);
-  x.fetch(w, a.x, a.ld_x, t.channel, row0);
-  v.fetch(w, a.dt, a.ld_dt, t.channel, row0);
-  if constexpr (MODE == kGradTotals) dy.fetch(w, a.dy, a.ld_dy, t.channel, row0);
+  constexpr bool kSoon = sizeof(T) == 2 || Staged<T, kWidth, kArrays>::kMine == 1;   // B and C are requested with the rows; wide ones, for lack of registers, when due
+  Column<T, P> x, v, dy;
+  const Line<const T> xs(w, (const T*)a.x, a.ld_x), vs(w, (const T*)a.dt, a.ld_dt), dys(w, (const T*)a.dy, a.ld_dy);
+  const Line<const T> bs(w, (const T*)a.b, a.ld_b), cs(w, (const T*)a.c, a.ld_c);
+  const Line<T> ys(w, (T*)a.y, a.ld_y);
+  const int32_t bytes = t.channel * (int32_t)sizeof(T);
+  bc.open(bs, cs, t.lane, 64);
+  const auto fetch = [&](int32_t r0) {
+    if constexpr (kSoon) bc.fetch(bs, cs, r0, end, a.states);
+    x.fetch(xs, bytes, q, r0, w.n);
+    v.fetch(vs, bytes, q, r0, w.n);
+    if constexpr (MODE == kGradTotals) dy.fetch(dys, bytes, q, r0, w.n);
+  };
+  fetch(row0);
   const float bias = a.dt_bias ? a.dt_bias[t.channel] : 0.0f;
   const float skip = MODE == kRun && a.skip ? a.skip[t.channel] : 0.0f;
-  const bool ragged = a.states != kWidth;
+  const bool ragged = a.states != kWidth || __any(!t.in);
   Cursor at;
   at.open(w, row0, t.lane);
   float decay[S];                                          // kGradTotals: of all rows so far
@@ -39,24 +49,17 @@ __device__ __forceinline__ void walk(const ScanArgs& a, const Walk& w, const Sta
     ended = false;
   }
   for (int32_t r0 = row0; r0 < end; r0 += kBatch) {
-    bc.put(lds, t.lane);
-    float d[kBatch], gain[kBatch], through_skip[kBatch], dyv[kBatch];
+    if constexpr (!kSoon) bc.fetch(bs, cs, r0, end, a.states);
+    bc.put(lds);
+    float d[R], xv[R], y[R], dyv[R];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
+    for (int j = 0; j < R; ++j) {
       float slope;
-      const float xv = (float)x.v[i];
-      step_of<kExact>((float)v.v[i] + bias, d[i], slope);
-      gain[i] = d[i] * xv;
-      if (r0 + i >= end) d[i] = 0.0f, gain[i] = 0.0f;      // changes nothing
-      through_skip[i] = a.skip ? skip * xv : 0.0f;
-      if constexpr (MODE == kGradTotals) dyv[i] = r0 + i < end ? (float)dy.v[i] : 0.0f;
+      step_of<kExact>((float)v.v[j] + bias, d[j], slope);
+      xv[j] = (float)x.v[j], y[j] = 0.0f, dyv[j] = 0.0f;
+      if constexpr (MODE == kGradTotals) dyv[j] = (float)dy.v[j];
     }
-    if (r0 + kBatch < end) {
-      bc.fetch(a, w, r0 + kBatch, end, t.lane);
-      x.fetch(w, a.x, a.ld_x, t.channel, r0 + kBatch);
-      v.fetch(w, a.dt, a.ld_dt, t.channel, r0 + kBatch);
-      if constexpr (MODE == kGradTotals) dy.fetch(w, a.dy, a.ld_dy, t.channel, r0 + kBatch);
-    }
+    fetch(r0 + kBatch < end ? r0 + kBatch : r0);           // (unconditional: what it replaces need not be kept for a second way)
     if constexpr (MODE == kGradTotals) {
       if (t.in) {
         t.store(a, a.batch_h, r0 / kBatch, h);
@@ -64,39 +67,45 @@ __device__ __forceinline__ void walk(const ScanArgs& a, const Walk& w, const Sta
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int32_t r = r0 + i;
-      if (r >= at.next && r < end) {                       // a sequence begins
-        at.locate(w, r, t.lane);
+    const Rows<P> y_rows(ys, bytes, q, r0, w.n);
+    // One row; returns what its states add to y.  PLAIN: it begins and ends no sequence, and its gain is finite where lanes have states that are none (an infinite
+    // gain stays out of those; a NaN is in the channel's other states too).  LIVE (kGradTotals): it adds to the flow; without PLAIN that is looked at here.
+    const auto row = [&](auto plain, auto live, int i, float di, float xi, float dyi) __attribute__((always_inline)) {
+      constexpr bool PLAIN = decltype(plain)::value, LIVE = decltype(live)::value;
+      const float gi = di * xi;
+      if (!PLAIN && r0 + i >= at.next) {                   // a sequence begins
+        at.locate(w, r0 + i, t.lane);
         t.load_or_zero(a, a.h0, w.number(at.j), h);
         begun = true;
       }
-      float b[S];
+      float b[S], keep[S];
+      int32_t there = t.there;
+      if (!PLAIN && MODE == kGradTotals) asm volatile("" : "+v"(there));   // (compared anew in every row: masks kept for all would take the registers)
       from_lds<S>(lds + i * kWidth + t.first, b);
 #pragma unroll
-      for (int s = 0; s < S; ++s) b[s] *= gain[i];
-      if (ragged) {                                        // an infinite gain stays out of states that are none
-#pragma unroll
-        for (int s = 0; s < S; ++s) b[s] = s < t.there ? b[s] : 0.0f;
-      }
-      float keep[S];
-#pragma unroll
       for (int s = 0; s < S; ++s) {
-        keep[s] = __builtin_amdgcn_exp2f(d[i] * a2[s]);
+        b[s] *= gi;
+        if (!PLAIN) b[s] = s < there ? b[s] : 0.0f;
+        keep[s] = __builtin_amdgcn_exp2f(di * a2[s]);
         h[s] = __builtin_fmaf(keep[s], h[s], b[s]);
       }
-      if constexpr (MODE != kRun) sum += d[i];
+      float all = 0.0f;
+      if constexpr (MODE != kRun) {
+        sum += di;
+#pragma unroll
+        for (int s = 0; s < S; ++s) row_ends_with(h[s]);
+      }
       if constexpr (MODE == kGradTotals) {
-        if (!ended) {
+        if (PLAIN ? LIVE : !ended) {
           float c[S];
           from_lds<S>(lds + (kBatch + i) * kWidth + t.first, c);
 #pragma unroll
           for (int s = 0; s < S; ++s) {
             decay[s] *= keep[s];
-            flow[s] = __builtin_fmaf(decay[s], c[s] * dyv[i], flow[s]);
+            flow[s] = __builtin_fmaf(decay[s], c[s] * dyi, flow[s]);
+            row_ends_with(flow[s]);
           }
-          if (r + 1 >= at.next && r < end) {               // a sequence ends
+          if (!PLAIN && r0 + i + 1 >= at.next) {           // a sequence ends
             float l[S];
             t.load_or_zero(a, a.dlast, w.number(at.j), l);
 #pragma unroll
@@ -106,17 +115,68 @@ __device__ __forceinline__ void walk(const ScanArgs& a, const Walk& w, const Sta
         }
       }
       if constexpr (MODE == kRun) {
-        float c[S], y[4] = {through_skip[i], 0.0f, 0.0f, 0.0f};
-        if constexpr (P > 1) y[0] = 0.0f;
+        float c[S], part[4] = {Q == 1 && a.skip ? skip * xi : 0.0f, 0.0f, 0.0f, 0.0f};
         from_lds<S>(lds + (kBatch + i) * kWidth + t.first, c);
 #pragma unroll
-        for (int s = 0; s < S; ++s) y[s & 3] = __builtin_fmaf(c[s], h[s], y[s & 3]);
-        float all = part_sum<P>((y[0] + y[1]) + (y[2] + y[3]));
-        if constexpr (P > 1) all += through_skip[i];
-        if (r < end) {
-          if (t.in && t.part == 0) ((T*)a.y + w.row(r) * a.ld_y)[t.channel] = (T)all;
-          if (r + 1 >= at.next && a.last && t.in) t.store(a, a.last, w.number(at.j), h);
+        for (int s = 0; s < S; ++s) part[s & 3] = __builtin_fmaf(c[s], h[s], part[s & 3]);
+        all = part_sum<P>((part[0] + part[1]) + (part[2] + part[3]));
+        if constexpr (Q == 1) {
+          if (t.in) y_rows.template store<T>(i, q, (T)all);
         }
+        if (!PLAIN && r0 + i + 1 >= at.next && a.last && t.in) t.store(a, a.last, w.number(at.j), h);
+      }
+      return all;
+    };
+    const auto rows = [&](auto live) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const float di = a_row<1 + decltype(live)::value>(of_row<P>(d, i));
+        const float all = row(Yes(), live, i, di, of_row<P>(xv, i), MODE == kGradTotals ? of_row<P>(dyv, i) : 0.0f);
+        if constexpr (MODE == kRun && Q > 1) {
+          y[i / Q] = q == i % Q ? all : y[i / Q];
+          row_ends_with(y[i / Q]);
+        }
+      }
+    };
+    bool plain = r0 + kBatch <= end && r0 + kBatch < at.next;
+    if (plain && ragged) {
+      float gain[R];
+#pragma unroll
+      for (int j = 0; j < R; ++j) gain[j] = d[j] * xv[j];
+      plain = !any_infinite(gain);
+    }
+    if (plain) {
+      if (MODE == kGradTotals && !ended) rows(Yes());
+      else rows(No());
+    } else if constexpr (MODE != kGradTotals) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (r0 + i >= end) break;
+        const float di = a_row<0>(of_row<P>(d, i)), all = row(No(), No(), i, di, of_row<P>(xv, i), 0.0f);
+        if constexpr (MODE == kRun && Q > 1) y[i / Q] = q == i % Q ? all : y[i / Q];
+      }
+    } else {
+      // In one copy of the row's code, which leaves registers for decays and flows: the lane's values move down behind each row; after all of them they are
+      // where they were.
+#pragma unroll 1
+      for (int i = 0; i < kBatch; ++i) {
+        if (r0 + i < end) {
+          const auto mine = [&](float v) { return Q == 1 ? v : __shfl(v, (t.lane & ~(Q - 1)) | (i & (Q - 1)), 64); };
+          row(No(), No(), i, a_row<0>(mine(d[0])), mine(xv[0]), mine(dyv[0]));
+        }
+        if ((i & (Q - 1)) == Q - 1) {
+          const float d0 = d[0], x0 = xv[0], dy0 = dyv[0];
+#pragma unroll
+          for (int j = 0; j + 1 < R; ++j) d[j] = d[j + 1], xv[j] = xv[j + 1], dyv[j] = dyv[j + 1];
+          d[R - 1] = d0, xv[R - 1] = x0, dyv[R - 1] = dy0;
+        }
+      }
+    }
+    if constexpr (MODE == kRun && Q > 1) {
+      if (t.in && t.part < Q) {
+#pragma unroll
+        for (int j = 0; j < R; ++j)
+          if (j * Q + q < end - r0) y_rows.template store<T>(j, q, (T)(a.skip ? __builtin_fmaf(skip, xv[j], y[j]) : y[j]));
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -124,7 +184,7 @@ __device__ __forceinline__ void walk(const ScanArgs& a, const Walk& w, const Sta
 }
 
 // First launch: what every chunk, and every span of eight, makes of a state of zeros.  Block (span, slice of the channels), a wave a chunk.
-template <bool GRAD, typename T, int S, int P> __global__ void __launch_bounds__(64 * kChunkWaves) k_scan_totals(const ScanArgs a) {
+template <bool GRAD, typename T, int S, int P> __global__ void __launch_bounds__(64 * kChunkWaves, GRAD ? 2 : 4) k_scan_totals(const ScanArgs a) {
   constexpr int kWidth = S * P, kOwn = (GRAD ? 2 : 1) * kBatch * kWidth, kLine = 64 * S;   // a wave's LDS; its total
   __shared__ float lds[kChunkWaves * (kOwn > kLine ? kOwn : kLine)];
   __shared__ float sums[kChunkWaves][64];
@@ -219,7 +279,7 @@ __global__ void __launch_bounds__(32 * kRuns) k_scan_enter(const ScanArgs a) {
 }
 
 // Third launch: the rows.  Blocks as in the first; those behind them deal with sequences without rows.
-template <typename T, int S, int P> __global__ void __launch_bounds__(64 * kChunkWaves) k_scan(const ScanArgs a) {
+template <typename T, int S, int P> __global__ void __launch_bounds__(64 * kChunkWaves, 4) k_scan(const ScanArgs a) {
   __shared__ float lds[kChunkWaves * 2 * kBatch * S * P];
   const Walk w(a.offsets, a.n_seq, a.capacity, a.backwards);
   if ((int32_t)blockIdx.x >= a.row_blocks) return hand_on(a, w, a.h0, a.last);
@@ -229,7 +289,7 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * kChun
   float a2[S], h[S], flow[S], sum;
   bool begun, ended;
   decays(a, t, a2);
-  entering<0, S, P>(a, t, a2, (int32_t)k, spans_of(a, w.n), h);
+  entering<0, S>(a, t, a2, (int32_t)k, spans_of(a, w.n), h);
   walk<kRun, T, S, P>(a, w, t, a2, (int32_t)row0, row0 + a.chunk < w.n ? (int32_t)row0 + a.chunk : w.n, lds + t.wave * 2 * kBatch * S * P, h, sum, begun, flow,
                       ended);
 }
@@ -353,11 +413,14 @@ emc2_status emc2_scan_check(emc2_ctx* ctx, const char* what, emc2_dtype dtype, i
 void emc2_scan_totals(const ScanArgs& a, emc2_dtype dtype, const emc2_scan_plan& p, bool grad, hipStream_t stream) {
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    with_form(a.states, [&](auto form) {
+    const auto launch = [&](auto form, auto both) {
       using F = decltype(form);
-      const dim3 grid((unsigned)p.spans, (unsigned)emc2_div_up(a.channels, 64 / F::p));
-      if (grad) hipLaunchKernelGGL((k_scan_totals<true, T, F::s, F::p>), grid, dim3(64 * kChunkWaves), 0, stream, a);
-      else hipLaunchKernelGGL((k_scan_totals<false, T, F::s, F::p>), grid, dim3(64 * kChunkWaves), 0, stream, a);
+      hipLaunchKernelGGL((k_scan_totals<decltype(both)::value, T, F::s, F::p>), dim3((unsigned)p.spans, (unsigned)emc2_div_up(a.channels, 64 / F::p)),
+                         dim3(64 * kChunkWaves), 0, stream, a);
+    };
+    with_form(a.states, [&](auto form) {
+      if (grad) launch(form, Yes());
+      else launch(form, No());
     });
   });
   if (p.spans > 1)
@@ -378,9 +441,9 @@ extern "C" emc2_status emc2_selective_scan(emc2_ctx* ctx, emc2_dtype dtype, cons
   const bool none = capacity == 0;
   const int64_t kept = (int64_t)n_seq * channels * states;
   if (!d_a) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null argument", what);
-  if (!emc2_rows_ok(d_x, ld_x, channels, size, none) || !emc2_rows_ok(d_dt, ld_dt, channels, size, none) ||
-      !emc2_rows_ok(d_b, ld_b, states, size, none) || !emc2_rows_ok(d_c, ld_c, states, size, none) || !emc2_rows_ok(d_y, ld_y, channels, size, none))
-    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null or misaligned rows, or a pitch below the values of a row", what);
+  if (!rows_ok(d_x, ld_x, channels, size, none) || !rows_ok(d_dt, ld_dt, channels, size, none) || !rows_ok(d_b, ld_b, states, size, none) ||
+      !rows_ok(d_c, ld_c, states, size, none) || !rows_ok(d_y, ld_y, channels, size, none))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null or misaligned rows, or a pitch below the values of a row or beyond 2^26", what);
   const emc2_rows y = {d_y, ld_y, channels}, own[] = {{d_x, ld_x, channels}, {d_dt, ld_dt, channels}}, shared[] = {{d_b, ld_b, states}, {d_c, ld_c, states}};
   if (!emc2_results_ok(&y, 1, own, 2, capacity, size, true) || !emc2_results_ok(&y, 1, shared, 2, capacity, size, false))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_y overlaps d_b or d_c, or d_x or d_dt at another place or pitch", what);

@@ -13,16 +13,16 @@
 
 namespace {
 
-// Sums of v[s] over the lanes that differ in channel only.  Bits 5, 4 and 3 of the lane choose between halves of what is left until one value is, whose number
-// is returned in `which`; the remaining channel bits add.  S = 8: bits 5 4 3; S = 4: bits 5 4.
-__device__ __forceinline__ float swapped_sum32(float p, float q) {
+__device__ __forceinline__ float swapped_sum32(float p, float q) {   // lanes below 32: p's two halves' sum; the others: q's
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(p), __float_as_uint(q), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-__device__ __forceinline__ float swapped_sum16(float p, float q) {
+__device__ __forceinline__ float swapped_sum16(float p, float q) {   // the same of neighbouring sixteens
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(p), __float_as_uint(q), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// Sums of v[s] over the lanes that differ in channel only.  Bits 5 and 4 (S = 8: and 3) of the lane choose between halves of what is left until one value is;
+// the other channel bits add.
 template <int S, int P> __device__ __forceinline__ float channel_sum(const float (&v)[S], int lane) {
   float w[S / 2];
 #pragma unroll
@@ -33,28 +33,33 @@ template <int S, int P> __device__ __forceinline__ float channel_sum(const float
   if constexpr (S == 8) {
     const bool high = lane & 8;
     r = (high ? w[1] : w[0]) + moved<0x128>(high ? w[0] : w[1]);     // row_ror:8, which is lane ^ 8
+    if constexpr (P <= 4) r += moved<0x1B>(moved<0x141>(r));         // lane ^ 7, then lane ^ 3
   } else {
-    r += moved<0x128>(r);
+    if constexpr (P <= 8) r += moved<0x128>(r);
+    if constexpr (P <= 4) r += moved<0x124>(r);                      // row_ror:4: as good as lane ^ 4 by now
   }
-  if constexpr (P <= 4) r += moved<0x1B>(moved<0x141>(r));           // lane ^ 7, then lane ^ 3
   if constexpr (P <= 2) r += moved<0x4E>(r);
   if constexpr (P == 1) r += moved<0xB1>(r);
   return r;
 }
-template <int S> __device__ __forceinline__ int kept_state(int lane) { return S == 8 ? (lane >> 5) * 4 + (lane >> 4 & 1) * 2 + (lane >> 3 & 1) : lane >> 4; }
+template <int S> __device__ __forceinline__ int kept_state(int lane) {
+  return S == 8 ? (lane >> 5) * 4 + (lane >> 4 & 1) * 2 + (lane >> 3 & 1) : (lane >> 5) * 2 + (lane >> 4 & 1);
+}
 // Lanes that write: one of those that hold the same value.
 template <int S, int P> __device__ __forceinline__ bool writes(int lane) { return (lane & (S == 8 ? 7 : 15) & ~(P - 1)) == 0; }
 
 constexpr int grad_waves(int width) { return width <= 32 ? 8 : 4; }
 
 template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_waves(S * P), 2) k_scan_grad(const ScanArgs a) {
-  constexpr int kWidth = S * P, kPair = 2 * kBatch * kWidth;
+  constexpr bool kKeep = S == 4;                           // decays stay in registers, too; otherwise they are made again
+  constexpr int kWidth = S * P, kPair = 2 * kBatch * kWidth, Q = Slots<P>::Q, R = Slots<P>::R;
   constexpr bool kExact = sizeof(T) == 4;
   extern __shared__ float lds[];                           // B and C of two batches [2][kPair], then the waves' sums for two batches [2][waves][kPair]
   const Walk w(a.offsets, a.n_seq, a.capacity, a.backwards);
   if ((int32_t)blockIdx.x >= a.row_blocks) return hand_on(a, w, a.dlast, a.dh0);
   const int waves = blockDim.x >> 6;
   const States<S, P> t(a, blockIdx.y * waves + (threadIdx.x >> 6));
+  const int q = t.part % Q;
   const int64_t first = (int64_t)blockIdx.x * a.chunk;
   float* const line = a.partial + (int64_t)blockIdx.x * ((int64_t)a.channels * (a.states + 2));
   float a2[S], flow[S], enter[S], dA[S], dskip = 0.0f, dbias = 0.0f;
@@ -63,128 +68,146 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
   for (int s = 0; s < S; ++s) dA[s] = 0.0f;
   if (first < w.n) {
     const int32_t row0 = (int32_t)first, end = first + a.chunk < w.n ? row0 + a.chunk : w.n;
-    const Spans q = spans_of(a, w.n);
-    entering<0, S, P>(a, t, a2, blockIdx.x, q, enter);
-    entering<1, S, P>(a, t, a2, blockIdx.x, q, flow);
+    const Spans spans = spans_of(a, w.n);
+    entering<0, S>(a, t, a2, blockIdx.x, spans, enter);
+    entering<1, S>(a, t, a2, blockIdx.x, spans, flow);
     const float bias = a.dt_bias ? a.dt_bias[t.channel] : 0.0f, skip = a.skip ? a.skip[t.channel] : 0.0f;
     const bool ragged = a.states != kWidth || __any(!t.in);
     Cursor at;
     Staged<T, kWidth, 2> bc;
     constexpr bool kSoon = Staged<T, kWidth, 2>::kMine <= 2;   // B and C are requested with the rows; wide ones, which would take 16 registers, when they are due
-    Column<T> x, v, dy;
+    Column<T, P> x, v, dy;
     float before[S], before_s;
+    const Line<const T> xs(w, (const T*)a.x, a.ld_x), vs(w, (const T*)a.dt, a.ld_dt), dys(w, (const T*)a.dy, a.ld_dy);
+    const Line<const T> bs(w, (const T*)a.b, a.ld_b), cs(w, (const T*)a.c, a.ld_c);
+    const Line<T> dxs(w, (T*)a.y, a.ld_y), ddts(w, (T*)a.ddt, a.ld_ddt);
+    const int32_t bytes = t.channel * (int32_t)sizeof(T);
+    bc.open(bs, cs, threadIdx.x, blockDim.x);
     const auto fetch = [&](int32_t r0) {
-      if constexpr (kSoon) bc.fetch(a, w, r0, end, threadIdx.x, blockDim.x);
-      x.fetch(w, a.x, a.ld_x, t.channel, r0);
-      v.fetch(w, a.dt, a.ld_dt, t.channel, r0);
-      dy.fetch(w, a.dy, a.ld_dy, t.channel, r0);
+      if constexpr (kSoon) bc.fetch(bs, cs, r0, end, a.states);
+      x.fetch(xs, bytes, q, r0, w.n);
+      v.fetch(vs, bytes, q, r0, w.n);
+      dy.fetch(dys, bytes, q, r0, w.n);
       t.load(a, a.batch_h + (int64_t)(r0 / kBatch) * a.channels * a.states, before);
       before_s = a.batch_s[(int64_t)(r0 / kBatch) * a.channels + t.channel];
     };
     const int32_t last = row0 + (end - row0 - 1) / kBatch * kBatch;
     fetch(last);
     at.fill(w, w.find(last, t.lane) - 31, t.lane);
-    if constexpr (!kSoon) bc.fetch(a, w, last, end, threadIdx.x, blockDim.x);
-    bc.put(lds + (last / kBatch & 1) * kPair, threadIdx.x, blockDim.x);
+    if constexpr (!kSoon) bc.fetch(bs, cs, last, end, a.states);
+    bc.put(lds + (last / kBatch & 1) * kPair);
     __syncthreads();
     for (int32_t r0 = last; r0 >= row0; r0 -= kBatch) {
       const int turn = r0 / kBatch & 1;
-      const float* const now = lds + turn * kPair;
-      float* const sums = lds + 2 * kPair + (turn * waves + t.wave) * kPair;
-      float d[kBatch], xv[kBatch], dyv[kBatch], slope[kBatch], h[S];
+      const float* const now = lds + turn * kPair + t.first;
+      float* const sums = lds + 2 * kPair + (turn * waves + t.wave) * kPair + t.first + kept_state<S>(t.lane);
+      float d[R], xv[R], dyv[R], slope[R], gb[R], dd[R], h[S];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        step_of<kExact>((float)v.v[i] + bias, d[i], slope[i]);
-        xv[i] = (float)x.v[i];
-        dyv[i] = t.in ? (float)dy.v[i] : 0.0f;
+      for (int j = 0; j < R; ++j) {
+        step_of<kExact>((float)v.v[j] + bias, d[j], slope[j]);
+        xv[j] = (float)x.v[j];
+        dyv[j] = t.in ? (float)dy.v[j] : 0.0f;
+        gb[j] = 0.0f, dd[j] = 0.0f;
       }
 #pragma unroll
       for (int s = 0; s < S; ++s) h[s] = enter[s];
       through<S>(a2, before_s, before, h);
-      // forward: the states before the rows
-      float prev[kBatch][S];
-      int32_t seq[kBatch];
-      uint32_t begins = 0, ends = 0;
+      fetch(r0 > row0 ? r0 - kBatch : row0);               // (unconditional: what it replaces need not be kept for a second way)
       at.before(w, r0, t.lane);
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int32_t r = r0 + i;
-        seq[i] = 0;
-        if (r >= end) continue;
-        if (r >= at.next) {
-          at.locate(w, r, t.lane);
-          t.load_or_zero(a, a.h0, w.number(at.j), h);
-          begins |= 1u << i;
+      const Rows<P> dx_rows(dxs, bytes, q, r0, w.n), ddt_rows(ddts, bytes, q, r0, w.n);
+      const auto finish = [&](int j, float row_gb, float row_dd) __attribute__((always_inline)) {
+        const float dv = __builtin_fmaf(row_dd, 0.693147180559945309f, row_gb * xv[j]) * slope[j];
+        float dx = d[j] * row_gb;
+        if (a.skip) dx = __builtin_fmaf(skip, dyv[j], dx);
+        if (j * Q + q < end - r0) {
+          dskip = __builtin_fmaf(dyv[j], xv[j], dskip);
+          dbias += dv;
+          if (t.in && t.part < Q) dx_rows.template store<T>(j, q, (T)dx), ddt_rows.template store<T>(j, q, (T)dv);
         }
-        seq[i] = w.number(at.j);
-        if (r + 1 >= at.next) ends |= 1u << i;
-        float b[S];
-        from_lds<S>(now + i * kWidth + t.first, b);
-        const float gain = d[i] * xv[i];
+      };
+      // PLAIN: all rows are there, none begins or ends a sequence, and nothing infinite has to be kept out of states that are none.
+      const auto rows = [&](auto plain) __attribute__((always_inline)) {
+        constexpr bool PLAIN = decltype(plain)::value;
+        float prev[kBatch][S], keep[kKeep ? kBatch : 1][S];
+        int32_t seq[kBatch];
+        uint32_t begins = 0, ends = 0;
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-          prev[i][s] = h[s];
-          b[s] *= gain;
-        }
-        if (ragged) {
+        for (int i = 0; i < kBatch; ++i) {
+          const int32_t r = r0 + i;
+          if (!PLAIN && r >= end) break;
+          const float di = a_row<PLAIN>(of_row<P>(d, i)), gi = di * of_row<P>(xv, i), dyi = of_row<P>(dyv, i);
+          if constexpr (!PLAIN) {
+            if (r >= at.next) {
+              at.locate(w, r, t.lane);
+              t.load_or_zero(a, a.h0, w.number(at.j), h);
+              begins |= 1u << i;
+            }
+            seq[i] = w.number(at.j);
+            if (r + 1 >= at.next) ends |= 1u << i;
+          }
+          float b[S];
+          from_lds<S>(now + i * kWidth, b);
 #pragma unroll
-          for (int s = 0; s < S; ++s) b[s] = s < t.there ? b[s] : 0.0f;
+          for (int s = 0; s < S; ++s) {
+            prev[i][s] = h[s];
+            const float one = __builtin_amdgcn_exp2f(di * a2[s]);
+            if constexpr (kKeep) keep[i][s] = one;
+            b[s] *= gi;
+            if (!PLAIN) b[s] = s < t.there ? b[s] : 0.0f;
+            h[s] = __builtin_fmaf(one, h[s], b[s]);
+            b[s] = dyi * h[s];
+          }
+          const float dC = channel_sum<S, P>(b, t.lane);
+          if (writes<S, P>(t.lane)) sums[(kBatch + i) * kWidth] = dC;
         }
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-          h[s] = __builtin_fmaf(__builtin_amdgcn_exp2f(d[i] * a2[s]), h[s], b[s]);
-          b[s] = dyv[i] * h[s];
+        for (int i = kBatch - 1; i >= 0; --i) {
+          const int32_t r = r0 + i;
+          if (!PLAIN && r >= end) continue;
+          const float di = a_row<PLAIN>(of_row<P>(d, i)), gi = di * of_row<P>(xv, i), dyi = of_row<P>(dyv, i);
+          if (!PLAIN && (ends >> i & 1)) t.load_or_zero(a, a.dlast, seq[i], flow);
+          float b[S], c[S], sum_gb = 0.0f, sum_dd = 0.0f;
+          from_lds<S>(now + i * kWidth, b);
+          from_lds<S>(now + (kBatch + i) * kWidth, c);
+#pragma unroll
+          for (int s = 0; s < S; ++s) {
+            float g = __builtin_fmaf(c[s], dyi, flow[s]);
+            if (!PLAIN) g = s < t.there ? g : 0.0f;
+            sum_gb = __builtin_fmaf(g, b[s], sum_gb);
+            flow[s] = (kKeep ? keep[kKeep ? i : 0][s] : __builtin_amdgcn_exp2f(di * a2[s])) * g;
+            const float e = flow[s] * prev[i][s];          // reaches the exponent
+            sum_dd = __builtin_fmaf(e, a2[s], sum_dd);
+            dA[s] = __builtin_fmaf(e, di, dA[s]);
+            b[s] = g * gi;
+          }
+          const float dB = channel_sum<S, P>(b, t.lane);
+          if (writes<S, P>(t.lane)) sums[i * kWidth] = dB;
+          sum_gb = part_sum<P>(sum_gb), sum_dd = part_sum<P>(sum_dd);
+          if constexpr (Q == 1) {
+            finish(i, sum_gb, sum_dd);
+          } else {
+            gb[i / Q] = q == i % Q ? sum_gb : gb[i / Q];
+            dd[i / Q] = q == i % Q ? sum_dd : dd[i / Q];
+          }
+          if (!PLAIN && (begins >> i & 1) && a.dh0 && t.in) t.store(a, a.dh0, seq[i], flow);
         }
-        const float dC = channel_sum<S, P>(b, t.lane);
-        if (writes<S, P>(t.lane)) sums[(kBatch + i) * kWidth + t.first + kept_state<S>(t.lane)] = dC;
+      };
+      bool plain = r0 + kBatch <= end && r0 + kBatch < at.next;
+      if (plain && ragged) {
+        float gain[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) gain[j] = d[j] * xv[j];
+        plain = !any_infinite(gain) && !any_infinite(dyv);
       }
-      // back
+      if (plain) rows(Yes());
+      else rows(No());
+      if constexpr (Q > 1) {
 #pragma unroll
-      for (int i = kBatch - 1; i >= 0; --i) {
-        const int32_t r = r0 + i;
-        // the next batch's rows, once half of this one's states have left their registers
-        if (i == kBatch / 2 - 1) {
-          __builtin_amdgcn_sched_barrier(0);
-          fetch(r0 > row0 ? r0 - kBatch : row0);           // (unconditional: what it replaces need not be kept for a second way out)
-        }
-        if (r >= end) continue;
-        if (ends >> i & 1) t.load_or_zero(a, a.dlast, seq[i], flow);
-        float b[S], c[S], g[S];
-        from_lds<S>(now + i * kWidth + t.first, b);
-        from_lds<S>(now + (kBatch + i) * kWidth + t.first, c);
-#pragma unroll
-        for (int s = 0; s < S; ++s) g[s] = __builtin_fmaf(c[s], dyv[i], flow[s]);
-        if (ragged) {
-#pragma unroll
-          for (int s = 0; s < S; ++s) g[s] = s < t.there ? g[s] : 0.0f;
-        }
-        const float gain = d[i] * xv[i];
-        float gb = 0.0f, dd = 0.0f;
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-          gb = __builtin_fmaf(g[s], b[s], gb);
-          flow[s] = __builtin_amdgcn_exp2f(d[i] * a2[s]) * g[s];
-          const float e = flow[s] * prev[i][s];            // reaches the exponent
-          dd = __builtin_fmaf(e, a2[s], dd);
-          dA[s] = __builtin_fmaf(e, d[i], dA[s]);
-          b[s] = g[s] * gain;
-        }
-        const float dB = channel_sum<S, P>(b, t.lane);
-        if (writes<S, P>(t.lane)) sums[i * kWidth + t.first + kept_state<S>(t.lane)] = dB;
-        gb = part_sum<P>(gb), dd = part_sum<P>(dd);
-        const float dv = __builtin_fmaf(dd, 0.693147180559945309f, gb * xv[i]) * slope[i];
-        float dx = d[i] * gb;
-        if (a.skip) dx = __builtin_fmaf(skip, dyv[i], dx), dskip = __builtin_fmaf(dyv[i], xv[i], dskip);
-        dbias += dv;
-        if (t.in && t.part == 0) {
-          ((T*)a.y + w.row(r) * a.ld_y)[t.channel] = (T)dx;
-          ((T*)a.ddt + w.row(r) * a.ld_ddt)[t.channel] = (T)dv;
-        }
-        if ((begins >> i & 1) && a.dh0 && t.in) t.store(a, a.dh0, seq[i], flow);
+        for (int j = 0; j < R; ++j) finish(j, gb[j], dd[j]);
       }
       // the next batch's B and C to the other half, this one's sums over the waves out of theirs
-      if constexpr (!kSoon) bc.fetch(a, w, r0 > row0 ? r0 - kBatch : row0, end, threadIdx.x, blockDim.x);
-      if (r0 > row0) bc.put(lds + (turn ^ 1) * kPair, threadIdx.x, blockDim.x);
+      if constexpr (!kSoon) bc.fetch(bs, cs, r0 > row0 ? r0 - kBatch : row0, end, a.states);
+      if (r0 > row0) bc.put(lds + (turn ^ 1) * kPair);
       __syncthreads();
       for (int e = threadIdx.x; e < kPair; e += blockDim.x) {
         const int n = e % kWidth, i = e / kWidth % kBatch, which = e / (kWidth * kBatch);
@@ -199,6 +222,8 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
       }
     }
   }
+  // rows of the channel's lanes; lanes beyond the first Q have the same again
+  dskip = part_sum<Q>(dskip), dbias = part_sum<Q>(dbias);
   if (t.in) {
     t.store(a, line, 0, dA);
     if (t.part == 0) {
@@ -224,7 +249,7 @@ template <typename T> __global__ void __launch_bounds__(kSumThreads) k_scan_grad
 
 template <typename F> void with_grad_form(int32_t states, F&& f) {
   if (states <= 4) return f(Form<4, 1>());
-  if (states <= 8) return f(Form<8, 1>());
+  if (states <= 8) return f(Form<4, 2>());
   if (states <= 16) return f(Form<8, 2>());
   if (states <= 32) return f(Form<8, 4>());
   f(Form<8, 8>());
@@ -271,12 +296,12 @@ extern "C" emc2_status emc2_selective_scan_backward(
   const bool none = capacity == 0;
   const int64_t kept = (int64_t)n_seq * channels * states;
   if (!d_a || !d_da || (!d_skip && d_dskip)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null argument", what);
-  if (!emc2_rows_ok(d_x, ld_x, channels, size, none) || !emc2_rows_ok(d_dt, ld_dt, channels, size, none) ||
-      !emc2_rows_ok(d_b, ld_b, states, size, none) || !emc2_rows_ok(d_c, ld_c, states, size, none) ||
-      !emc2_rows_ok(d_dy, ld_dy, channels, size, none) || !emc2_rows_ok(d_dx, ld_dx, channels, size, none) ||
-      !emc2_rows_ok(d_ddt, ld_ddt, channels, size, none) || !emc2_rows_ok(d_db, ld_db, states, size, none) ||
-      !emc2_rows_ok(d_dc, ld_dc, states, size, none))
-    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null or misaligned rows, or a pitch below the values of a row", what);
+  if (!rows_ok(d_x, ld_x, channels, size, none) || !rows_ok(d_dt, ld_dt, channels, size, none) ||
+      !rows_ok(d_b, ld_b, states, size, none) || !rows_ok(d_c, ld_c, states, size, none) ||
+      !rows_ok(d_dy, ld_dy, channels, size, none) || !rows_ok(d_dx, ld_dx, channels, size, none) ||
+      !rows_ok(d_ddt, ld_ddt, channels, size, none) || !rows_ok(d_db, ld_db, states, size, none) ||
+      !rows_ok(d_dc, ld_dc, states, size, none))
+    return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null or misaligned rows, or a pitch below the values of a row or beyond 2^26", what);
   const emc2_rows outs[] = {{d_dx, ld_dx, channels}, {d_ddt, ld_ddt, channels}, {d_db, ld_db, states}, {d_dc, ld_dc, states}},
                   own[] = {{d_x, ld_x, channels}, {d_dt, ld_dt, channels}, {d_dy, ld_dy, channels}}, shared[] = {{d_b, ld_b, states}, {d_c, ld_c, states}};
   if (!emc2_results_ok(outs, 4, shared, 2, capacity, size, false) || !emc2_results_ok(outs, 2, own, 3, capacity, size, true) ||

@@ -280,4 +280,8 @@ def test_refusals(ctx):
         ctx.selective_scan_step(B.F16, g["x"], g["dt"], g["a"], g["b"], g["c"], both[:n * c * m].view(n, c, m), both[4:4 + n * c * m].view(n, c, m), y)
     with pytest.raises(ValueError):
         ctx.selective_scan_step(B.F16, g["x"], g["dt"], g["a"], g["b"], g["c"], h[:5], h, y)
+    one = {q: g[q][:1] for q in ("x", "dt", "b", "c")}
+    far = torch.as_strided(torch.zeros(c, dtype=torch.float16, device="cuda"), (1, c), ((1 << 26) + 1, 1))
+    with pytest.raises(B.Emc2Error, match="2\\^26"):
+        ctx.selective_scan(B.F16, far, one["dt"], g["a"], one["b"], one["c"], dev, y[:1], w)
     assert ctx.selective_scan_work(B.F16, n, c, 65) == -1 and ctx.selective_scan_work(B.I8, n, c, m) == -1
