@@ -219,6 +219,19 @@ def make_sequence_params(channels: int, hidden: int, seed: int, block_id: int = 
     return p
 
 
+def make_selective_params(channels: int, states: int, taps: int, seed: int, block_id: int = 0) -> Dict[str, np.ndarray]:
+    """Parameters of a selective block in fp32: the convolution's taps ~ N(0, 1 / taps) and shifts ~ U[-0.1, 0.1]; decays of 1 to `states` a unit of step, steps
+    of 0.001 to 0.1 about their rows' zero (log-uniform), so that a new block remembers some ten to a thousand voxels; skips of 1; gains ~ U[0.8, 1.2]; residual
+    scale 0.5."""
+    st = Stream(seed, 5000 + block_id)
+    inner = channels + 2 * states
+    step = np.exp(st.uniform(channels, math.log(0.001), math.log(0.1)))
+    p = {"conv_w": st.normal(taps * inner, 1.0 / math.sqrt(taps)).reshape(taps, inner), "conv_bias": st.uniform(inner, -0.1, 0.1),
+         "a": -np.tile(np.arange(1.0, states + 1.0), (channels, 1)), "dt_bias": np.log(np.expm1(step)), "skip": np.ones(channels),
+         "post": st.uniform(channels, 0.8, 1.2), "scale": np.array([0.5]), "next": st.uniform(channels, 0.8, 1.2)}
+    return {k: v.astype(np.float32) for k, v in p.items()}
+
+
 def make_camera(seed: int) -> np.ndarray:
     """Seeded 3x4 pinhole matrix P = K [R | t], row-major float32[12].
 
