@@ -10,7 +10,8 @@ struct emc2_scan_args {
   const int32_t* offsets;
   void *y, *ddt, *db, *dc;                     // y: forward: y; backward: dx
   float *last, *dh0;                           // may be null
-  // totals of chunks and spans (forward; in gradients also of the flow towards earlier rows), what enters each span, the state before every batch
+  // of chunks: what those before them in their span make of a state of zeros; of spans: what they make of it (forward; in gradients also of the flow towards
+  // earlier rows); what enters each span; the state before every batch
   float *chunk_s[2], *chunk_h[2], *span_s[2], *span_h[2], *enter[2], *batch_s, *batch_h;
   float *partial, *partial_bc;                 // weights' sums per chunk; sums of dB and dC per part of the channels
   int32_t* flags;
@@ -23,8 +24,10 @@ namespace {
 
 constexpr int kBatch = 8;                // rows under way together
 constexpr int kChunkWaves = 8;           // chunks side by side in a block of the launch that reduces them: a block's total stands for them ("span")
-constexpr int kMaxChunks = 4096;         // chunks of a call times slices of its channels, and
-constexpr int kMinChunk = 16;            // rows of a chunk at least
+// Chunks of a call times slices of its channels at most, and rows of a chunk at least: as many waves as the chip holds at once of the forward pass, and of the
+// gradients, whose waves have twice the registers.
+constexpr int kMaxChunks = 4096, kMinChunk = 16;
+constexpr int kMaxChunksGrad = 2048, kMinChunkGrad = 32;
 constexpr int kMaxSpans = kMaxChunks / kChunkWaves;
 constexpr int kMaxStates = 64;
 
@@ -124,7 +127,7 @@ struct Cursor {
   }
   // Before row r: a sequence that starts with it is still to come.
   __device__ __forceinline__ void open(const Walk& w, int32_t r, int lane) {
-    fill(w, w.find(r, lane) - 31, lane);
+    fill(w, w.n_seq < 64 ? 0 : w.find(r, lane) - 31, lane);
     before(w, r, lane);
   }
   __device__ __forceinline__ void before(const Walk& w, int32_t r, int lane) {
@@ -301,20 +304,18 @@ __device__ __forceinline__ Spans spans_of(const ScanArgs& a, int32_t n) {
   return {(chunks + kChunkWaves - 1) / kChunkWaves, chunks};
 }
 
-// The state that enters chunk `k` (direction 0), or the flow that enters it from later rows (1): what enters its span, then the chunks of the span before it.
+// The state that enters chunk `k` (direction 0), or the flow that enters it from later rows (1): what enters its span, behind the chunks of the span before it.
 template <int DIR, int S, typename Lanes>
 __device__ __forceinline__ void entering(const ScanArgs& a, const Lanes& t, const float (&a2)[S], int32_t k, const Spans& q, float (&h)[S]) {
-  const int32_t span = k / kChunkWaves, lo = span * kChunkWaves, hi = lo + kChunkWaves < q.chunks ? lo + kChunkWaves : q.chunks;
-  if (q.spans > 1) t.load(a, a.enter[DIR] + (int64_t)span * a.channels * a.states, h);
+  float v[S];
+  t.load(a, a.chunk_h[DIR] + (int64_t)k * a.channels * a.states, v);
+  const float s = a.chunk_s[DIR][(int64_t)k * a.channels + t.channel];
+  if (q.spans > 1) t.load(a, a.enter[DIR] + (int64_t)(k / kChunkWaves) * a.channels * a.states, h);
   else {
 #pragma unroll
     for (int i = 0; i < S; ++i) h[i] = 0.0f;
   }
-  for (int32_t m = DIR == 0 ? lo : hi - 1; m != k; m += DIR == 0 ? 1 : -1) {
-    float v[S];
-    t.load(a, a.chunk_h[DIR] + (int64_t)m * a.channels * a.states, v);
-    through<S>(a2, a.chunk_s[DIR][(int64_t)m * a.channels + t.channel], v, h);
-  }
+  through<S>(a2, s, v, h);
 }
 
 // Sequences without rows hand their states on; blocks of their own, a sequence at a time.
@@ -347,14 +348,13 @@ struct emc2_scan_plan {
   int32_t chunk, chunks, spans;          // rows of a chunk; chunks and spans of the capacity
   int64_t most;                          // chunks that no call of up to that many rows exceeds
 };
-static inline emc2_scan_plan emc2_plan_scan(int64_t capacity, int32_t channels) {
-  const int64_t slices = emc2_div_up(channels, 64), room = slices < kMaxChunks ? kMaxChunks / slices : 1;
+static inline emc2_scan_plan emc2_plan_scan(int64_t capacity, int32_t channels, bool grad) {
+  const int64_t slices = emc2_div_up(channels, 64), all = grad ? kMaxChunksGrad : kMaxChunks, room = slices < all ? all / slices : 1;
+  const int64_t least = grad ? kMinChunkGrad : kMinChunk, per = emc2_div_up(capacity, room), some = emc2_div_up(capacity, least);
   emc2_scan_plan p;
-  const int64_t per = emc2_div_up(capacity, room);
-  p.chunk = (int32_t)(per < kMinChunk ? kMinChunk : emc2_div_up(per, kBatch) * kBatch);
+  p.chunk = (int32_t)(per < least ? least : emc2_div_up(per, kBatch) * kBatch);
   p.chunks = (int32_t)emc2_div_up(capacity, p.chunk);
   p.spans = (int32_t)emc2_div_up(p.chunks, kChunkWaves);
-  const int64_t some = emc2_div_up(capacity, kMinChunk);
   p.most = some < room ? some : room;
   return p;
 }

@@ -183,7 +183,7 @@ __device__ __forceinline__ void walk(const ScanArgs& a, const Walk& w, const Sta
   }
 }
 
-// First launch: what every chunk, and every span of eight, makes of a state of zeros.  Block (span, slice of the channels), a wave a chunk.
+// First launch: every chunk from a state of zeros, and what spans of eight chunks make of it.  Block (span, slice of the channels), a wave a chunk.
 template <bool GRAD, typename T, int S, int P> __global__ void __launch_bounds__(64 * kChunkWaves, GRAD ? 2 : 4) k_scan_totals(const ScanArgs a) {
   constexpr int kWidth = S * P, kOwn = (GRAD ? 2 : 1) * kBatch * kWidth, kLine = 64 * S;   // a wave's LDS; its total
   __shared__ float lds[kChunkWaves * (kOwn > kLine ? kOwn : kLine)];
@@ -205,32 +205,33 @@ template <bool GRAD, typename T, int S, int P> __global__ void __launch_bounds__
   for (int dir = 0; dir < (GRAD ? 2 : 1); ++dir) {
     const float s0 = (dir == 0 ? begun : ended) ? -1.0f : sum;
     const float(&mine)[S] = dir == 0 ? h : flow;
-    if (t.in && row0 < w.n) {
-      t.store(a, a.chunk_h[dir], k, mine);
-      if (t.part == 0) a.chunk_s[dir][k * a.channels + t.channel] = s0;
-    }
     __syncthreads();                                       // all waves are through with their rows, or the direction before
 #pragma unroll
     for (int s = 0; s < S; ++s) lds[(t.wave * S + s) * 64 + t.lane] = mine[s];
     sums[t.wave][t.lane] = s0;
     __syncthreads();
-    if (t.wave == 0) {
-      float all[S], total = 0.0f;
+    // what the chunks before this one make together, in the order of the direction; behind the last of them, the span
+    float all[S], total = 0.0f;
 #pragma unroll
-      for (int s = 0; s < S; ++s) all[s] = 0.0f;
-      for (int m = 0; m < kChunkWaves; ++m) {
-        const int from = dir == 0 ? m : kChunkWaves - 1 - m;
-        float v[S];
+    for (int s = 0; s < S; ++s) all[s] = 0.0f;
+    const int before = dir == 0 ? t.wave : kChunkWaves - 1 - t.wave;
+    for (int m = 0; m < before; ++m) {
+      const int from = dir == 0 ? m : kChunkWaves - 1 - m;
+      float v[S];
 #pragma unroll
-        for (int s = 0; s < S; ++s) v[s] = lds[(from * S + s) * 64 + t.lane];
-        const float one = sums[from][t.lane];
-        through<S>(a2, one, v, all);
-        total = one < 0.0f ? -1.0f : total < 0.0f ? total : total + one;
-      }
-      if (t.in) {
-        t.store(a, a.span_h[dir], blockIdx.x, all);
-        if (t.part == 0) a.span_s[dir][(int64_t)blockIdx.x * a.channels + t.channel] = total;
-      }
+      for (int s = 0; s < S; ++s) v[s] = lds[(from * S + s) * 64 + t.lane];
+      const float one = sums[from][t.lane];
+      through<S>(a2, one, v, all);
+      total = one < 0.0f ? -1.0f : total < 0.0f ? total : total + one;
+    }
+    if (t.in && row0 < w.n) {
+      t.store(a, a.chunk_h[dir], k, all);
+      if (t.part == 0) a.chunk_s[dir][k * a.channels + t.channel] = total;
+    }
+    if (before == kChunkWaves - 1 && t.in) {
+      through<S>(a2, s0, mine, all);
+      t.store(a, a.span_h[dir], blockIdx.x, all);
+      if (t.part == 0) a.span_s[dir][(int64_t)blockIdx.x * a.channels + t.channel] = s0 < 0.0f ? -1.0f : total < 0.0f ? total : total + s0;
     }
   }
 }
@@ -448,7 +449,7 @@ extern "C" emc2_status emc2_selective_scan(emc2_ctx* ctx, emc2_dtype dtype, cons
   if (!emc2_results_ok(&y, 1, own, 2, capacity, size, true) || !emc2_results_ok(&y, 1, shared, 2, capacity, size, false))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_y overlaps d_b or d_c, or d_x or d_dt at another place or pitch", what);
   if (!emc2_apart(d_last, kept, d_h0, kept)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_last must not overlap d_h0", what);
-  const emc2_scan_plan p = emc2_plan_scan(capacity, channels);
+  const emc2_scan_plan p = emc2_plan_scan(capacity, channels, false);
   const bool small = capacity <= kShortRows;
   const int64_t need = small ? 0 : emc2_scan_totals_size(p.chunks, channels, states) * (int64_t)sizeof(float);
   if (work_bytes < need || (need && (!d_work || ((uintptr_t)d_work & 15))))
