@@ -2,18 +2,13 @@
 // and the sums of their weights' gradients.
 #pragma once
 #include "column_sums.h"
+#include "lane_sums.h"
 #include "rows.h"
 
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxChannels = 1024;
-
-template <int L> __device__ __forceinline__ float lane_sum(float v) {
-#pragma unroll
-  for (int d = 1; d < L; d <<= 1) v += __shfl_xor(v, d, 64);
-  return v;
-}
 
 // A lane's vectors: vector v begins at channel at[v] (-1: there is none).  A row whose length is no multiple of N (MOVED) ends with a vector moved
 // back over its neighbour: the first twice[v] of its values are that one's too, computed alike by both and counted by one.

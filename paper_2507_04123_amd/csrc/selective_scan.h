@@ -1,6 +1,7 @@
 // What the kernels of the selective scan (selective_scan.hip, selective_scan_grad.hip) share: how states lie over lanes, the rows' way into registers and
 // LDS, steps and decays, and the totals of runs of rows.
 #pragma once
+#include "lane_sums.h"
 #include "rows.h"
 #include "sequences.h"
 
@@ -81,18 +82,6 @@ template <int S, int P> struct States {
     }
   }
 };
-
-// Sums over the P lanes of a channel, in all of them.
-template <int CTRL> __device__ __forceinline__ float moved(float v) {
-  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-template <int P> __device__ __forceinline__ float part_sum(float v) {
-  if constexpr (P > 1) v += moved<0xB1>(v);                // quad_perm: lane ^ 1
-  if constexpr (P > 2) v += moved<0x4E>(v);                // lane ^ 2
-  if constexpr (P > 4) v += moved<0x141>(v);               // mirrored within eight lanes, whose halves are uniform by now
-  if constexpr (P > 8) v += moved<0x140>(v);               // mirrored within sixteen
-  return v;
-}
 
 // Steps: softplus(v) = log(1 + e), e = exp(v), and its slope e / (1 + e).  u = 1 + e is rounded; log(1 + e) = log(u) + (e - (u - 1)) / u to second order, so
 // that steps far below 1 keep their places.  Beyond 20 the logarithm is v itself, to 2e-9.

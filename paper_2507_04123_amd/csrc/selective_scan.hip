@@ -119,7 +119,7 @@ __device__ __forceinline__ void walk(const ScanArgs& a, const Walk& w, const Sta
         from_lds<S>(lds + (kBatch + i) * kWidth + t.first, c);
 #pragma unroll
         for (int s = 0; s < S; ++s) part[s & 3] = __builtin_fmaf(c[s], h[s], part[s & 3]);
-        all = part_sum<P>((part[0] + part[1]) + (part[2] + part[3]));
+        all = lane_sum<P>((part[0] + part[1]) + (part[2] + part[3]));
         if constexpr (Q == 1) {
           if (t.in) y_rows.template store<T>(i, q, (T)all);
         }
@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(kStepThreads) k_scan_step(const ScanArgs a, co
         y = __builtin_fmaf((float)cc[s], h[s], y);
       }
   }
-  y = part_sum<P>(y);
+  y = lane_sum<P>(y);
   if (!in) return;
   float* const to = h_out + line * a.states + first;
   if (there == S) {

@@ -13,14 +13,6 @@
 
 namespace {
 
-__device__ __forceinline__ float swapped_sum32(float p, float q) {   // lanes below 32: p's two halves' sum; the others: q's
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(p), __float_as_uint(q), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ __forceinline__ float swapped_sum16(float p, float q) {   // the same of neighbouring sixteens
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(p), __float_as_uint(q), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 // Sums of v[s] over the lanes that differ in channel only.  Bits 5 and 4 (S = 8: and 3) of the lane choose between halves of what is left until one value is;
 // the other channel bits add.
 template <int S, int P> __device__ __forceinline__ float channel_sum(const float (&v)[S], int lane) {
@@ -182,7 +174,7 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
           }
           const float dB = channel_sum<S, P>(b, t.lane);
           if (writes<S, P>(t.lane)) sums[i * kWidth] = dB;
-          sum_gb = part_sum<P>(sum_gb), sum_dd = part_sum<P>(sum_dd);
+          sum_gb = lane_sum<P>(sum_gb), sum_dd = lane_sum<P>(sum_dd);
           if constexpr (Q == 1) {
             finish(i, sum_gb, sum_dd);
           } else {
@@ -223,7 +215,7 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
     }
   }
   // rows of the channel's lanes; lanes beyond the first Q have the same again
-  dskip = part_sum<Q>(dskip), dbias = part_sum<Q>(dbias);
+  dskip = lane_sum<Q>(dskip), dbias = lane_sum<Q>(dbias);
   if (t.in) {
     t.store(a, line, 0, dA);
     if (t.part == 0) {
