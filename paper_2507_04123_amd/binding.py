@@ -263,11 +263,69 @@ def _raw_stream() -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _stream_of(dev: int) -> int:
+    """The stream of torch that is current on device `dev`."""
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _shape_of(x: torch.Tensor) -> torch.Size:
+    """Shape of the first operand of a call, whose rows the others' are like."""
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError(f"x: need rows [n][channels], got {tuple(shape)}")
+    return shape
+
+
+def _rows_at(dev: int, td: torch.dtype, shape: torch.Size, names: Tuple[str, ...], *rows: Optional[torch.Tensor]) -> list:
+    """Pointer and pitch of each operand, one after the other (None and 0: there is none): rows of the one shape and type on device `dev`, any distance apart,
+    channels neighbours.  One pass over all of a call's rows: with checks and pointers one by one, issuing a call of a few rows took up to 0.5 us longer."""
+    out = []
+    for name, t in zip(names, rows):
+        if t is None:
+            out += (None, 0)
+            continue
+        if t.shape != shape or t.dtype is not td or t.get_device() != dev:
+            raise ValueError(f"{name}: need {td} rows {tuple(shape)} on device {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        ld, step = t.stride()
+        out += (t.data_ptr(), ld if step == 1 and ld >= shape[1] else _pitch(t, (True, td, shape), name))
+    return out
+
+
+def _floats_at(dev: int, *operands: Tuple[Optional[torch.Tensor], Tuple[int, ...], str]) -> list:
+    """Pointers of contiguous fp32 operands (tensor, shape, name) on device `dev`."""
+    out = []
+    for t, shape, name in operands:
+        if t is None:
+            out.append(None)
+            continue
+        if t.shape != shape or t.dtype is not torch.float32 or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError(f"{name}: need a contiguous {torch.float32} tensor {tuple(shape)} on device {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        out.append(t.data_ptr())
+    return out
+
+
+def _ints_at(dev: int, t: Optional[torch.Tensor], name: str) -> Optional[int]:
+    """Pointer of a contiguous int32 operand on device `dev` with one value at least."""
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous() or t.numel() < 1:
+        raise ValueError(f"{name}: need a contiguous {torch.int32} tensor on device {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
 def _count_check(n: Optional[torch.Tensor]) -> None:
     if n is not None:
         _dev_check(n, torch.int32, "n")
         if n.numel() < 1:
             raise ValueError("n: need one count")
+
+
+def _work_at(dev: int, work: torch.Tensor, need: int) -> Tuple[int, int]:
+    """Pointer and bytes of a work buffer on device `dev`."""
+    size = _work_check(work, need)
+    if work.get_device() != dev:
+        raise ValueError(f"work: need a tensor on device {dev}, got {work.device}")
+    return work.data_ptr(), size
 
 
 def _work_check(work: torch.Tensor, need: int) -> int:
@@ -841,24 +899,21 @@ class Context:
                     silu: bool = True, backwards: bool = False, before: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None) -> None:
         """y_t = silu(bias + sum of w[k] x_{t-k}) along every sequence; w [taps][channels]; before and last [sequences][taps - 1][channels]: the rows
         before each sequence's first and the last ones behind it, oldest first.  y must not overlap x, nor last before."""
-        like, rows, c = _rows_of(x, dtype)
-        ld = _pitch(x, like, "x"), _pitch(y, like, "y")
-        taps, n_seq = self._conv_check(w, bias, c, offsets, ((before, "before"), (last, "last")))
-        self._chk(self.lib.emc2_causal_conv(self.h, dtype, _at(x), ld[0], _at(w), _at(bias), int(bool(silu)), _at(offsets), n_seq, rows, c, taps,
-                                            int(bool(backwards)), _at(before), _at(y), ld[1], _at(last), _raw_stream()))
+        dev, shape = self._current(), _shape_of(x)
+        rows, c = shape
+        xp, ld_x, yp, ld_y = _rows_at(dev, _TORCH_DTYPE[dtype], shape, ("x", "y"), x, y)
+        at, taps, n_seq = _ints_at(dev, offsets, "offsets"), w.shape[0] if w.dim() == 2 else 0, offsets.numel() - 1
+        kept = (n_seq, taps - 1, c)
+        wp, bp, fp, lp = _floats_at(dev, (w, (taps, c), "w"), (bias, (c,), "bias"), (before, kept, "before"), (last, kept, "last"))
+        self._chk(self.lib.emc2_causal_conv(self.h, dtype, xp, ld_x, wp, bp, bool(silu), at, n_seq, rows, c, taps, bool(backwards), fp, yp, ld_y, lp,
+                                            _stream_of(dev)))
 
-    def _conv_check(self, w: torch.Tensor, bias: Optional[torch.Tensor], c: int, offsets: Optional[torch.Tensor], states: Sequence,
-                    n_seq: int = 0) -> Tuple[int, int]:
-        """Taps and number of sequences."""
-        taps = w.shape[0] if w.dim() == 2 else 0
-        _params_check(w, torch.float32, (taps, c), "w")
-        _params_check(bias, torch.float32, (c,), "bias")
-        if offsets is not None:
-            _dev_check(offsets, torch.int32, "offsets")
-            n_seq = offsets.numel() - 1
-        for t, nm in states:
-            _params_check(t, torch.float32, (n_seq, taps - 1, c), nm)
-        return taps, n_seq
+    def _current(self) -> int:
+        """The current device, which has to be the context's."""
+        dev = torch._C._cuda_getDevice()
+        if dev != self.device:
+            raise ValueError(f"the context's device is {self.device}, the current one {dev}")
+        return dev
 
     def causal_conv_work(self, dtype: int, capacity: int, channels: int, taps: int) -> int:
         return self.lib.emc2_causal_conv_work(dtype, capacity, channels, taps)
@@ -868,36 +923,39 @@ class Context:
                              silu: bool = True, backwards: bool = False, before: Optional[torch.Tensor] = None,
                              dlast: Optional[torch.Tensor] = None, dbefore: Optional[torch.Tensor] = None) -> None:
         """dx, dw, dbias and dbefore of a causal_conv of x for dy and the gradient of the rows kept; dx must not overlap x or dy."""
-        like, rows, c = _rows_of(x, dtype)
-        ld = _pitch(x, like, "x"), _pitch(dy, like, "dy"), _pitch(dx, like, "dx")
-        taps, n_seq = self._conv_check(w, bias, c, offsets, ((before, "before"), (dlast, "dlast"), (dbefore, "dbefore")))
-        _params_check(dw, torch.float32, (taps, c), "dw")
-        _params_check(dbias, torch.float32, (c,), "dbias")
-        size = _work_check(work, self.lib.emc2_causal_conv_work(dtype, rows, c, taps))
-        self._chk(self.lib.emc2_causal_conv_backward(self.h, dtype, _at(x), ld[0], _at(w), _at(bias), int(bool(silu)), _at(offsets), n_seq, rows, c,
-                                                     taps, int(bool(backwards)), _at(before), _at(dy), ld[1], _at(dlast), _at(dx), ld[2], _at(dw),
-                                                     _at(dbias), _at(dbefore), _at(work), size, _raw_stream()))
+        dev, shape = self._current(), _shape_of(x)
+        rows, c = shape
+        xp, ld_x, dyp, ld_dy, dxp, ld_dx = _rows_at(dev, _TORCH_DTYPE[dtype], shape, ("x", "dy", "dx"), x, dy, dx)
+        at, taps, n_seq = _ints_at(dev, offsets, "offsets"), w.shape[0] if w.dim() == 2 else 0, offsets.numel() - 1
+        kept = (n_seq, taps - 1, c)
+        wp, bp, fp, dlp, dwp, dbp, dfp = _floats_at(dev, (w, (taps, c), "w"), (bias, (c,), "bias"), (before, kept, "before"), (dlast, kept, "dlast"),
+                                                    (dw, (taps, c), "dw"), (dbias, (c,), "dbias"), (dbefore, kept, "dbefore"))
+        wk, size = _work_at(dev, work, self.lib.emc2_causal_conv_work(dtype, rows, c, taps))
+        self._chk(self.lib.emc2_causal_conv_backward(self.h, dtype, xp, ld_x, wp, bp, bool(silu), at, n_seq, rows, c, taps, bool(backwards), fp, dyp, ld_dy,
+                                                     dlp, dxp, ld_dx, dwp, dbp, dfp, wk, size, _stream_of(dev)))
 
     def causal_conv_step(self, dtype: int, x: torch.Tensor, w: torch.Tensor, state: torch.Tensor, state_out: torch.Tensor, y: torch.Tensor,
                          bias: Optional[torch.Tensor] = None, silu: bool = True) -> None:
         """One row per sequence; state [rows][taps - 1][channels]: the rows before, oldest first; state_out (may be state): moved on by the row."""
-        like, rows, c = _rows_of(x, dtype)
-        ld = _pitch(x, like, "x"), _pitch(y, like, "y")
-        taps, _ = self._conv_check(w, bias, c, None, ((state, "state"), (state_out, "state_out")), rows)
-        self._chk(self.lib.emc2_causal_conv_step(self.h, dtype, _at(x), ld[0], _at(w), _at(bias), int(bool(silu)), _at(state), rows, c, taps,
-                                                 _at(state_out), _at(y), ld[1], _raw_stream()))
+        dev, shape = self._current(), _shape_of(x)
+        rows, c = shape
+        xp, ld_x, yp, ld_y = _rows_at(dev, _TORCH_DTYPE[dtype], shape, ("x", "y"), x, y)
+        taps = w.shape[0] if w.dim() == 2 else 0
+        kept = (rows, taps - 1, c)
+        wp, bp, sp, op = _floats_at(dev, (w, (taps, c), "w"), (bias, (c,), "bias"), (state, kept, "state"), (state_out, kept, "state_out"))
+        self._chk(self.lib.emc2_causal_conv_step(self.h, dtype, xp, ld_x, wp, bp, bool(silu), sp, rows, c, taps, op, yp, ld_y, _stream_of(dev)))
 
     def gated_residual(self, dtype: int, x: torch.Tensor, branch: torch.Tensor, post: torch.Tensor, scale: torch.Tensor, total: torch.Tensor,
                        eps: float, gate: Optional[torch.Tensor] = None, next_gain: Optional[torch.Tensor] = None,
                        y: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None) -> None:
         """total = x + scale silu(gate) rms(branch) post and, if y is given, y = rms(total) next_gain; scale: one value; n: device count of the rows present."""
-        like, rows, c = _rows_of(x, dtype)
-        ld = (_pitch(x, like, "x"), _pitch(branch, like, "branch"), _pitch(gate, like, "gate"), _pitch(total, like, "total"), _pitch(y, like, "y"))
-        for t, shape, nm in ((post, (c,), "post"), (scale, (1,), "scale"), (next_gain, (c,), "next_gain")):
-            _params_check(t, torch.float32, shape, nm)
-        _count_check(n)
-        self._chk(self.lib.emc2_gated_residual(self.h, dtype, _at(x), ld[0], _at(branch), ld[1], _at(gate), ld[2], _at(post), _at(scale),
-                                               _at(next_gain), eps, _at(n), rows, c, _at(total), ld[3], _at(y), ld[4], _raw_stream()))
+        dev, shape = self._current(), _shape_of(x)
+        rows, c = shape
+        xp, ld_x, bp, ld_b, gp, ld_g, tp, ld_t, yp, ld_y = _rows_at(dev, _TORCH_DTYPE[dtype], shape, ("x", "branch", "gate", "total", "y"),
+                                                                    x, branch, gate, total, y)
+        pp, sp, np = _floats_at(dev, (post, (c,), "post"), (scale, (1,), "scale"), (next_gain, (c,), "next_gain"))
+        self._chk(self.lib.emc2_gated_residual(self.h, dtype, xp, ld_x, bp, ld_b, gp, ld_g, pp, sp, np, eps, _ints_at(dev, n, "n"), rows, c, tp, ld_t, yp,
+                                               ld_y, _stream_of(dev)))
 
     def gated_residual_work(self, dtype: int, capacity: int, channels: int) -> int:
         return self.lib.emc2_gated_residual_work(dtype, capacity, channels)
@@ -909,30 +967,16 @@ class Context:
                                 dy: Optional[torch.Tensor] = None, dnext: Optional[torch.Tensor] = None,
                                 n: Optional[torch.Tensor] = None) -> None:
         """dx, dbranch, dgate, dpost, dscale and dnext of a gated_residual for dtotal and dy (either may be None)."""
-        like, rows, c = _rows_of(x, dtype)
-        ld = [_pitch(t, like, nm) for t, nm in ((x, "x"), (branch, "branch"), (gate, "gate"), (dtotal, "dtotal"), (dy, "dy"), (dx, "dx"),
-                                                (dbranch, "dbranch"), (dgate, "dgate"))]
-        for t, shape, nm in ((post, (c,), "post"), (scale, (1,), "scale"), (next_gain, (c,), "next_gain"), (dpost, (c,), "dpost"),
-                             (dscale, (1,), "dscale"), (dnext, (c,), "dnext")):
-            _params_check(t, torch.float32, shape, nm)
-        _count_check(n)
-        size = _work_check(work, self.lib.emc2_gated_residual_work(dtype, rows, c))
-        self._chk(self.lib.emc2_gated_residual_backward(self.h, dtype, _at(x), ld[0], _at(branch), ld[1], _at(gate), ld[2], _at(post), _at(scale),
-                                                        _at(next_gain), eps, _at(dtotal), ld[3], _at(dy), ld[4], _at(n), rows, c, _at(dx), ld[5],
-                                                        _at(dbranch), ld[6], _at(dgate), ld[7], _at(dpost), _at(dscale), _at(dnext), _at(work),
-                                                        size, _raw_stream()))
-
-    def _scan_check(self, dtype: int, x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor,
-                    skip: Optional[torch.Tensor], dt_bias: Optional[torch.Tensor]) -> Tuple[tuple, tuple, list]:
-        """What rows of channels and rows of states look like, and the arguments that all calls of the scan begin with."""
-        like, rows, ch = _rows_of(x, dtype)
-        m = a.shape[1] if a.dim() == 2 else 0
-        _params_check(a, torch.float32, (ch, m), "a")
-        shared = (True, like[1], torch.Size((rows, m)))
-        for t, nm in ((skip, "skip"), (dt_bias, "dt_bias")):
-            _params_check(t, torch.float32, (ch,), nm)
-        return like, shared, [self.h, dtype, _at(x), _pitch(x, like, "x"), _at(dt), _pitch(dt, like, "dt"), _at(a), _at(b), _pitch(b, shared, "b"), _at(c),
-                              _pitch(c, shared, "c"), _at(skip), _at(dt_bias)]
+        dev, shape = self._current(), _shape_of(x)
+        rows, c = shape
+        xp, ld_x, bp, ld_b, gp, ld_g, dtp, ld_dt, dyp, ld_dy, dxp, ld_dx, dbp, ld_db, dgp, ld_dg = _rows_at(
+            dev, _TORCH_DTYPE[dtype], shape, ("x", "branch", "gate", "dtotal", "dy", "dx", "dbranch", "dgate"), x, branch, gate, dtotal, dy, dx, dbranch, dgate)
+        pp, sp, np, dpp, dsp, dnp = _floats_at(dev, (post, (c,), "post"), (scale, (1,), "scale"), (next_gain, (c,), "next_gain"), (dpost, (c,), "dpost"),
+                                               (dscale, (1,), "dscale"), (dnext, (c,), "dnext"))
+        wk, size = _work_at(dev, work, self.lib.emc2_gated_residual_work(dtype, rows, c))
+        self._chk(self.lib.emc2_gated_residual_backward(self.h, dtype, xp, ld_x, bp, ld_b, gp, ld_g, pp, sp, np, eps, dtp, ld_dt, dyp, ld_dy,
+                                                        _ints_at(dev, n, "n"), rows, c, dxp, ld_dx, dbp, ld_db, dgp, ld_dg, dpp, dsp, dnp, wk, size,
+                                                        _stream_of(dev)))
 
     def selective_scan_work(self, dtype: int, capacity: int, channels: int, states: int) -> int:
         return self.lib.emc2_selective_scan_work(dtype, capacity, channels, states)
@@ -942,15 +986,16 @@ class Context:
                        backwards: bool = False, h0: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None) -> None:
         """h_t = exp(D_t a) h_{t-1} + D_t x_t b_t and y_t = c_t . h_t + skip x_t along every sequence, D = softplus(dt + dt_bias); x, dt, y rows of channels,
         b, c rows of states, a [channels][states], h0 and last [sequences][channels][states].  `last` must not overlap h0."""
-        like, shared, args = self._scan_check(dtype, x, dt, a, b, c, skip, dt_bias)
-        ld = _pitch(y, like, "y")
-        _dev_check(offsets, torch.int32, "offsets")
-        n_seq, rows, (ch, m) = offsets.numel() - 1, like[2][0], a.shape
-        _params_check(h0, torch.float32, (n_seq, ch, m), "h0")
-        _params_check(last, torch.float32, (n_seq, ch, m), "last")
-        size = _work_check(work, self.lib.emc2_selective_scan_work(dtype, rows, ch, m))
-        self._chk(self.lib.emc2_selective_scan(*args, _at(offsets), n_seq, rows, ch, m, int(bool(backwards)), _at(h0), _at(y), ld, _at(last), _at(work), size,
-                                               _raw_stream()))
+        dev, shape = self._current(), _shape_of(x)
+        td, (rows, ch), m = _TORCH_DTYPE[dtype], shape, a.shape[1] if a.dim() == 2 else 0
+        xp, ld_x, dtp, ld_dt, yp, ld_y = _rows_at(dev, td, shape, ("x", "dt", "y"), x, dt, y)
+        bp, ld_b, cp, ld_c = _rows_at(dev, td, torch.Size((rows, m)), ("b", "c"), b, c)
+        at, n_seq = _ints_at(dev, offsets, "offsets"), offsets.numel() - 1
+        ap, sp, op, hp, lp = _floats_at(dev, (a, (ch, m), "a"), (skip, (ch,), "skip"), (dt_bias, (ch,), "dt_bias"), (h0, (n_seq, ch, m), "h0"),
+                                        (last, (n_seq, ch, m), "last"))
+        wk, size = _work_at(dev, work, self.lib.emc2_selective_scan_work(dtype, rows, ch, m))
+        self._chk(self.lib.emc2_selective_scan(self.h, dtype, xp, ld_x, dtp, ld_dt, ap, bp, ld_b, cp, ld_c, sp, op, at, n_seq, rows, ch, m, bool(backwards),
+                                               hp, yp, ld_y, lp, wk, size, _stream_of(dev)))
 
     def selective_scan_backward(self, dtype: int, x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor,
                                 offsets: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor, ddt: torch.Tensor, da: torch.Tensor, db: torch.Tensor,
@@ -959,24 +1004,28 @@ class Context:
                                 h0: Optional[torch.Tensor] = None, dlast: Optional[torch.Tensor] = None,
                                 dh0: Optional[torch.Tensor] = None) -> None:
         """The gradients of a selective_scan for dy and the gradient of the last states; dh0 must not overlap dlast or h0."""
-        like, shared, args = self._scan_check(dtype, x, dt, a, b, c, skip, dt_bias)
-        ld = [_pitch(t, s, nm) for t, s, nm in ((dy, like, "dy"), (dx, like, "dx"), (ddt, like, "ddt"), (db, shared, "db"), (dc, shared, "dc"))]
-        _dev_check(offsets, torch.int32, "offsets")
-        n_seq, rows, (ch, m) = offsets.numel() - 1, like[2][0], a.shape
-        for t, shape, nm in ((da, (ch, m), "da"), (dskip, (ch,), "dskip"), (ddt_bias, (ch,), "ddt_bias"), (h0, (n_seq, ch, m), "h0"),
-                             (dlast, (n_seq, ch, m), "dlast"), (dh0, (n_seq, ch, m), "dh0")):
-            _params_check(t, torch.float32, shape, nm)
-        size = _work_check(work, self.lib.emc2_selective_scan_work(dtype, rows, ch, m))
-        self._chk(self.lib.emc2_selective_scan_backward(*args, _at(offsets), n_seq, rows, ch, m, int(bool(backwards)), _at(h0), _at(dy), ld[0], _at(dlast),
-                                                        _at(dx), ld[1], _at(ddt), ld[2], _at(da), _at(db), ld[3], _at(dc), ld[4], _at(dskip),
-                                                        _at(ddt_bias), _at(dh0), _at(work), size, _raw_stream()))
+        dev, shape = self._current(), _shape_of(x)
+        td, (rows, ch), m = _TORCH_DTYPE[dtype], shape, a.shape[1] if a.dim() == 2 else 0
+        xp, ld_x, dtp, ld_dt, dyp, ld_dy, dxp, ld_dx, ddtp, ld_ddt = _rows_at(dev, td, shape, ("x", "dt", "dy", "dx", "ddt"), x, dt, dy, dx, ddt)
+        bp, ld_b, cp, ld_c, dbp, ld_db, dcp, ld_dc = _rows_at(dev, td, torch.Size((rows, m)), ("b", "c", "db", "dc"), b, c, db, dc)
+        at, n_seq = _ints_at(dev, offsets, "offsets"), offsets.numel() - 1
+        kept = (n_seq, ch, m)
+        ap, sp, op, hp, dlp, dap, dsp, dop, dhp = _floats_at(dev, (a, (ch, m), "a"), (skip, (ch,), "skip"), (dt_bias, (ch,), "dt_bias"), (h0, kept, "h0"),
+                                                             (dlast, kept, "dlast"), (da, (ch, m), "da"), (dskip, (ch,), "dskip"),
+                                                             (ddt_bias, (ch,), "ddt_bias"), (dh0, kept, "dh0"))
+        wk, size = _work_at(dev, work, self.lib.emc2_selective_scan_work(dtype, rows, ch, m))
+        self._chk(self.lib.emc2_selective_scan_backward(self.h, dtype, xp, ld_x, dtp, ld_dt, ap, bp, ld_b, cp, ld_c, sp, op, at, n_seq, rows, ch, m,
+                                                        bool(backwards), hp, dyp, ld_dy, dlp, dxp, ld_dx, ddtp, ld_ddt, dap, dbp, ld_db, dcp, ld_dc, dsp, dop,
+                                                        dhp, wk, size, _stream_of(dev)))
 
     def selective_scan_step(self, dtype: int, x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor, h: torch.Tensor,
                             h_out: torch.Tensor, y: torch.Tensor, skip: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None) -> None:
         """One row per sequence: the states h [rows][channels][states] moved on by the row, to h_out (may be h), and y."""
-        like, _, args = self._scan_check(dtype, x, dt, a, b, c, skip, dt_bias)
-        ld = _pitch(y, like, "y")
-        rows, (ch, m) = like[2][0], a.shape
-        _params_check(h, torch.float32, (rows, ch, m), "h")
-        _params_check(h_out, torch.float32, (rows, ch, m), "h_out")
-        self._chk(self.lib.emc2_selective_scan_step(*args, _at(h), rows, ch, m, _at(h_out), _at(y), ld, _raw_stream()))
+        dev, shape = self._current(), _shape_of(x)
+        td, (rows, ch), m = _TORCH_DTYPE[dtype], shape, a.shape[1] if a.dim() == 2 else 0
+        xp, ld_x, dtp, ld_dt, yp, ld_y = _rows_at(dev, td, shape, ("x", "dt", "y"), x, dt, y)
+        bp, ld_b, cp, ld_c = _rows_at(dev, td, torch.Size((rows, m)), ("b", "c"), b, c)
+        kept = (rows, ch, m)
+        ap, sp, op, hp, to = _floats_at(dev, (a, (ch, m), "a"), (skip, (ch,), "skip"), (dt_bias, (ch,), "dt_bias"), (h, kept, "h"), (h_out, kept, "h_out"))
+        self._chk(self.lib.emc2_selective_scan_step(self.h, dtype, xp, ld_x, dtp, ld_dt, ap, bp, ld_b, cp, ld_c, sp, op, hp, rows, ch, m, to, yp, ld_y,
+                                                    _stream_of(dev)))
