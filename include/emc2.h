@@ -4,7 +4,8 @@
  *   ->  point-to-image projection with bilinear feature gather,
  * and on the same data structures: inverse kernel map + bird's-eye-view flattening (decoder side),
  * Multiscale Pooling of image features + multimodal fusion, the scene dispatcher, an int8 sparse conv, and operators that mix
- * along the voxels of whole frames: layer norm, a gated linear recurrence, a gated feed-forward network, with their gradients.
+ * along the voxels of whole frames: layer norm, a gated linear recurrence, a gated feed-forward network, a short causal convolution, a selective state space
+ * scan and the gated residual with its norms, with their gradients.
  *
  * Conventions
  *   - Pointers named d_* are DEVICE pointers (HBM, on the context's device); h_* and plain
