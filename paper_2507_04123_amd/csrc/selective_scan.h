@@ -25,10 +25,12 @@ namespace {
 
 constexpr int kBatch = 8;                // rows under way together
 constexpr int kChunkWaves = 8;           // chunks side by side in a block of the launch that reduces them: a block's total stands for them ("span")
-// Chunks of a call times slices of its channels at most, and rows of a chunk at least: as many waves as the chip holds at once of the forward pass, and of the
-// gradients, whose waves have twice the registers (30,011 rows of 90 channels by 12 states in fp32: k_scan_grad 111 us with the forward pass' cut, 91 with its own).
-constexpr int kMaxChunks = 4096, kMinChunk = 16;
-constexpr int kMaxChunksGrad = 2048, kMinChunkGrad = 32;
+// Chunks of a call times slices of its channels at most: as many waves as the chip holds at once of the forward pass, and of the gradients, whose waves have
+// twice the registers (30,011 rows of 90 channels by 12 states in fp32: k_scan_grad 111 us with the forward pass' cut, 91 with its own).
+constexpr int kMaxChunks = 4096, kMaxChunksGrad = 2048;
+// A chunk has 16 rows at least, or 8 while that makes no more chunks than this, two waves a SIMD (128 channels by 16 states in bf16, 2000 rows forward and gradients
+// 35 and 69 us with 16 and 32 rows, 27 and 40 with 8; 12,000 rows forward 39 us with 8 rows, 35 with 16).
+constexpr int kFewChunks = 2048;
 constexpr int kMaxSpans = kMaxChunks / kChunkWaves;
 constexpr int kMaxStates = 64;
 
@@ -338,13 +340,14 @@ struct emc2_scan_plan {
   int64_t most;                          // chunks that no call of up to that many rows exceeds
 };
 static inline emc2_scan_plan emc2_plan_scan(int64_t capacity, int32_t channels, bool grad) {
-  const int64_t slices = emc2_div_up(channels, 64), all = grad ? kMaxChunksGrad : kMaxChunks, room = slices < all ? all / slices : 1;
-  const int64_t least = grad ? kMinChunkGrad : kMinChunk, per = emc2_div_up(capacity, room), some = emc2_div_up(capacity, least);
+  const int64_t slices = emc2_div_up(channels, 64), room = (grad ? kMaxChunksGrad : kMaxChunks) / slices, few = kFewChunks / slices;
+  const int64_t per = emc2_div_up(capacity, room), least = capacity <= few * kBatch ? kBatch : 2 * kBatch;
+  const int64_t eights = emc2_div_up(capacity, kBatch), sixteens = emc2_div_up(eights, 2);
   emc2_scan_plan p;
   p.chunk = (int32_t)(per < least ? least : emc2_div_up(per, kBatch) * kBatch);
   p.chunks = (int32_t)emc2_div_up(capacity, p.chunk);
   p.spans = (int32_t)emc2_div_up(p.chunks, kChunkWaves);
-  p.most = some < room ? some : room;
+  p.most = eights < few ? eights : sixteens < few ? few : sixteens < room ? sixteens : room;
   return p;
 }
 // Totals of chunks and spans in one direction, and what enters the spans: floats.
