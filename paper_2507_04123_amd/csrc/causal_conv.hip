@@ -87,17 +87,24 @@ __device__ __forceinline__ Reach reach(const Walk& w, int32_t lo, int32_t hi) {
   return r;
 }
 
-// The rows that sequences keep: one value a thread.  Row i of them (oldest first) is row length - (taps - 1) + i of the sequence, or one of those before it.
-template <typename T> __device__ __forceinline__ void keep_last(const ConvArgs& a, const Walk& w, int32_t taps) {
-  const int64_t all = (int64_t)a.n_seq * (taps - 1) * a.channels, step = (int64_t)(gridDim.x - a.row_blocks) * gridDim.y * kConvThreads;
+// The rows that sequences keep: a thread has a channel of a sequence.  Row i of them (oldest first) is row length - (TAPS - 1) + i of the sequence, or one of those
+// before it.
+template <typename T, int TAPS> __device__ __forceinline__ void keep_last(const ConvArgs& a, const Walk& w) {
+  const int64_t all = (int64_t)a.n_seq * a.channels, step = (int64_t)(gridDim.x - a.row_blocks) * gridDim.y * kConvThreads;
   for (int64_t i = (((int64_t)blockIdx.x - a.row_blocks) * gridDim.y + blockIdx.y) * kConvThreads + threadIdx.x; i < all; i += step) {
-    const int64_t line = i / a.channels;
-    const int32_t c = (int32_t)(i - line * a.channels), j = (int32_t)(line / (taps - 1)), k = (int32_t)(line - (int64_t)j * (taps - 1));
-    const int32_t start = w.start(j), at = max(w.start(j + 1) - start, 0) - (taps - 1) + k, seq = w.number(j);
-    float v = 0.0f;
-    if (at >= 0) v = (float)((const T*)a.x)[w.row(start + at) * a.ld_x + c];
-    else if (a.before) v = a.before[((int64_t)seq * (taps - 1) + at + taps - 1) * a.channels + c];
-    a.last[((int64_t)seq * (taps - 1) + k) * a.channels + c] = v;
+    const int32_t j = (int32_t)(i / a.channels), c = (int32_t)(i - (int64_t)j * a.channels), seq = w.number(j);
+    const int32_t start = w.start(j), length = max(w.start(j + 1) - start, 0);
+    const int64_t kept = (int64_t)seq * (TAPS - 1) * a.channels + c;
+    float v[TAPS - 1];
+#pragma unroll
+    for (int k = 0; k < TAPS - 1; ++k) {
+      const int32_t at = length - (TAPS - 1) + k;
+      v[k] = 0.0f;
+      if (at >= 0) v[k] = (float)((const T*)a.x)[w.row(start + at) * a.ld_x + c];
+      else if (a.before) v[k] = a.before[kept + (int64_t)(at + TAPS - 1) * a.channels];
+    }
+#pragma unroll
+    for (int k = 0; k < TAPS - 1; ++k) a.last[kept + (int64_t)k * a.channels] = v[k];
   }
 }
 
@@ -105,7 +112,7 @@ template <typename T, int N, int TAPS>
 __global__ void __launch_bounds__(kConvThreads) k_causal_conv(const ConvArgs a) {
   const Walk w(a.offsets, a.n_seq, a.capacity, a.backwards);
   report_rows(a.offsets, a.n_seq, a.capacity, a.flags);
-  if ((int32_t)blockIdx.x >= a.row_blocks) return keep_last<T>(a, w, TAPS);
+  if ((int32_t)blockIdx.x >= a.row_blocks) return keep_last<T, TAPS>(a, w);
   const int64_t block_row = (int64_t)blockIdx.x * a.runs_a_block * kRows;
   if (block_row >= w.n) return;
   const Lane<N> t(a);
@@ -157,33 +164,39 @@ __global__ void __launch_bounds__(kConvThreads) k_causal_conv(const ConvArgs a) 
   }
 }
 
-// dz of one value: row p of sequence j, whose rows begin at `start`.
-template <typename T> __device__ float dz_at(const ConvArgs& a, const Walk& w, int32_t taps, int32_t seq, int32_t start, int32_t p, int32_t c) {
-  const float dy = (float)((const T*)a.dy)[w.row(start + p) * a.ld_dy + c];
-  if (!a.silu) return dy;
-  float z = a.bias ? a.bias[c] : 0.0f;
-  for (int32_t k = 0; k < taps; ++k) {
-    float v = 0.0f;
-    if (p >= k) v = (float)((const T*)a.x)[w.row(start + p - k) * a.ld_x + c];
-    else if (a.before) v = a.before[((int64_t)seq * (taps - 1) + taps - 1 + p - k) * a.channels + c];
-    z += a.w[(int64_t)k * a.channels + c] * v;
-  }
-  return dy * silu_slope<sizeof(T) == 4, 1>(emc2_fvec<1>(z))[0];
-}
-// Gradients of the rows before the first: one value a thread.
-template <typename T> __device__ __forceinline__ void before_grad(const ConvArgs& a, const Walk& w, int32_t taps) {
-  const int64_t all = (int64_t)a.n_seq * (taps - 1) * a.channels, step = (int64_t)(gridDim.x - a.row_blocks) * gridDim.y * kConvThreads;
+// Gradients of the rows before the first: a thread has a channel of a sequence, whose first TAPS - 1 rows are all that they reach.
+template <typename T, int TAPS> __device__ __forceinline__ void before_grad(const ConvArgs& a, const Walk& w) {
+  const int64_t all = (int64_t)a.n_seq * a.channels, step = (int64_t)(gridDim.x - a.row_blocks) * gridDim.y * kConvThreads;
   for (int64_t i = (((int64_t)blockIdx.x - a.row_blocks) * gridDim.y + blockIdx.y) * kConvThreads + threadIdx.x; i < all; i += step) {
-    const int64_t line = i / a.channels;
-    const int32_t c = (int32_t)(i - line * a.channels), j = (int32_t)(line / (taps - 1)), row = (int32_t)(line - (int64_t)j * (taps - 1));
-    const int32_t start = w.start(j), length = max(w.start(j + 1) - start, 0), seq = w.number(j);
-    float v = 0.0f;
-    for (int32_t k = taps - 1 - row; k < taps; ++k) {        // row - (taps - 1) + k: rows of the sequence that it reaches
-      const int32_t p = row - (taps - 1) + k;
-      if (p < length) v += a.w[(int64_t)k * a.channels + c] * dz_at<T>(a, w, taps, seq, start, p, c);
+    const int32_t j = (int32_t)(i / a.channels), c = (int32_t)(i - (int64_t)j * a.channels), seq = w.number(j);
+    const int32_t start = w.start(j), length = max(w.start(j + 1) - start, 0);
+    const int64_t kept = (int64_t)seq * (TAPS - 1) * a.channels + c;
+    float x[2 * (TAPS - 1)], dz[TAPS - 1], taps[TAPS], v[TAPS - 1];   // x: the rows before, oldest first, and the first rows
+#pragma unroll
+    for (int k = 0; k < TAPS; ++k) taps[k] = a.w[(int64_t)k * a.channels + c];
+#pragma unroll
+    for (int p = 0; p < TAPS - 1; ++p) {
+      x[p] = a.before ? a.before[kept + (int64_t)p * a.channels] : 0.0f;
+      x[TAPS - 1 + p] = p < length ? (float)((const T*)a.x)[w.row(start + p) * a.ld_x + c] : 0.0f;
+      dz[p] = p < length ? (float)((const T*)a.dy)[w.row(start + p) * a.ld_dy + c] : 0.0f;
+      v[p] = a.dlast && p >= length ? a.dlast[kept + (int64_t)(p - length) * a.channels] : 0.0f;
     }
-    if (a.dlast && row >= length) v += a.dlast[((int64_t)seq * (taps - 1) + row - length) * a.channels + c];
-    a.dbefore[((int64_t)seq * (taps - 1) + row) * a.channels + c] = v;
+    if (a.silu) {
+      const float bias = a.bias ? a.bias[c] : 0.0f;
+#pragma unroll
+      for (int p = 0; p < TAPS - 1; ++p) {
+        float z = bias;
+#pragma unroll
+        for (int k = 0; k < TAPS; ++k) z += taps[k] * x[TAPS - 1 + p - k];
+        if (p < length) dz[p] *= silu_slope<sizeof(T) == 4, 1>(emc2_fvec<1>(z))[0];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < TAPS - 1; ++k) {                     // row k reaches rows p of the sequence, TAPS - 1 - k + p rows behind it
+#pragma unroll
+      for (int p = 0; p <= k; ++p) v[k] += p < length ? taps[TAPS - 1 - k + p] * dz[p] : 0.0f;
+      a.dbefore[kept + (int64_t)k * a.channels] = v[k];
+    }
   }
 }
 
@@ -262,7 +275,7 @@ __global__ void __launch_bounds__(kConvThreads) k_causal_conv_grad(const ConvArg
   __shared__ emc2_fvec<N> part[TAPS + 1][kConvThreads / 2];
   const Walk w(a.offsets, a.n_seq, a.capacity, a.backwards);
   report_rows(a.offsets, a.n_seq, a.capacity, a.flags);
-  if ((int32_t)blockIdx.x >= a.row_blocks) return before_grad<T>(a, w, TAPS);
+  if ((int32_t)blockIdx.x >= a.row_blocks) return before_grad<T, TAPS>(a, w);
   const Lane<N> t(a);
   emc2_fvec<N> taps[TAPS], bias = emc2_fvec<N>(0.0f), dw[TAPS], db = emc2_fvec<N>(0.0f);
 #pragma unroll
@@ -343,10 +356,10 @@ Plan plan_of(int whole, int32_t channels) {
 }
 int whole_forward(emc2_dtype dtype) { return dtype == EMC2_F32 ? 4 : 8; }
 constexpr int kWholeGrad = 4;
-// Blocks that write the states: eight values a thread, as many blocks as keep the chip busy at most.
-int64_t state_blocks(int32_t n_seq, int32_t taps, int32_t channels, int32_t slices, bool any) {
+// Blocks that write the states: a channel of a sequence a thread, as many blocks as keep the chip busy at most.
+int64_t state_blocks(int32_t n_seq, int32_t channels, int32_t slices, bool any) {
   if (!any) return 0;
-  const int64_t b = emc2_div_up((int64_t)n_seq * (taps - 1) * channels, (int64_t)kConvThreads * 8 * slices);
+  const int64_t b = emc2_div_up((int64_t)n_seq * channels, (int64_t)kConvThreads * slices);
   return b < 2048 ? b : 2048;
 }
 // Rows of a run: as many as leave every block that the chip holds at once its share, so that no second round of blocks runs half empty
@@ -416,7 +429,7 @@ extern "C" emc2_status emc2_causal_conv(emc2_ctx* ctx, emc2_dtype dtype, const v
   a.ld_x = ld_x, a.ld_y = ld_y, a.capacity = (int32_t)capacity, a.channels = channels, a.n_seq = n_seq, a.backwards = backwards != 0;
   a.silu = silu != 0, a.pieces = p.pieces, a.runs_a_block = p.runs;
   a.row_blocks = (int32_t)emc2_div_up(capacity, (int64_t)p.runs * kRows);
-  int64_t blocks = a.row_blocks + state_blocks(n_seq, taps, channels, p.slices, d_last);
+  int64_t blocks = a.row_blocks + state_blocks(n_seq, channels, p.slices, d_last);
   if (blocks == 0) a.row_blocks = 1, blocks = 1;           // a block that reports rows beyond the capacity
   const dim3 grid((unsigned)blocks, (unsigned)p.slices);
   with_type(dtype, [&](auto type) {
@@ -467,7 +480,7 @@ extern "C" emc2_status emc2_causal_conv_backward(emc2_ctx* ctx, emc2_dtype dtype
   a.capacity = (int32_t)capacity, a.channels = channels, a.n_seq = n_seq, a.backwards = backwards != 0, a.silu = silu != 0;
   a.pieces = p.pieces, a.runs_a_block = p.runs, a.run = run_of(capacity, p);
   a.row_blocks = (int32_t)grad_blocks(emc2_div_up(capacity, a.run), p);
-  const dim3 grid((unsigned)(a.row_blocks + state_blocks(n_seq, taps, channels, p.slices, d_dbefore)), (unsigned)p.slices);
+  const dim3 grid((unsigned)(a.row_blocks + state_blocks(n_seq, channels, p.slices, d_dbefore)), (unsigned)p.slices);
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
     with_taps(taps, [&](auto k) {
