@@ -453,7 +453,7 @@ extern "C" emc2_status emc2_selective_scan(emc2_ctx* ctx, emc2_dtype dtype, cons
   if (!emc2_results_ok(&y, 1, own, 2, capacity, size, true) || !emc2_results_ok(&y, 1, shared, 2, capacity, size, false))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_y overlaps d_b or d_c, or d_x or d_dt at another place or pitch", what);
   if (!emc2_apart(d_last, kept, d_h0, kept)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_last must not overlap d_h0", what);
-  const emc2_scan_plan p = emc2_plan_scan(capacity, channels, false);
+  const emc2_scan_plan p = emc2_plan_scan(capacity, channels, states, false);
   const bool small = capacity <= kShortRows;
   const int64_t need = small ? 0 : emc2_scan_totals_size(p.chunks, channels, states) * (int64_t)sizeof(float);
   if (work_bytes < need || (need && (!d_work || ((uintptr_t)d_work & 15))))

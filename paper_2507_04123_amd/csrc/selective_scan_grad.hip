@@ -273,8 +273,8 @@ int64_t grad_size(int64_t capacity, int64_t chunks, int32_t channels, int32_t st
 
 extern "C" int64_t emc2_selective_scan_work(emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t states) {
   if (!emc2_is_float(dtype) || channels < 1 || channels > (1 << 16) || states < 1 || states > kMaxStates || capacity < 0 || capacity > (1ll << 30)) return -1;
-  const int64_t forward = emc2_scan_totals_size(emc2_plan_scan(capacity, channels, false).most, channels, states),
-                grad = grad_size(capacity, emc2_plan_scan(capacity, channels, true).most, channels, states);
+  const int64_t forward = emc2_scan_totals_size(emc2_plan_scan(capacity, channels, states, false).most, channels, states),
+                grad = grad_size(capacity, emc2_plan_scan(capacity, channels, states, true).most, channels, states);
   return (forward > grad ? forward : grad) * (int64_t)sizeof(float);
 }
 
@@ -306,7 +306,7 @@ extern "C" emc2_status emc2_selective_scan_backward(
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: results overlap each other or inputs (only d_dx and d_ddt may lie where d_x, d_dt or d_dy do)", what);
   if (!emc2_apart(d_dh0, kept, d_dlast, kept) || !emc2_apart(d_dh0, kept, d_h0, kept))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_dh0 must not overlap d_dlast or d_h0", what);
-  const emc2_scan_plan p = emc2_plan_scan(capacity, channels, true);
+  const emc2_scan_plan p = emc2_plan_scan(capacity, channels, states, true);
   if (work_bytes < grad_size(capacity, p.chunks, channels, states) * (int64_t)sizeof(float) || !d_work || ((uintptr_t)d_work & 15))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: work buffer null, misaligned or smaller than emc2_selective_scan_work", what);
   ScanArgs a = {};
