@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libemc2.so")
 PROBE_LIB = os.path.join(HERE, "libemc2probe.so")     # measurement probes of the bench (include/emc2_probe.h)
-SOURCES = ["selective_scan.hip", "causal_conv.hip", "selective_scan_grad.hip", "ffn_grad.hip", "ffn.hip", "recurrence.hip",          # the longest compilations first
+SOURCES = ["selective_scan.hip", "selective_scan_totals.hip", "causal_conv.hip", "selective_scan_grad.hip", "ffn_grad.hip", "ffn.hip", "recurrence.hip",          # the longest compilations first
            "context.hip", "cellindex.hip", "voxelize.hip", "voxel_bins.hip", "kmap.hip", "spconv.hip", "spconv_mfma.hip", "spconv_narrow.hip", "spconv_span.hip",
            "spconv_direct.hip", "spconv_resident.hip", "project.hip", "decoder.hip", "pool.hip", "dispatch.hip", "spconv_i8.hip",
            "stack.hip", "layernorm.hip", "gated_residual.hip"]

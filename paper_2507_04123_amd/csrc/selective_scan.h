@@ -334,18 +334,36 @@ template <int S, int P> struct Form { static constexpr int s = S, p = P; };
 
 }  // namespace
 
-// How a call is cut (host): by the waves that a chunk's channels fill, of up to 32 states half as many channels a wave, of more a quarter (100,000 rows of 128 channels by
-// 32 states, gradients 556 us; cut as for 16 states 603).
+// Lanes a channel that walk long lists (host), and so states a lane.  Fewer states a lane are a shorter row, but more lanes repeat what belongs to the channel: it is best
+// while the chip is not full (128 channels by 16 states in bf16, forward and gradients: 2000 rows 26 and 40 us with one lane, 20 and 32 with four; 20,000 rows 50 and 97,
+// 43 and 88; 80,000 rows 90 and 242, 109 and 272) and wherever lanes would be idle otherwise (100,000 rows of 16 channels 75 and 131 us with one lane, 36 and 79 with four).
+constexpr int64_t kFewWaveRows = 160000;
+static inline int32_t emc2_scan_lanes(int64_t capacity, int32_t channels, int32_t states) {
+  const int32_t fewest = states <= 16 ? 1 : states <= 32 ? 2 : 4, most = states <= 4 ? 1 : states <= 8 ? 2 : 4;
+  constexpr int kCost[3] = {16, 10, 7};  // of a wave's row, with the fewest lanes and with twice and four times as many
+  int32_t best = fewest;
+  int64_t least = -1;
+  for (int32_t lanes = fewest, i = 0; lanes <= most; lanes *= 2, ++i) {
+    const int64_t slices = emc2_div_up((int64_t)channels * lanes, 64);
+    if (least < 0 || slices * kCost[i] < least) best = lanes, least = slices * kCost[i];
+    else if (capacity * slices <= kFewWaveRows) best = lanes;
+  }
+  return best;
+}
+
+// How a call is cut (host): by the waves that a chunk's channels fill (100,000 rows of 128 channels by 32 states, gradients 556 us; cut as for 16 states 603).
 struct emc2_scan_plan {
+  int32_t lanes;                         // a channel's
   int32_t chunk, chunks, spans;          // rows of a chunk; chunks and spans of the capacity
   int64_t most;                          // chunks that no call of up to that many rows exceeds
 };
 static inline emc2_scan_plan emc2_plan_scan(int64_t capacity, int32_t channels, int32_t states, bool grad) {
-  const int64_t slices = emc2_div_up((int64_t)channels * (states <= 16 ? 1 : states <= 32 ? 2 : 4), 64), all = grad ? kMaxChunksGrad : kMaxChunks;
+  emc2_scan_plan p;
+  p.lanes = emc2_scan_lanes(capacity, channels, states);
+  const int64_t slices = emc2_div_up((int64_t)channels * p.lanes, 64), all = grad ? kMaxChunksGrad : kMaxChunks;
   const int64_t room = slices < all ? all / slices : 1, few = slices < kFewChunks ? kFewChunks / slices : 1;
   const int64_t per = emc2_div_up(capacity, room), least = capacity <= few * kBatch ? kBatch : 2 * kBatch;
   const int64_t eights = emc2_div_up(capacity, kBatch), sixteens = emc2_div_up(eights, 2);
-  emc2_scan_plan p;
   p.chunk = (int32_t)(per < least ? least : emc2_div_up(per, kBatch) * kBatch);
   p.chunks = (int32_t)emc2_div_up(capacity, p.chunk);
   p.spans = (int32_t)emc2_div_up(p.chunks, kChunkWaves);

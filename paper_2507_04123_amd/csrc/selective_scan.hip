@@ -11,277 +11,9 @@
 // the vector units busy 84 and 88 % of the time; a row's 64 x 16 states take 108 and 131 issue slots, 80 and 96 of them for the recurrence (an exponential is two).  Rows
 // without sequence ends go in straight-line code without masks (an infinite gain excepted where lanes have states that are none); against one code for all rows 299 -> 273 us
 // for the call.  The sums over states on the small matrix instructions: 172 -> 211 us.  B and C read from LDS ahead of the exponentials: no change.
-#include "selective_scan.h"
+#include "selective_walk.h"
 
 namespace {
-
-enum { kTotals = 0, kGradTotals = 1, kRun = 2 };
-
-// Walks rows [row0, end) of a chunk, a wave alone, with LDS of its own (lds [2][kBatch][WIDTH]).  kTotals: h becomes what the chunk makes of it, sum the sum of its
-// steps and `begun` whether a sequence begins in it.  kGradTotals: also what flows out of the chunk towards earlier rows, from none behind it (flow), and whether
-// a sequence ends in it (ended); the states before every batch are written.  kRun: writes y and the last states.
-template <int MODE, typename T, int S, int P>
-__device__ __forceinline__ void walk(const ScanArgs& a, const Walk& w, const States<S, P>& t, const float (&a2)[S], int32_t row0, int32_t end, float* lds,
-                                     float (&h)[S], float& sum, bool& begun, float (&flow)[S], bool& ended) {
-  constexpr int kWidth = S * P, kArrays = MODE == kTotals ? 1 : 2, Q = Slots<P>::Q, R = Slots<P>::R;
-  constexpr bool kExact = sizeof(T) == 4;
-  const int q = t.part % Q;
-  Staged<T, kWidth, kArrays> bc;
-  constexpr bool kSoon = sizeof(T) == 2 || Staged<T, kWidth, kArrays>::kMine == 1;   // B and C are requested with the rows; wide ones, for lack of registers, when due
-  Column<T, P> x, v, dy;
-  const Line<const T> xs(w, (const T*)a.x, a.ld_x), vs(w, (const T*)a.dt, a.ld_dt), dys(w, (const T*)a.dy, a.ld_dy);
-  const Line<const T> bs(w, (const T*)a.b, a.ld_b), cs(w, (const T*)a.c, a.ld_c);
-  const Line<T> ys(w, (T*)a.y, a.ld_y);
-  const int32_t bytes = t.channel * (int32_t)sizeof(T);
-  bc.open(bs, cs, t.lane, 64);
-  const auto fetch = [&](int32_t r0) {
-    if constexpr (kSoon) bc.fetch(bs, cs, r0, end, a.states);
-    x.fetch(xs, bytes, q, r0, w.n);
-    v.fetch(vs, bytes, q, r0, w.n);
-    if constexpr (MODE == kGradTotals) dy.fetch(dys, bytes, q, r0, w.n);
-  };
-  fetch(row0);
-  const float bias = a.dt_bias ? a.dt_bias[t.channel] : 0.0f;
-  const float skip = MODE == kRun && a.skip ? a.skip[t.channel] : 0.0f;
-  const bool ragged = a.states != kWidth || __any(!t.in);
-  Cursor at;
-  at.open(w, row0, t.lane);
-  float decay[S];                                          // kGradTotals: of all rows so far
-  if constexpr (MODE == kGradTotals) {
-#pragma unroll
-    for (int s = 0; s < S; ++s) decay[s] = 1.0f, flow[s] = 0.0f;
-    ended = false;
-  }
-  for (int32_t r0 = row0; r0 < end; r0 += kBatch) {
-    if constexpr (!kSoon) bc.fetch(bs, cs, r0, end, a.states);
-    bc.put(lds);
-    float d[R], xv[R], y[R], dyv[R];
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      float slope;
-      step_of<kExact>((float)v.v[j] + bias, d[j], slope);
-      xv[j] = (float)x.v[j], y[j] = 0.0f, dyv[j] = 0.0f;
-      if constexpr (MODE == kGradTotals) dyv[j] = (float)dy.v[j];
-    }
-    fetch(r0 + kBatch < end ? r0 + kBatch : r0);           // (unconditional: what it replaces need not be kept for a second way)
-    if constexpr (MODE == kGradTotals) {
-      if (t.in) {
-        t.store(a, a.batch_h, r0 / kBatch, h);
-        if (t.part == 0) a.batch_s[(int64_t)(r0 / kBatch) * a.channels + t.channel] = begun ? -1.0f : sum;
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const Rows<P> y_rows(ys, bytes, q, r0, w.n);
-    // One row; returns what its states add to y.  PLAIN: it begins and ends no sequence, and its gain is finite where lanes have states that are none (an infinite
-    // gain stays out of those; a NaN is in the channel's other states too).  LIVE (kGradTotals): it adds to the flow; without PLAIN that is looked at here.
-    const auto row = [&](auto plain, auto live, int i, float di, float xi, float dyi) __attribute__((always_inline)) {
-      constexpr bool PLAIN = decltype(plain)::value, LIVE = decltype(live)::value;
-      const float gi = di * xi;
-      if (!PLAIN && r0 + i >= at.next) {                   // a sequence begins
-        at.locate(w, r0 + i, t.lane);
-        t.load_or_zero(a, a.h0, w.number(at.j), h);
-        begun = true;
-      }
-      float b[S], keep[S];
-      int32_t there = t.there;
-      if (!PLAIN && MODE == kGradTotals) asm volatile("" : "+v"(there));   // (compared anew in every row: masks kept for all would take the registers)
-      from_lds<S>(lds + i * kWidth + t.first, b);
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        b[s] *= gi;
-        if (!PLAIN) b[s] = s < there ? b[s] : 0.0f;
-        keep[s] = __builtin_amdgcn_exp2f(di * a2[s]);
-        h[s] = __builtin_fmaf(keep[s], h[s], b[s]);
-      }
-      float all = 0.0f;
-      if constexpr (MODE != kRun) {
-        sum += di;
-#pragma unroll
-        for (int s = 0; s < S; ++s) row_ends_with(h[s]);
-      }
-      if constexpr (MODE == kGradTotals) {
-        if (PLAIN ? LIVE : !ended) {
-          float c[S];
-          from_lds<S>(lds + (kBatch + i) * kWidth + t.first, c);
-#pragma unroll
-          for (int s = 0; s < S; ++s) {
-            decay[s] *= keep[s];
-            flow[s] = __builtin_fmaf(decay[s], c[s] * dyi, flow[s]);
-            row_ends_with(flow[s]);
-          }
-          if (!PLAIN && r0 + i + 1 >= at.next) {           // a sequence ends
-            float l[S];
-            t.load_or_zero(a, a.dlast, w.number(at.j), l);
-#pragma unroll
-            for (int s = 0; s < S; ++s) flow[s] = __builtin_fmaf(decay[s], l[s], flow[s]);
-            ended = true;
-          }
-        }
-      }
-      if constexpr (MODE == kRun) {
-        float c[S], part[4] = {Q == 1 && a.skip ? skip * xi : 0.0f, 0.0f, 0.0f, 0.0f};
-        from_lds<S>(lds + (kBatch + i) * kWidth + t.first, c);
-#pragma unroll
-        for (int s = 0; s < S; ++s) part[s & 3] = __builtin_fmaf(c[s], h[s], part[s & 3]);
-        all = lane_sum<P>((part[0] + part[1]) + (part[2] + part[3]));
-        if constexpr (Q == 1) {
-          if (t.in) y_rows.template store<T>(i, q, (T)all);
-        }
-        if (!PLAIN && r0 + i + 1 >= at.next && a.last && t.in) t.store(a, a.last, w.number(at.j), h);
-      }
-      return all;
-    };
-    const auto rows = [&](auto live) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const float di = a_row<1 + decltype(live)::value>(of_row<P>(d, i));
-        const float all = row(Yes(), live, i, di, of_row<P>(xv, i), MODE == kGradTotals ? of_row<P>(dyv, i) : 0.0f);
-        if constexpr (MODE == kRun && Q > 1) {
-          y[i / Q] = q == i % Q ? all : y[i / Q];
-          row_ends_with(y[i / Q]);
-        }
-      }
-    };
-    bool plain = r0 + kBatch <= end && r0 + kBatch < at.next;
-    if (plain && ragged) {
-      float gain[R];
-#pragma unroll
-      for (int j = 0; j < R; ++j) gain[j] = d[j] * xv[j];
-      plain = !any_infinite(gain);
-    }
-    if (plain) {
-      if (MODE == kGradTotals && !ended) rows(Yes());
-      else rows(No());
-    } else if constexpr (MODE != kGradTotals) {
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        if (r0 + i >= end) break;
-        const float di = a_row<0>(of_row<P>(d, i)), all = row(No(), No(), i, di, of_row<P>(xv, i), 0.0f);
-        if constexpr (MODE == kRun && Q > 1) y[i / Q] = q == i % Q ? all : y[i / Q];
-      }
-    } else {
-      // In one copy of the row's code, which leaves registers for decays and flows: the lane's values move down behind each row; after all of them they are
-      // where they were.
-#pragma unroll 1
-      for (int i = 0; i < kBatch; ++i) {
-        if (r0 + i < end) {
-          const auto mine = [&](float v) { return Q == 1 ? v : __shfl(v, (t.lane & ~(Q - 1)) | (i & (Q - 1)), 64); };
-          row(No(), No(), i, a_row<0>(mine(d[0])), mine(xv[0]), mine(dyv[0]));
-        }
-        if ((i & (Q - 1)) == Q - 1) {
-          const float d0 = d[0], x0 = xv[0], dy0 = dyv[0];
-#pragma unroll
-          for (int j = 0; j + 1 < R; ++j) d[j] = d[j + 1], xv[j] = xv[j + 1], dyv[j] = dyv[j + 1];
-          d[R - 1] = d0, xv[R - 1] = x0, dyv[R - 1] = dy0;
-        }
-      }
-    }
-    if constexpr (MODE == kRun && Q > 1) {
-      if (t.in && t.part < Q) {
-#pragma unroll
-        for (int j = 0; j < R; ++j)
-          if (j * Q + q < end - r0) y_rows.template store<T>(j, q, (T)(a.skip ? __builtin_fmaf(skip, xv[j], y[j]) : y[j]));
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  }
-}
-
-// First launch: every chunk from a state of zeros, and what spans of eight chunks make of it.  Block (span, slice of the channels), a wave a chunk.
-template <bool GRAD, typename T, int S, int P> __global__ void __launch_bounds__(64 * kChunkWaves, GRAD ? 2 : 4) k_scan_totals(const ScanArgs a) {
-  constexpr int kWidth = S * P, kOwn = (GRAD ? 2 : 1) * kBatch * kWidth, kLine = 64 * S;   // a wave's LDS; its total
-  __shared__ float lds[kChunkWaves * (kOwn > kLine ? kOwn : kLine)];
-  __shared__ float sums[kChunkWaves][64];
-  const Walk w(a.offsets, a.n_seq, a.capacity, a.backwards);
-  report_rows(a.offsets, a.n_seq, a.capacity, a.flags);
-  const States<S, P> t(a, blockIdx.y);
-  const int64_t k = (int64_t)blockIdx.x * kChunkWaves + t.wave, row0 = k * a.chunk;
-  if ((int64_t)blockIdx.x * kChunkWaves * a.chunk >= w.n) return;
-  float a2[S], h[S], flow[S], sum = 0.0f;
-  bool begun = false, ended = false;
-  decays(a, t, a2);
-#pragma unroll
-  for (int s = 0; s < S; ++s) h[s] = 0.0f, flow[s] = 0.0f;
-  if (row0 < w.n)
-    walk<GRAD ? kGradTotals : kTotals, T, S, P>(a, w, t, a2, (int32_t)row0, row0 + a.chunk < w.n ? (int32_t)row0 + a.chunk : w.n, lds + t.wave * kOwn, h, sum,
-                                                begun, flow, ended);
-#pragma unroll
-  for (int dir = 0; dir < (GRAD ? 2 : 1); ++dir) {
-    const float s0 = (dir == 0 ? begun : ended) ? -1.0f : sum;
-    const float(&mine)[S] = dir == 0 ? h : flow;
-    __syncthreads();                                       // all waves are through with their rows, or the direction before
-#pragma unroll
-    for (int s = 0; s < S; ++s) lds[(t.wave * S + s) * 64 + t.lane] = mine[s];
-    sums[t.wave][t.lane] = s0;
-    __syncthreads();
-    // what the chunks before this one make together, in the order of the direction; behind the last of them, the span
-    float all[S], total = 0.0f;
-#pragma unroll
-    for (int s = 0; s < S; ++s) all[s] = 0.0f;
-    const int before = dir == 0 ? t.wave : kChunkWaves - 1 - t.wave;
-    for (int m = 0; m < before; ++m) {
-      const int from = dir == 0 ? m : kChunkWaves - 1 - m;
-      float v[S];
-#pragma unroll
-      for (int s = 0; s < S; ++s) v[s] = lds[(from * S + s) * 64 + t.lane];
-      const float one = sums[from][t.lane];
-      through<S>(a2, one, v, all);
-      total = one < 0.0f ? -1.0f : total < 0.0f ? total : total + one;
-    }
-    if (t.in && row0 < w.n) {
-      t.store(a, a.chunk_h[dir], k, all);
-      if (t.part == 0) a.chunk_s[dir][k * a.channels + t.channel] = total;
-    }
-    if (before == kChunkWaves - 1 && t.in) {
-      through<S>(a2, s0, mine, all);
-      t.store(a, a.span_h[dir], blockIdx.x, all);
-      if (t.part == 0) a.span_s[dir][(int64_t)blockIdx.x * a.channels + t.channel] = s0 < 0.0f ? -1.0f : total < 0.0f ? total : total + s0;
-    }
-  }
-}
-
-// Second launch: what enters every span.  A block has 32 states of the line [channels][states] and 32 runs of spans; a thread composes its run and, from what
-// enters it, walks it again, out of registers.  blockIdx.y: the direction.
-constexpr int kRuns = 32, kRunSpans = kMaxSpans / kRuns;
-__global__ void __launch_bounds__(32 * kRuns) k_scan_enter(const ScanArgs a) {
-  __shared__ float part_p[kRuns][33], part_h[kRuns][33];
-  const int32_t rows = a.offsets[a.n_seq], n = rows < 0 ? 0 : rows < a.capacity ? rows : a.capacity;
-  const int32_t spans = spans_of(a, n).spans, per = (spans + kRuns - 1) / kRuns;
-  const int col = threadIdx.x & 31, run = threadIdx.x >> 5, dir = blockIdx.y;
-  const int64_t line = (int64_t)a.channels * a.states, at = (int64_t)blockIdx.x * 32 + col, mine = at < line ? at : line - 1;
-  const float* const span_s = dir == 0 ? a.span_s[0] : a.span_s[1];
-  const float* const span_h = dir == 0 ? a.span_h[0] : a.span_h[1];
-  float* const enter = dir == 0 ? a.enter[0] : a.enter[1];
-  const float a2 = a.a[mine] * kLog2e;
-  const int32_t c = (int32_t)(mine / a.states), from = run * per;
-  float p[kRunSpans], h[kRunSpans];
-#pragma unroll
-  for (int i = 0; i < kRunSpans; ++i) {
-    const int32_t m = from + i;
-    const bool there = i < per && m < spans;
-    const int64_t span = there ? (dir == 0 ? m : spans - 1 - m) : 0;
-    p[i] = there ? span_s[span * a.channels + c] : 0.0f;
-    h[i] = there ? span_h[span * line + mine] : 0.0f;
-  }
-  // products of decays; a run in which a sequence begins has -1
-  float all_p = 1.0f, all_h = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kRunSpans; ++i) {
-    p[i] = p[i] < 0.0f ? -1.0f : __builtin_amdgcn_exp2f(a2 * p[i]);
-    all_h = p[i] < 0.0f ? h[i] : __builtin_fmaf(p[i], all_h, h[i]);
-    all_p = p[i] < 0.0f || all_p < 0.0f ? -1.0f : all_p * p[i];
-  }
-  part_p[run][col] = all_p, part_h[run][col] = all_h;
-  __syncthreads();
-  float state = 0.0f;
-  for (int m = 0; m < run; ++m) state = part_p[m][col] < 0.0f ? part_h[m][col] : __builtin_fmaf(part_p[m][col], state, part_h[m][col]);
-#pragma unroll
-  for (int i = 0; i < kRunSpans; ++i) {
-    const int32_t m = from + i;
-    if (i < per && m < spans && at < line) enter[(int64_t)(dir == 0 ? m : spans - 1 - m) * line + at] = state;
-    state = p[i] < 0.0f ? h[i] : __builtin_fmaf(p[i], state, h[i]);
-  }
-}
 
 // Third launch: the rows.  Blocks as in the first; those behind them deal with sequences without rows.
 template <typename T, int S, int P> __global__ void __launch_bounds__(64 * kChunkWaves, 4) k_scan(const ScanArgs a) {
@@ -382,14 +114,7 @@ __global__ void __launch_bounds__(kStepThreads) k_scan_step(const ScanArgs a, co
   if (first == 0) ((T*)a.y + row * a.ld_y)[c] = (T)(a.skip ? y + a.skip[c] * x : y);
 }
 
-// States a lane and lanes a channel: many rows 16 states a lane (few lanes repeat what belongs to the channel), short calls four (short chains).
-template <typename F> void with_form(int32_t states, F&& f) {
-  if (states <= 4) return f(Form<4, 1>());
-  if (states <= 8) return f(Form<8, 1>());
-  if (states <= 16) return f(Form<16, 1>());
-  if (states <= 32) return f(Form<16, 2>());
-  f(Form<16, 4>());
-}
+// Short calls have four states a lane (short chains).
 template <typename F> void with_short_form(int32_t states, F&& f) {
   if (states <= 4) return f(Form<4, 1>());
   if (states <= 8) return f(Form<4, 2>());
@@ -413,23 +138,6 @@ emc2_status emc2_scan_check(emc2_ctx* ctx, const char* what, emc2_dtype dtype, i
   if (states < 1 || states > kMaxStates) return emc2_fail(ctx, EMC2_ERR_UNSUPPORTED, "%s: states outside [1, %d]", what, kMaxStates);
   if (capacity < 0 || capacity > (1ll << 30)) return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: rows outside [0, 2^30]", what);
   return EMC2_OK;
-}
-
-void emc2_scan_totals(const ScanArgs& a, emc2_dtype dtype, const emc2_scan_plan& p, bool grad, hipStream_t stream) {
-  with_type(dtype, [&](auto type) {
-    using T = decltype(type);
-    const auto launch = [&](auto form, auto both) {
-      using F = decltype(form);
-      hipLaunchKernelGGL((k_scan_totals<decltype(both)::value, T, F::s, F::p>), dim3((unsigned)p.spans, (unsigned)emc2_div_up(a.channels, 64 / F::p)),
-                         dim3(64 * kChunkWaves), 0, stream, a);
-    };
-    with_form(a.states, [&](auto form) {
-      if (grad) launch(form, Yes());
-      else launch(form, No());
-    });
-  });
-  if (p.spans > 1)
-    hipLaunchKernelGGL(k_scan_enter, dim3((unsigned)emc2_div_up((int64_t)a.channels * a.states, 32), grad ? 2u : 1u), dim3(32 * kRuns), 0, stream, a);
 }
 
 extern "C" emc2_status emc2_selective_scan(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_dt, int64_t ld_dt,
@@ -486,7 +194,7 @@ extern "C" emc2_status emc2_selective_scan(emc2_ctx* ctx, emc2_dtype dtype, cons
   emc2_scan_totals(a, dtype, p, false, s);
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    with_form(states, [&](auto form) {
+    with_form(states, p.lanes, [&](auto form) {
       using F = decltype(form);
       const int32_t slices = (int32_t)emc2_div_up(channels, 64 / F::p);
       const dim3 grid((unsigned)(p.spans + hand_on_blocks(n_seq, slices, d_last)), (unsigned)slices);

@@ -242,18 +242,18 @@ template <typename T> __global__ void __launch_bounds__(kSumThreads) k_scan_grad
   else ((T*)a.db + w.row((int32_t)r) * a.ld_db)[n] = (T)all;
 }
 
-template <typename F> void with_grad_form(int32_t states, F&& f) {
+template <typename F> void with_grad_form(int32_t states, int32_t lanes, F&& f) {
   if (states <= 4) return f(Form<4, 1>());
   if (states <= 8) return f(Form<4, 2>());
-  if (states <= 16) return f(Form<8, 2>());
+  if (states <= 16) return lanes == 4 ? f(Form<4, 4>()) : f(Form<8, 2>());
   if (states <= 32) return f(Form<8, 4>());
   f(Form<8, 8>());
 }
 // Slices of the channels, waves of a block, blocks side by side.
 struct Cut { int32_t slices, waves, parts; };
-Cut cut_of(int32_t channels, int32_t states) {
+Cut cut_of(int32_t channels, int32_t states, int32_t lanes) {
   Cut c;
-  with_grad_form(states, [&](auto form) {
+  with_grad_form(states, lanes, [&](auto form) {
     using F = decltype(form);
     c.slices = (int32_t)emc2_div_up(channels, 64 / F::p);
     const int32_t most = grad_waves(F::s * F::p);
@@ -262,19 +262,22 @@ Cut cut_of(int32_t channels, int32_t states) {
   });
   return c;
 }
+int64_t shared_size(int64_t capacity, int32_t states, int64_t parts) { return parts > 1 ? parts * capacity * 2 * states : 0; }
 // Floats of scratch: totals of both directions, states before batches, weights' sums, sums of dB and dC.
-int64_t grad_size(int64_t capacity, int64_t chunks, int32_t channels, int32_t states) {
-  const int64_t lines = chunks > 1 ? chunks : 1, parts = cut_of(channels, states).parts;
+int64_t grad_size(int64_t capacity, int64_t chunks, int32_t channels, int32_t states, int64_t shared) {
   return 2 * emc2_scan_totals_size(chunks, channels, states) + emc2_div_up(capacity, kBatch) * channels * (states + 1) +
-         lines * channels * (states + 2) + (parts > 1 ? parts * capacity * 2 * states : 0);
+         (chunks > 1 ? chunks : 1) * channels * (states + 2) + shared;
 }
 
 }  // namespace
 
 extern "C" int64_t emc2_selective_scan_work(emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t states) {
   if (!emc2_is_float(dtype) || channels < 1 || channels > (1 << 16) || states < 1 || states > kMaxStates || capacity < 0 || capacity > (1ll << 30)) return -1;
-  const int64_t forward = emc2_scan_totals_size(emc2_plan_scan(capacity, channels, states, false).most, channels, states),
-                grad = grad_size(capacity, emc2_plan_scan(capacity, channels, states, true).most, channels, states);
+  const int64_t forward = emc2_scan_totals_size(emc2_plan_scan(capacity, channels, states, false).most, channels, states);
+  const emc2_scan_plan p = emc2_plan_scan(capacity, channels, states, true);
+  // fewer rows may have more lanes a channel, and so more parts to sum
+  const int64_t few = kFewWaveRows / emc2_div_up((int64_t)channels * 4, 64), narrow = shared_size(capacity < few ? capacity : few, states, cut_of(channels, states, 4).parts),
+                now = shared_size(capacity, states, cut_of(channels, states, p.lanes).parts), grad = grad_size(capacity, p.most, channels, states, narrow > now ? narrow : now);
   return (forward > grad ? forward : grad) * (int64_t)sizeof(float);
 }
 
@@ -307,7 +310,8 @@ extern "C" emc2_status emc2_selective_scan_backward(
   if (!emc2_apart(d_dh0, kept, d_dlast, kept) || !emc2_apart(d_dh0, kept, d_h0, kept))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_dh0 must not overlap d_dlast or d_h0", what);
   const emc2_scan_plan p = emc2_plan_scan(capacity, channels, states, true);
-  if (work_bytes < grad_size(capacity, p.chunks, channels, states) * (int64_t)sizeof(float) || !d_work || ((uintptr_t)d_work & 15))
+  const Cut cut = cut_of(channels, states, p.lanes);
+  if (work_bytes < grad_size(capacity, p.chunks, channels, states, shared_size(capacity, states, cut.parts)) * (int64_t)sizeof(float) || !d_work || ((uintptr_t)d_work & 15))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: work buffer null, misaligned or smaller than emc2_selective_scan_work", what);
   ScanArgs a = {};
   a.x = d_x, a.dt = d_dt, a.b = d_b, a.c = d_c, a.dy = d_dy, a.a = d_a, a.skip = d_skip, a.dt_bias = d_dt_bias, a.h0 = d_h0, a.dlast = d_dlast;
@@ -321,12 +325,11 @@ extern "C" emc2_status emc2_selective_scan_backward(
   a.partial = place, place += (int64_t)a.row_blocks * channels * (states + 2);
   a.partial_bc = place;
   hipStream_t s = (hipStream_t)stream;
-  const Cut cut = cut_of(channels, states);
   if (capacity > 0) emc2_scan_totals(a, dtype, p, true, s);
   const int64_t more = d_dh0 ? emc2_div_up(n_seq, 16ll * cut.parts) : 0;
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    with_grad_form(states, [&](auto form) {
+    with_grad_form(states, p.lanes, [&](auto form) {
       using F = decltype(form);
       const dim3 grid((unsigned)(a.row_blocks + (more < 1024 ? more : 1024)), (unsigned)cut.parts);
       hipLaunchKernelGGL((k_scan_grad<T, F::s, F::p>), grid, dim3((unsigned)(64 * cut.waves)),
