@@ -598,7 +598,8 @@ emc2_status emc2_causal_conv_step(emc2_ctx* ctx, emc2_dtype dtype, const void* d
  *   D_t[c] = log(1 + exp(dt_t[c] + dt_bias[c]));  h_t[c][n] = exp(D_t[c] a[c][n]) h_{t-1}[c][n] + D_t[c] x_t[c] B_t[n]
  *   y_t[c] = sum over n of C_t[n] h_t[c][n] + skip[c] x_t[c]
  * Sequences, d_offsets and `backwards` as for emc2_recurrence.  d_x, d_dt, d_y rows of `channels` values, d_b and d_c of `states`, which all channels share (several
- * groups of channels with their own B and C: one call each).  d_a [channels][states], usually negative; d_skip and d_dt_bias [channels], NULL = 0.
+ * groups of channels with their own B and C: one call each).  d_a [channels][states], usually negative (of positive ones, exp(a times the sum of a sequence's steps) has
+ * to stay within fp32: products of decays are formed apart from the states); d_skip and d_dt_bias [channels], NULL = 0.
  * d_h0 [n_seq][channels][states] states before the first row, NULL = zeros; d_last receives the states after the last (an empty sequence's is its d_h0), NULL to
  * skip.  States are fp32 throughout, and a sequence's reach no other sequence.  channels in [1, 65536], states in [1, 64]; rows at most 2^26 values apart (the
  * one-row form: any distance).

@@ -195,6 +195,8 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 4 : 2) k_gated_residual_gra
   }
 }
 
+// Lanes of a row at least (500,000 rows of 16 bf16 values forward and backward 29 and 63 us with eight, 16 and 30 with two).
+constexpr int kLeastLanes = 2;
 // Blocks of the backward pass, each walking the rows in steps of all blocks: as many as the chip holds at once with the registers of 16-bit rows.  A few more
 // run alone at the end: 240,001 rows of 128 bf16 values 102 us (4.8 TB/s) with 1024, 108 with 1792, 114 with 1536, 134 with 1280; fp32 rows, whose kernels
 // leave room for more blocks, 205 us with any of these.  60,000 rows of 1000 bf16 values: 267 us with 512, 335 with 768.
@@ -235,7 +237,7 @@ extern "C" emc2_status emc2_gated_residual(emc2_ctx* ctx, emc2_dtype dtype, cons
   a.x = d_x, a.branch = d_branch, a.gate = d_gate, a.post = d_post, a.scale = d_scale, a.next = d_next, a.d_n = d_n, a.sum = d_sum, a.y = d_y;
   a.ld_x = ld_x, a.ld_branch = ld_branch, a.ld_gate = ld_gate, a.ld_sum = ld_sum, a.ld_y = ld_y, a.capacity = capacity, a.channels = channels;
   a.eps = eps, a.inv_channels = 1.0f / (float)channels;
-  with_type(dtype, shape_of(dtype, channels), [&](auto form, auto type) {
+  with_type<kLeastLanes>(dtype, shape_of(dtype, channels, kLeastLanes), [&](auto form, auto type) {
     using F = decltype(form);
     using T = decltype(type);
     constexpr int U = F::u > 1 ? F::u / 2 : 1;             // three operands of each row
@@ -284,7 +286,7 @@ extern "C" emc2_status emc2_gated_residual_backward(
   a.ld_dgate = ld_dgate, a.capacity = capacity, a.channels = channels, a.eps = eps, a.inv_channels = 1.0f / (float)channels;
   hipStream_t s = (hipStream_t)stream;
   int64_t blocks = 1;
-  with_type(dtype, shape_of(dtype, channels), [&](auto form, auto type) {
+  with_type<kLeastLanes>(dtype, shape_of(dtype, channels, kLeastLanes), [&](auto form, auto type) {
     using F = decltype(form);
     using T = decltype(type);
     blocks = emc2_div_up(capacity, kThreads / F::l * 2);

@@ -33,12 +33,12 @@ template <int N, int L, int V, bool MOVED> struct Places {
   }
 };
 
-// How the rows of a call lie over the lanes: vectors of 16 bytes, single values where a row has not even one.
+// How the rows of a call lie over the lanes, `least` of them at least: vectors of 16 bytes, single values where a row has not even one.
 struct Shape { bool wide, moved; int lanes, vectors; };
-Shape shape_of(emc2_dtype dtype, int32_t channels) {
+Shape shape_of(emc2_dtype dtype, int32_t channels, int least = 8) {
   const int whole = dtype == EMC2_F32 ? 4 : 8, per = channels >= whole ? whole : 1;
   const int pieces = (channels + per - 1) / per;
-  int lanes = 8;
+  int lanes = least;
   while (lanes < 64 && lanes < pieces) lanes *= 2;
   int vectors = 1;
   while (vectors * lanes < pieces) vectors *= 2;
@@ -51,7 +51,11 @@ template <int N, int L, int V, int U, bool MOVED = false> struct Form {
   static constexpr int n = N, l = L, v = V, u = U;
   static constexpr bool moved = MOVED;
 };
-template <int N, bool MOVED, typename F> void with_form(const Shape& s, F&& f) {
+template <int N, bool MOVED, int LEAST, typename F> void with_form(const Shape& s, F&& f) {
+  if constexpr (LEAST <= 2) {
+    if (s.lanes == 2) return f(Form<N, 2, 1, 4, MOVED>());
+    if (s.lanes == 4) return f(Form<N, 4, 1, 4, MOVED>());
+  }
   switch (s.lanes) {
     case 8: return f(Form<N, 8, 1, 4, MOVED>());
     case 16: return f(Form<N, 16, 1, 4, MOVED>());
@@ -63,17 +67,17 @@ template <int N, bool MOVED, typename F> void with_form(const Shape& s, F&& f) {
   }
   if constexpr (N == 4) return f(Form<N, 64, 4, 1, MOVED>());
 }
-template <typename T, typename F> void with_type(const Shape& s, F&& f) {
+template <typename T, int LEAST, typename F> void with_type(const Shape& s, F&& f) {
   constexpr int N = 16 / sizeof(T);
   const auto with_T = [&](auto form) { f(form, T()); };
   if (!s.wide) with_T(Form<1, 8, 1, 4>());
-  else if (s.moved) with_form<N, true>(s, with_T);
-  else with_form<N, false>(s, with_T);
+  else if (s.moved) with_form<N, true, LEAST>(s, with_T);
+  else with_form<N, false, LEAST>(s, with_T);
 }
-template <typename F> void with_type(emc2_dtype dtype, const Shape& s, F&& f) {
-  if (dtype == EMC2_F32) with_type<float>(s, f);
-  else if (dtype == EMC2_F16) with_type<_Float16>(s, f);
-  else with_type<__bf16>(s, f);
+template <int LEAST = 8, typename F> void with_type(emc2_dtype dtype, const Shape& s, F&& f) {
+  if (dtype == EMC2_F32) with_type<float, LEAST>(s, f);
+  else if (dtype == EMC2_F16) with_type<_Float16, LEAST>(s, f);
+  else with_type<__bf16, LEAST>(s, f);
 }
 
 }  // namespace

@@ -136,3 +136,31 @@ def test_refusals(ctx):
             back(**bad)
     with pytest.raises(ValueError):
         back(work=w[:-4])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("c", [2, 4, 5, 7, 9, 11, 12, 13, 15, 18, 20, 24, 27, 31, 32, 33])
+def test_narrow_rows(ctx, dtype, c):
+    """Rows that two and four lanes hold, in whole vectors and with a last one moved back."""
+    test_forward(ctx, dtype, c)
+    test_backward(ctx, dtype, c)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_more_narrow_rows_than_all_blocks_hold_at_once(ctx, dtype):
+    n, c = 140001, 12
+    p = _case(3, n, c, dtype)
+    dsum, dy = draw(4, n, c, dtype=dtype), draw(5, n, c, dtype=dtype)
+    g, total, y = _forward(ctx, p, dtype, "packed")
+    args = _oracle(p)
+    for got, exp, bound in zip((total, y), V.gated_residual(*args), L.gated_residual(*args, dtype)):
+        within(got, exp, bound, "forward")
+    out = {k: like(p["x"], "packed") for k in ("dx", "dbranch", "dgate")}
+    out.update({k: torch.full((size,), 9.0, device="cuda") for k, size in (("dpost", c), ("dscale", 1), ("dnext", c))})
+    ctx.gated_residual_backward(DT[dtype], g["x"], g["branch"], g["post"], g["scale"], 1e-5, dsum.cuda(), out["dx"], out["dbranch"], out["dpost"], out["dscale"],
+                                work(ctx.gated_residual_work(DT[dtype], n, c)), gate=g["gate"], dgate=out["dgate"], next_gain=g["next"], dy=dy.cuda(),
+                                dnext=out["dnext"])
+    args += [f64(dsum), f64(dy)]
+    exp, bound = V.gated_residual_backward(*args), L.gated_residual_backward(*args, dtype)
+    for k in exp:
+        within(out[k], exp[k], bound[k], k)
