@@ -354,7 +354,9 @@ Plan plan_of(int whole, int32_t channels) {
   p.runs = kConvThreads / p.pieces;
   return p;
 }
-int whole_forward(emc2_dtype dtype) { return dtype == EMC2_F32 ? 4 : 8; }
+// Values a piece: 16 bytes, half of that where eight taps of as many values would leave registers for one wave a SIMD (613,217 rows of 96 f16 values: 54 us, 84 with
+// whole pieces; six taps 51 and 47).
+constexpr int whole_forward(size_t size, int32_t taps) { return size == 4 || taps == kMaxTaps ? 4 : 8; }
 constexpr int kWholeGrad = 4;
 // Blocks that write the states: a channel of a sequence a thread, as many blocks as keep the chip busy at most.
 int64_t state_blocks(int32_t n_seq, int32_t channels, int32_t slices, bool any) {
@@ -423,7 +425,7 @@ extern "C" emc2_status emc2_causal_conv(emc2_ctx* ctx, emc2_dtype dtype, const v
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: null or misaligned rows, or a pitch below the channels", what);
   if (!emc2_apart({d_y, ld_y, channels}, {d_x, ld_x, channels}, capacity, size) || !emc2_apart(d_last, kept, d_before, kept))
     return emc2_fail(ctx, EMC2_ERR_INVALID_ARG, "%s: d_y must not overlap d_x, nor d_last d_before", what);
-  const Plan p = plan_of(whole_forward(dtype), channels);
+  const Plan p = plan_of(whole_forward(size, taps), channels);
   ConvArgs a = {};
   a.x = d_x, a.w = d_w, a.bias = d_bias, a.before = d_before, a.offsets = d_offsets, a.y = d_y, a.last = d_last, a.flags = ctx->dev_words;
   a.ld_x = ld_x, a.ld_y = ld_y, a.capacity = (int32_t)capacity, a.channels = channels, a.n_seq = n_seq, a.backwards = backwards != 0;
@@ -435,7 +437,7 @@ extern "C" emc2_status emc2_causal_conv(emc2_ctx* ctx, emc2_dtype dtype, const v
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
     with_taps(taps, [&](auto k) {
-      constexpr int K = decltype(k)::k, N = 16 / sizeof(T);
+      constexpr int K = decltype(k)::k, N = whole_forward(sizeof(T), K);
       if (p.n > 1) hipLaunchKernelGGL((k_causal_conv<T, N, K>), grid, dim3(kConvThreads), 0, (hipStream_t)stream, a);
       else hipLaunchKernelGGL((k_causal_conv<T, 1, K>), grid, dim3(kConvThreads), 0, (hipStream_t)stream, a);
     });
