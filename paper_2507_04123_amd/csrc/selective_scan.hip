@@ -123,8 +123,9 @@ template <typename F> void with_short_form(int32_t states, F&& f) {
   f(Form<4, 16>());
 }
 
-// Rows up to which one block a slice deals with all: 128 channels by 16 states in bf16, 400 rows 20 us in one launch, 25 in three; 600 rows 29 and 26; 1000 rows 42 and 26.
-constexpr int64_t kShortRows = 512;
+// Rows up to which one block a slice deals with all: 128 channels by 16 states in bf16, 200 rows 14 us in one launch, 19 in three; 320 rows 20 and 19; 512 rows 25 and 19
+// (64 channels by 64 states, 384 rows 24 and 25).
+constexpr int64_t kShortRows = 320;
 int64_t hand_on_blocks(int32_t n_seq, int32_t slices, bool any) {
   const int64_t b = any ? emc2_div_up(n_seq, 16ll * slices) : 0;
   return b < 1024 ? b : 1024;
