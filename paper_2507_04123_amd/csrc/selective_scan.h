@@ -300,7 +300,7 @@ template <int DIR, int S, typename Lanes>
 __device__ __forceinline__ void entering(const ScanArgs& a, const Lanes& t, const float (&a2)[S], int32_t k, const Spans& q, float (&h)[S]) {
   float v[S];
   t.load(a, a.chunk_h[DIR] + (int64_t)k * a.channels * a.states, v);
-  const float s = a.chunk_s[DIR][(int64_t)k * a.channels + t.channel];
+  const float s = t.in ? a.chunk_s[DIR][(int64_t)k * a.channels + t.channel] : 0.0f;
   if (q.spans > 1) t.load(a, a.enter[DIR] + (int64_t)(k / kChunkWaves) * a.channels * a.states, h);
   else {
 #pragma unroll

@@ -67,7 +67,7 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
     entering<0, S>(a, t, a2, blockIdx.x, spans, enter);
     entering<1, S>(a, t, a2, blockIdx.x, spans, flow);
     const float bias = a.dt_bias ? a.dt_bias[t.channel] : 0.0f, skip = a.skip ? a.skip[t.channel] : 0.0f;
-    const bool ragged = a.states != kWidth || __any(!t.in);
+    const bool idle = __any(!t.in), ragged = a.states != kWidth || idle;
     Cursor at;
     Staged<T, kWidth, 2> bc;
     constexpr bool kSoon = Staged<T, kWidth, 2>::kMine <= 2;   // B and C are requested with the rows; wide ones, which would take 16 registers, when they are due
@@ -100,9 +100,15 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
 #pragma unroll
       for (int j = 0; j < R; ++j) {
         step_of<kExact>((float)v.v[j] + bias, d[j], slope[j]);
-        xv[j] = (float)x.v[j];
-        dyv[j] = t.in ? (float)dy.v[j] : 0.0f;
+        xv[j] = (float)x.v[j], dyv[j] = (float)dy.v[j];
         gb[j] = 0.0f, dd[j] = 0.0f;
+      }
+      // Lanes without a channel, which take part in the sums over channels, have rows of zeros: what they have read is channel 0's, and another block may be writing
+      // its gradients there.
+      if (idle && !t.in) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) d[j] = 0.0f, xv[j] = 0.0f, dyv[j] = 0.0f;
+        before_s = 0.0f;
       }
 #pragma unroll
       for (int s = 0; s < S; ++s) h[s] = enter[s];

@@ -135,7 +135,7 @@ __device__ __forceinline__ void walk(const ScanArgs& a, const Walk& w, const Sta
     if (plain && ragged) {
       float gain[R];
 #pragma unroll
-      for (int j = 0; j < R; ++j) gain[j] = d[j] * xv[j];
+      for (int j = 0; j < R; ++j) gain[j] = t.in ? d[j] * xv[j] : 0.0f;   // (lanes without a channel read channel 0's rows, which another block may be writing)
       plain = !any_infinite(gain);
     }
     if (plain) {
