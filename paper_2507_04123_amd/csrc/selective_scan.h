@@ -275,11 +275,12 @@ template <typename T, int P> struct Column {
   }
 };
 
-// A times log2(e): the rows' decays are powers of two.
+// A times log2(e): the rows' decays are powers of two.  States that are none have any value below 0: their decays end with an infinite step as all others do (0 would make
+// them NaN), so that they stay 0.
 template <int S, typename Lanes> __device__ __forceinline__ void decays(const ScanArgs& a, const Lanes& t, float (&a2)[S]) {
   t.load(a, a.a, a2);
 #pragma unroll
-  for (int s = 0; s < S; ++s) a2[s] *= kLog2e;
+  for (int s = 0; s < S; ++s) a2[s] = s < t.there ? a2[s] * kLog2e : -1.0f;
 }
 
 // `h` behind a run of rows that multiply a state by exp(A s) and add `t`; s < 0: a sequence begins in the run, and nothing from before it is left.

@@ -8,10 +8,10 @@ from oracle import selective as V
 from paper_2507_04123_amd import binding as B
 
 import selective_bounds as L
-from selective_helpers import DT, TYPES, draw, f64, offsets, work
+from selective_helpers import TYPES, offsets, work
+from selective_infinite import GRADS, case, oracle, run, same_kind
 
 pytestmark = pytest.mark.gpu
-GRADS = ("dx", "ddt", "da", "db", "dc", "dskip", "ddt_bias", "dh0")
 
 
 @pytest.fixture(scope="module")
@@ -22,46 +22,6 @@ def ctx():
     c.close()
 
 
-def _case(lens, c, m, dtype):
-    """States that remember hundreds of rows, B and C above 0: an infinite state has one sign."""
-    n, s = sum(lens), len(lens)
-    p = {"x": draw(1, n, c, dtype=dtype), "dt": draw(2, n, c, scale=0.5, dtype=dtype), "b": draw(3, n, m, dtype=dtype).abs() + 0.25,
-         "c": draw(4, n, m, dtype=dtype).abs() + 0.25, "dy": draw(5, n, c, dtype=dtype), "a": -torch.exp(draw(6, c, m, scale=0.5, shift=-3.0)).float(),
-         "skip": draw(7, c), "dt_bias": torch.full((c,), -4.0), "h0": draw(8, s, c, m), "dlast": draw(9, s, c, m)}
-    return p
-
-
-def _run(ctx, dtype, p, dev, backwards):
-    """(y, last, gradients), nothing in place."""
-    g = {k: t.cuda() for k, t in p.items()}
-    n, c = g["x"].shape
-    w = work(ctx.selective_scan_work(DT[dtype], n, c, g["a"].shape[1]))
-    args = [g[k] for k in ("x", "dt", "a", "b", "c")]
-    kw = dict(skip=g["skip"], dt_bias=g["dt_bias"], backwards=backwards, h0=g["h0"])
-    y, last = torch.empty_like(g["x"]), torch.empty_like(g["h0"])
-    ctx.selective_scan(DT[dtype], *args, dev, y, w, last=last, **kw)
-    out = {k: torch.empty_like(g[q]) for k, q in zip(GRADS, ("x", "dt", "a", "b", "c", "skip", "dt_bias", "h0"))}
-    ctx.selective_scan_backward(DT[dtype], *args, dev, g["dy"], *[out[k] for k in ("dx", "ddt", "da", "db", "dc")], w, dskip=out["dskip"],
-                                ddt_bias=out["ddt_bias"], dlast=g["dlast"], dh0=out["dh0"], **kw)
-    return y, last, out
-
-
-def _oracle(p, off, backwards):
-    e = {k: f64(t) for k, t in p.items()}
-    args = [e[k] for k in ("x", "dt", "a", "b", "c")] + [off] + [e[k] for k in ("h0", "skip", "dt_bias")]
-    return args, args + [e["dy"], e["dlast"], backwards]
-
-
-def _same_kind(got, exp, bound, what):
-    """NaN where the formula gives NaN, an infinity where it gives that one; the finite values within the bound."""
-    got = f64(got)
-    assert np.array_equal(np.isnan(got), np.isnan(exp)), what
-    inf = np.isinf(exp)
-    assert np.array_equal(np.isinf(got), inf) and np.array_equal(got[inf], exp[inf]), what
-    ok = np.isfinite(exp)
-    assert (np.abs(got[ok] - exp[ok]) <= bound[ok]).all(), what
-
-
 # An infinite value or step in one row of channel 0.  What the formula leaves finite does not depend on the value, nor on a step beyond some thousands, whose decays
 # are 0: the bounds are taken from such a call.
 @pytest.mark.parametrize("dtype", TYPES)
@@ -70,23 +30,23 @@ def _same_kind(got, exp, bound, what):
 def test_infinite_rows_of_channel_0(ctx, dtype, lens, what, finite):
     off, dev = offsets(lens)
     for c, m, at, backwards in ((9, 16, 11, False), (9, 16, 16, True), (5, 4, 8, False), (70, 32, 21, False)):
-        p = _case(lens, c, m, dtype)
+        p = case(lens, c, m, dtype)
         row = int(off[1]) + at
         p["x"][row, 0] = 2.0
         p[what][row, 0] = finite
-        args, grads = _oracle(p, off, backwards)
+        args, grads = oracle(p, off, backwards)
         by, bl = L.selective_scan(*args, backwards, dtype)
         bound = L.selective_scan_backward(*grads, dtype)
         p[what][row, 0] = float("inf")
-        y, last, out = _run(ctx, dtype, p, dev, backwards)
-        args, grads = _oracle(p, off, backwards)
+        y, last, out = run(ctx, dtype, p, dev, backwards)
+        args, grads = oracle(p, off, backwards)
         with np.errstate(invalid="ignore"):
             ey, el = V.selective_scan(*args, backwards)
             exp = V.selective_scan_backward(*grads)
-        _same_kind(y, ey, by, "y")
-        _same_kind(last, el, bl, "last")
+        same_kind(y, ey, by, "y")
+        same_kind(last, el, bl, "last")
         for k in GRADS:
-            _same_kind(out[k], exp[k], bound[k], (k, c, m))
+            same_kind(out[k], exp[k], bound[k], (k, c, m))
         assert np.isinf(exp["db"][row]).all() and np.isfinite(np.delete(exp["db"], row, 0)).all() and np.isinf(ey[row, 0])
 
 
@@ -95,9 +55,9 @@ def test_infinite_rows_of_channel_0(ctx, dtype, lens, what, finite):
 @pytest.mark.parametrize("c,m,lens", [(265, 16, [300, 0, 211]), (290, 16, [40, 33]), (265, 16, [21000]), (45, 64, [100, 77]), (300, 30, [500])])
 def test_results_in_place_of_several_blocks(ctx, c, m, lens):
     off, dev = offsets(lens)
-    p = _case(lens, c, m, "f16")
+    p = case(lens, c, m, "f16")
     p["skip"][0] = 1e6                                                       # channel 0: dx and y beyond the type's range
-    y, last, want = _run(ctx, "f16", p, dev, False)
+    y, last, want = run(ctx, "f16", p, dev, False)
     assert torch.isinf(want["dx"][:, 0]).any() and torch.isinf(y[:, 0]).any()
     assert all(torch.isfinite(want[k]).all() for k in GRADS[1:]) and torch.isfinite(want["dx"][:, 1:]).all() and torch.isfinite(y[:, 1:]).all()
     g = {k: t.cuda() for k, t in p.items()}
