@@ -49,7 +49,7 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
   constexpr bool kKeep = S == 4;                           // decays stay in registers, too; otherwise they are made again
   constexpr int kWidth = S * P, kPair = 2 * kBatch * kWidth, Q = Slots<P>::Q, R = Slots<P>::R;
   constexpr bool kExact = sizeof(T) == 4;
-  extern __shared__ float lds[];                           // B and C of two batches [2][kPair], then the waves' sums for two batches [2][waves][kPair]
+  extern __shared__ float lds[];                           // B and C of two batches [2][kPair], zeros [kPair], then the waves' sums for two batches [2][waves][kPair]
   const Walk w(a.offsets, a.n_seq, a.capacity, a.backwards);
   if ((int32_t)blockIdx.x >= a.row_blocks) return hand_on(a, w, a.dlast, a.dh0);
   const int waves = blockDim.x >> 6;
@@ -87,6 +87,7 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
       before_s = a.batch_s[(int64_t)(r0 / kBatch) * a.channels + t.channel];
     };
     const int32_t last = row0 + (end - row0 - 1) / kBatch * kBatch;
+    for (int i = threadIdx.x; i < kPair; i += blockDim.x) lds[2 * kPair + i] = 0.0f;
     fetch(last);
     at.fill(w, w.n_seq < 64 ? 0 : w.find(last, t.lane) - 31, t.lane);
     if constexpr (!kSoon) bc.fetch(bs, cs, last, end, a.states);
@@ -94,8 +95,8 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
     __syncthreads();
     for (int32_t r0 = last; r0 >= row0; r0 -= kBatch) {
       const int turn = r0 / kBatch & 1;
-      const float* const now = lds + turn * kPair + t.first;
-      float* const sums = lds + 2 * kPair + (turn * waves + t.wave) * kPair + t.first + kept_state<S>(t.lane);
+      const float* const now = lds + (t.in ? turn : 2) * kPair + t.first;
+      float* const sums = lds + 3 * kPair + (turn * waves + t.wave) * kPair + t.first + kept_state<S>(t.lane);
       float d[R], xv[R], dyv[R], slope[R], gb[R], dd[R], h[S];
 #pragma unroll
       for (int j = 0; j < R; ++j) {
@@ -103,8 +104,8 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
         xv[j] = (float)x.v[j], dyv[j] = (float)dy.v[j];
         gb[j] = 0.0f, dd[j] = 0.0f;
       }
-      // Lanes without a channel, which take part in the sums over channels, have rows of zeros: what they have read is channel 0's, and another block may be writing
-      // its gradients there.
+      // Lanes without a channel, which take part in the sums over channels, have rows of zeros, B and C too: what they have read is channel 0's, and another block may
+      // be writing its gradients there.
       if (idle && !t.in) {
 #pragma unroll
         for (int j = 0; j < R; ++j) d[j] = 0.0f, xv[j] = 0.0f, dyv[j] = 0.0f;
@@ -214,7 +215,7 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
         const int n = e % kWidth, i = e / kWidth % kBatch, which = e / (kWidth * kBatch);
         const int32_t r = r0 + i;
         float all = 0.0f;
-        for (int m = 0; m < waves; ++m) all += lds[2 * kPair + (turn * waves + m) * kPair + e];
+        for (int m = 0; m < waves; ++m) all += lds[3 * kPair + (turn * waves + m) * kPair + e];
         if (n < a.states && r < end) {
           if (gridDim.y > 1) a.partial_bc[(((int64_t)blockIdx.y * a.capacity + r) * 2 + which) * a.states + n] = all;
           else if (which == 0) ((T*)a.db + w.row(r) * a.ld_db)[n] = (T)all;
@@ -339,7 +340,7 @@ extern "C" emc2_status emc2_selective_scan_backward(
       using F = decltype(form);
       const dim3 grid((unsigned)(a.row_blocks + (more < 1024 ? more : 1024)), (unsigned)cut.parts);
       hipLaunchKernelGGL((k_scan_grad<T, F::s, F::p>), grid, dim3((unsigned)(64 * cut.waves)),
-                         (size_t)((2 + 2 * cut.waves) * 2 * kBatch * F::s * F::p * sizeof(float)), s, a);
+                         (size_t)((3 + 2 * cut.waves) * 2 * kBatch * F::s * F::p * sizeof(float)), s, a);
     });
     if (cut.parts > 1 && capacity > 0)
       hipLaunchKernelGGL((k_scan_grad_bc<T>), emc2_grid(emc2_div_up(capacity * 2 * states, kSumThreads)), dim3(kSumThreads), 0, s, a, cut.parts);
