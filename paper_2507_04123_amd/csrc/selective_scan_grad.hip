@@ -51,6 +51,7 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
   constexpr bool kExact = sizeof(T) == 4;
   extern __shared__ float lds[];                           // B and C of two batches [2][kPair], zeros [kPair], then the waves' sums for two batches [2][waves][kPair]
   const Walk w(a.offsets, a.n_seq, a.capacity, a.backwards);
+  if (a.capacity == 0) report_rows(a.offsets, a.n_seq, a.capacity, a.flags);   // (otherwise the totals' launch has done so)
   if ((int32_t)blockIdx.x >= a.row_blocks) return hand_on(a, w, a.dlast, a.dh0);
   const int waves = blockDim.x >> 6;
   const States<S, P> t(a, blockIdx.y * waves + (threadIdx.x >> 6));
