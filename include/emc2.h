@@ -601,10 +601,11 @@ emc2_status emc2_causal_conv_step(emc2_ctx* ctx, emc2_dtype dtype, const void* d
  * groups of channels with their own B and C: one call each).  d_a [channels][states], usually negative (of positive ones, exp(a times the sum of a sequence's steps) has
  * to stay within fp32: products of decays are formed apart from the states); d_skip and d_dt_bias [channels], NULL = 0.
  * d_h0 [n_seq][channels][states] states before the first row, NULL = zeros; d_last receives the states after the last (an empty sequence's is its d_h0), NULL to
- * skip.  States are fp32 throughout, and a sequence's reach no other sequence.  channels in [1, 65536], states in [1, 64]; rows at most 2^26 values apart (the
- * one-row form: any distance).
+ * skip.  States are fp32 throughout, and a sequence's reach no other sequence.  What is infinite or NaN in x, dt, B or a state stays in the state to the end of its
+ * sequence: an infinity as such while the product of the decays since is above 0 in fp32, then as NaN; an infinite step forgets what came before (exp(-infinity) = 0).
+ * channels in [1, 65536], states in [1, 64]; rows at most 2^26 values apart (the one-row form: any distance).
  * d_y may lie where d_x or d_dt does (as d_dx and d_ddt below may where d_x, d_dt or d_dy do); d_last must not overlap d_h0, nor d_dh0 d_h0 or d_dlast.
- * Other overlaps are refused.
+ * Other overlaps of rows, and of states, are refused.
  */
 int64_t emc2_selective_scan_work(emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t states);
 emc2_status emc2_selective_scan(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_dt, int64_t ld_dt, const float* d_a,
@@ -631,7 +632,7 @@ emc2_status emc2_selective_scan_step(emc2_ctx* ctx, emc2_dtype dtype, const void
  * norm before the next block:
  *   sum = x + scale * act * rms(branch) * post;   y = rms(sum) * next;   rms(v) = v / sqrt(mean of v^2 + eps), act = gate / (1 + exp(-gate))
  * d_gate NULL: act = 1.  d_post, d_next [channels]; d_scale one value.  d_next and d_y NULL: the sum only (behind the last block).  y is taken from the sum
- * before that is rounded.  channels in [1, 1024].
+ * before that is rounded.  Squares are summed in fp32: of values beyond 5e17 the norm is 0.  channels in [1, 1024].
  */
 emc2_status emc2_gated_residual(emc2_ctx* ctx, emc2_dtype dtype, const void* d_x, int64_t ld_x, const void* d_branch, int64_t ld_branch,
                                 const void* d_gate, int64_t ld_gate, const float* d_post, const float* d_scale, const float* d_next, float eps,

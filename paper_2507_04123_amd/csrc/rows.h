@@ -1,5 +1,5 @@
 // Rows of 32- and 16-bit floating-point values, read and written in vectors and computed with in fp32: what the kernels of the
-// sequence operators (layernorm.hip, recurrence.hip, ffn.hip, ffn_grad.hip) share.
+// sequence and selective operators (layernorm.hip, recurrence.hip, ffn.hip, ffn_grad.hip, causal_conv.hip, gated_residual.hip, selective_scan*.hip) share.
 #pragma once
 #include "common.h"
 

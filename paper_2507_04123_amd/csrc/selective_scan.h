@@ -1,4 +1,4 @@
-// What the kernels of the selective scan (selective_scan.hip, selective_scan_grad.hip) share: how states lie over lanes, the rows' way into registers and
+// What the kernels of the selective scan (selective_scan.hip, selective_scan_totals.hip, selective_scan_grad.hip) share: how states lie over lanes, the rows' way into registers and
 // LDS, steps and decays, and the totals of runs of rows.
 #pragma once
 #include "lane_sums.h"
@@ -18,7 +18,7 @@ struct emc2_scan_args {
   int32_t* flags;
   int64_t ld_x, ld_dt, ld_b, ld_c, ld_dy, ld_y, ld_ddt, ld_db, ld_dc;
   int32_t capacity, channels, states, n_seq, backwards;
-  int32_t chunk, row_blocks, totals;           // rows of a chunk; blocks that walk rows; whether a first launch was needed
+  int32_t chunk, row_blocks;                   // rows of a chunk; blocks that walk rows
 };
 
 namespace {
@@ -26,7 +26,8 @@ namespace {
 constexpr int kBatch = 8;                // rows under way together
 constexpr int kChunkWaves = 8;           // chunks side by side in a block of the launch that reduces them: a block's total stands for them ("span")
 // Chunks of a call times slices of its channels at most: as many waves as the chip holds at once of the forward pass, and of the gradients, whose waves have
-// twice the registers (30,011 rows of 90 channels by 12 states in fp32: k_scan_grad 111 us with the forward pass' cut, 91 with its own).
+// twice the registers (forward and gradients with the forward pass' cut and with its own: 200,003 rows of 128 channels by 16 states in bf16 783 and 747 us, 30,011 rows of
+// 90 channels by 12 states in fp32 215 and 217).
 constexpr int kMaxChunks = 4096, kMaxChunksGrad = 2048;
 // A chunk has 16 rows at least, or 8 while that makes no more chunks than this, two waves a SIMD (128 channels by 16 states in bf16, 2000 rows forward and gradients
 // 35 and 69 us with 16 and 32 rows, 27 and 40 with 8; 12,000 rows forward 39 us with 8 rows, 35 with 16).
@@ -289,20 +290,19 @@ template <int S> __device__ __forceinline__ void through(const float (&a2)[S], f
   for (int i = 0; i < S; ++i) h[i] = s < 0.0f ? t[i] : __builtin_fmaf(__builtin_amdgcn_exp2f(a2[i] * s), h[i], t[i]);
 }
 
-// One direction of what a block's chunks make of a state together: chunk after chunk, in the order of the direction.
-struct Spans { int32_t spans, chunks; };
-__device__ __forceinline__ Spans spans_of(const ScanArgs& a, int32_t n) {
+// Spans that n rows make.
+__device__ __forceinline__ int32_t spans_of(const ScanArgs& a, int32_t n) {
   const int32_t chunks = (int32_t)(((int64_t)n + a.chunk - 1) / a.chunk);
-  return {(chunks + kChunkWaves - 1) / kChunkWaves, chunks};
+  return (chunks + kChunkWaves - 1) / kChunkWaves;
 }
 
 // The state that enters chunk `k` (direction 0), or the flow that enters it from later rows (1): what enters its span, behind the chunks of the span before it.
 template <int DIR, int S, typename Lanes>
-__device__ __forceinline__ void entering(const ScanArgs& a, const Lanes& t, const float (&a2)[S], int32_t k, const Spans& q, float (&h)[S]) {
+__device__ __forceinline__ void entering(const ScanArgs& a, const Lanes& t, const float (&a2)[S], int32_t k, int32_t spans, float (&h)[S]) {
   float v[S];
   t.load(a, a.chunk_h[DIR] + (int64_t)k * a.channels * a.states, v);
   const float s = t.in ? a.chunk_s[DIR][(int64_t)k * a.channels + t.channel] : 0.0f;
-  if (q.spans > 1) t.load(a, a.enter[DIR] + (int64_t)(k / kChunkWaves) * a.channels * a.states, h);
+  if (spans > 1) t.load(a, a.enter[DIR] + (int64_t)(k / kChunkWaves) * a.channels * a.states, h);
   else {
 #pragma unroll
     for (int i = 0; i < S; ++i) h[i] = 0.0f;
@@ -385,7 +385,7 @@ static inline float* emc2_place_totals(ScanArgs& a, int dir, float* at, const em
   a.span_s[dir] = at, at += p.spans * c;
   return at;
 }
-// Launches the reduction of chunks and what enters the spans (selective_scan.hip); `grad`: of both directions, with the states before every batch.
+// Launches the reduction of chunks and what enters the spans (selective_scan_totals.hip); `grad`: of both directions, with the states before every batch.
 void emc2_scan_totals(const ScanArgs& a, emc2_dtype dtype, const emc2_scan_plan& p, bool grad, hipStream_t stream);
 // Refuses what both directions refuse.
 emc2_status emc2_scan_check(emc2_ctx* ctx, const char* what, emc2_dtype dtype, int64_t capacity, int32_t channels, int32_t states);

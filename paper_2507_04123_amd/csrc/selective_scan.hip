@@ -7,8 +7,8 @@
 // a chunk, and nothing from one reaches another.
 // A lane holds S states of a channel and walks rows one after the other; x and dt of the next rows are on their way in registers, B and C, which all channels
 // share, pass through LDS as floats.  The order of composition is fixed: equal inputs give equal bits.  States are fp32.
-// The issue of vector instructions bounds both walks of long lists: 613,217 rows of 64 channels by 16 states in f16 take the totals 134 us, k_scan 161 us, with
-// the vector units busy 84 and 88 % of the time; a row's 64 x 16 states take 108 and 131 issue slots, 80 and 96 of them for the recurrence (an exponential is two).  Rows
+// The issue of vector instructions bounds both walks of long lists: 613,217 rows of 64 channels by 16 states in f16 take the totals 137 us, k_scan 167 us, with
+// the vector units busy 85 and 88 % of the time; a row's 64 x 16 states take 108 and 131 issue slots, 80 and 96 of them for the recurrence (an exponential is two).  Rows
 // without sequence ends go in straight-line code without masks (an infinite gain excepted where lanes have states that are none); against one code for all rows 299 -> 273 us
 // for the call.  The sums over states on the small matrix instructions: 172 -> 211 us.  B and C read from LDS ahead of the exponentials: no change.
 #include "selective_walk.h"
@@ -123,8 +123,10 @@ template <typename F> void with_short_form(int32_t states, F&& f) {
   f(Form<4, 16>());
 }
 
-// Rows up to which one block a slice deals with all: 128 channels by 16 states in bf16, 200 rows 14 us in one launch, 19 in three; 320 rows 20 and 19; 512 rows 25 and 19
-// (64 channels by 64 states, 384 rows 24 and 25).
+// Rows up to which one block a slice deals with all.  us of the GPU in one launch and in three (of a call alone from Python, which issues one in 10 and three in 15),
+// bf16: 128 channels by 16 states, 256 rows 15.5 and 16.7 (34 and 36), 288 rows 17.0 and 16.3, 320 rows 19.2 and 16.8 (38 and 36), 512 rows 24 and 17 (43 and 36); 64 by 64,
+// 320 rows 20 and 24 (38 and 44), 448 rows 26 and 24; 2048 by 16, 320 rows 20 and 39, 512 rows 26 and 44.  So up to 16 states the two meet at about 280 rows (alone:
+// 310), with more states or thousands of channels later; the constant lies between.
 constexpr int64_t kShortRows = 320;
 int64_t hand_on_blocks(int32_t n_seq, int32_t slices, bool any) {
   const int64_t b = any ? emc2_div_up(n_seq, 16ll * slices) : 0;

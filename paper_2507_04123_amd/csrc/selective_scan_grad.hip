@@ -2,14 +2,14 @@
 //   g_t = C_t dy_t + a_{t+1} g_{t+1} (+ dlast behind the last row), a = exp(D A): the gradient of the state h_t
 //   dC_t = sum over channels of dy h_t;  dB_t = sum over channels of g D x;  dx = skip dy + D sum over states of g B
 //   dD = sum over states of (g a h_{t-1}) A + x sum of g B;  ddt = dD softplus';  dA = sum over rows of g a h_{t-1} D;  dskip = sum of dy x;  dh0 = a_1 g_1
-// g runs against h with the same factors.  The first launch (selective_scan.hip) walks every chunk of rows once for the totals of both directions and writes the
+// g runs against h with the same factors.  The first launch (selective_scan_totals.hip) walks every chunk of rows once for the totals of both directions and writes the
 // state before every eight rows; the second finds what enters the spans of chunks from either side; the third (k_scan_grad) walks a chunk's batches of eight
 // rows from the last to the first: forward through a batch, whose states stay in registers, then back through it with the decays made again.  Nothing is kept from the forward pass.
 // A block has up to eight waves, all with the same rows, each with a slice of the channels: sums over channels, dB and dC, are taken over a wave's lanes by
 // swaps that halve the number of values with every step, over the waves through LDS.  Wider rows have several such blocks, whose sums are added in a last launch.
 // Weights' gradients stay in registers along a chunk and are added over chunks by halves.  No atomics, no order that may change: equal inputs give equal bits.
-// Vector issue bounds it: 200,003 rows of 128 channels by 16 states in bf16 take the first launch 149 us, k_scan_grad 416 us, 237 issue slots a row of 32 channels, the units
-// busy 76 % of the time at the two waves a SIMD that a batch's states leave room for.  Eight states a lane with the decays kept beside them: one wave, 538 us; four states
+// Vector issue bounds it: 200,003 rows of 128 channels by 16 states in bf16 take the first launch 147 us, k_scan_grad 413 us, 237 issue slots a row of 32 channels (the recurrence
+// about 130 of them, its decays made twice included; the sums over channels about 40), the units busy 76 % of the time at the two waves a SIMD that a batch's states leave room for.  Eight states a lane with the decays kept beside them: one wave, 538 us; four states
 // a lane: 528 us, for what belongs to the channel is repeated in more lanes.
 #include "column_sums.h"
 #include "selective_scan.h"
@@ -64,7 +64,7 @@ template <typename T, int S, int P> __global__ void __launch_bounds__(64 * grad_
   for (int s = 0; s < S; ++s) dA[s] = 0.0f;
   if (first < w.n) {
     const int32_t row0 = (int32_t)first, end = first + a.chunk < w.n ? row0 + a.chunk : w.n;
-    const Spans spans = spans_of(a, w.n);
+    const int32_t spans = spans_of(a, w.n);
     entering<0, S>(a, t, a2, blockIdx.x, spans, enter);
     entering<1, S>(a, t, a2, blockIdx.x, spans, flow);
     const float bias = a.dt_bias ? a.dt_bias[t.channel] : 0.0f, skip = a.skip ? a.skip[t.channel] : 0.0f;

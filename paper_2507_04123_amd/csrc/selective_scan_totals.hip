@@ -62,7 +62,7 @@ constexpr int kRuns = 32, kRunSpans = kMaxSpans / kRuns;
 __global__ void __launch_bounds__(32 * kRuns) k_scan_enter(const ScanArgs a) {
   __shared__ float part_p[kRuns][33], part_h[kRuns][33];
   const int32_t rows = a.offsets[a.n_seq], n = rows < 0 ? 0 : rows < a.capacity ? rows : a.capacity;
-  const int32_t spans = spans_of(a, n).spans, per = (spans + kRuns - 1) / kRuns;
+  const int32_t spans = spans_of(a, n), per = (spans + kRuns - 1) / kRuns;
   const int col = threadIdx.x & 31, run = threadIdx.x >> 5, dir = blockIdx.y;
   const int64_t line = (int64_t)a.channels * a.states, at = (int64_t)blockIdx.x * 32 + col, mine = at < line ? at : line - 1;
   const float* const span_s = dir == 0 ? a.span_s[0] : a.span_s[1];

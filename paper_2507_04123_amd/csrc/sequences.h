@@ -1,4 +1,4 @@
-// Sequences of packed rows as a kernel walks them (causal_conv.hip, selective_scan.hip).
+// Sequences of packed rows as a kernel walks them (causal_conv.hip, selective_scan*.hip).
 #pragma once
 #include "common.h"
 

@@ -6,7 +6,8 @@
 
     [x' B C] = silu(conv([x B C])),  s = scan(x', dt, B, C),  total = residual + scale silu(z) rms(s) post,  y = rms(total) next
 
-between the caller's projections: rows [z x B C dt] of one product of the block's input go in, y is the next one's input.
+behind the caller's projection: rows [z x B C dt] of one product of the block's input go in, y is the input of the next block's.  There is no projection behind
+the scan; a layer that has one takes convolution and scan, and makes silu(z) s and its product itself.
 
 A 3x3x3 convolution sees 27 cells; the recurrence and the scan carry a state along a frame's whole voxel list (ascending key), from its first voxel to
 its last or backwards.  As in ``pipeline``, only call order and buffers live here: everything is allocated once, ``run``, ``backward`` and
